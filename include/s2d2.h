@@ -378,6 +378,71 @@ int s2d2_gemm_bf16_noalloc(const void* d_x, const void* d_w, float* d_y, int32_t
                            void* cuda_stream);
 const char* s2d2_noalloc_last_error(void);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Stand-alone operators: a 4-bit language-model head (or any linear layer) and the scores of tokens.
+ * (The paper has no counterpart: its decoding is bound by the bytes of the weights, and a server reports log
+ * probabilities of the tokens that a step commits.)
+ *
+ * All pointers with d_ are device (or managed) memory of the current device, owned by the caller; `cuda_stream` is a
+ * stream of that device.  The calls are ASYNCHRONOUS, keep nothing between calls, allocate nothing and may be captured
+ * into CUDA graphs (make the first call of each on a device outside any capture); calls on different streams may overlap.  They return S2D2_OK or a negative
+ * s2d2_status before anything is launched, with the text in s2d2_ops_last_error() (per host thread).
+ *
+ * MXFP4 (microscaling, block size 32): the elements of a row are cut into blocks of 32; a block has one scale 2^e, held
+ * as the byte e + 127 (255: the whole block is NaN), and 32 e2m1 codes (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 and their negatives), two per byte, the lower nibble first.
+ *   codes:  row-major, ceil(cols / 32) * 16 bytes per row (a last block that is not full is padded with zeros);
+ *           16-byte aligned.
+ *   scales: tiles of 128 rows x 4 blocks, 512 bytes each: the byte of (row r, block b) is byte
+ *           (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4 of tile (r / 128) * ceil(ceil(cols / 32) / 4) + b / 4.  The tiles are
+ *           whole; bytes of rows and blocks that do not exist are zero.  16-byte aligned. */
+#define S2D2_SCORE_MAX_TOP 32
+#define S2D2_SCORE_MAX_VOCAB 2097152
+#define S2D2_MXFP4_MAX_DIM 4194304       /* rows, N and M of an MXFP4 matrix; columns and K: 1048576 */
+
+const char* s2d2_ops_last_error(void);
+/* Waits for the stream; S2D2_ERR_TIMEOUT if a bounded wait inside a kernel of these operators ran out since the last
+ * call (the outputs of that kernel are NaN then, never stale), else S2D2_OK. */
+int s2d2_ops_status(void* cuda_stream);
+
+/* Bytes of the codes and of the scales of a [rows, cols] matrix. */
+int s2d2_mxfp4_sizes(int64_t rows, int64_t cols, int64_t* codes_bytes, int64_t* scales_bytes);
+
+/* codes, scales <- x [rows, cols] (dtype S2D2_DTYPE_*, rows row_stride elements apart).  Per block e =
+ * clamp(floor(log2 max|x|) - 2, -127, 127) (all zeros: -127), element = x * 2^-e rounded to the nearest e2m1 value, ties to the
+ * even code, magnitudes above 6 to 6.  A block that holds a NaN or an infinity becomes NaN.  Padding is written, too. */
+int s2d2_mxfp4_quantize(const void* d_x, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, void* d_codes,
+                        void* d_scales, void* cuda_stream);
+/* y [rows, cols] <- the values that codes and scales stand for (exact in fp32 and in bf16, except that values of 2^128 and
+ * more become infinite).  Only the rows' own cols elements are written. */
+int s2d2_mxfp4_dequantize(const void* d_codes, const void* d_scales, int64_t rows, int64_t cols, void* d_y, int32_t dtype,
+                          int64_t row_stride, void* cuda_stream);
+
+/* y[M, N] = scale * x[M, K] w[N, K]^T, both operands MXFP4 (x a matrix of M rows and K columns, w one of N rows and K
+ * columns), products and sums in fp32, one rounding to y's type (y_dtype S2D2_DTYPE_*, rows y_stride elements apart).
+ * M = 0 is allowed and does nothing. */
+int s2d2_mxfp4_gemm(const void* d_x_codes, const void* d_x_scales, const void* d_w_codes, const void* d_w_scales, void* d_y,
+                    int32_t y_dtype, int32_t M, int32_t N, int32_t K, int64_t y_stride, float scale, void* cuda_stream);
+
+/* Scores of n_rows rows of logits (dtype S2D2_DTYPE_*, rows row_stride elements apart, any alignment of the element type).
+ * With pi = softmax of a row:
+ *   d_logprob[r]   log pi(token r)             d_rank[r]  tokens that come before it (larger logit, or equal and lower id)
+ *   d_lse[r]       log sum exp of the logits   d_entropy[r]  entropy of pi in nats
+ *   d_top_ids, d_top_logprobs [n_rows, top_k]: the top_k most probable tokens, equal ones by ascending id
+ * Any output may be NULL (tokens too, if neither logprob nor rank is asked for).  0 <= top_k <= S2D2_SCORE_MAX_TOP.
+ * Logits of -inf have probability zero: they are never listed (unused places hold id -1 and -inf).  A row that is -inf
+ * throughout gives lse = logprob = -inf, entropy 0.  A token outside [0, vocab) gives logprob NaN, rank -1.
+ * A row with a NaN or a +inf gives NaN, ids and rank -1.  n_rows = 0 does nothing. */
+int s2d2_score_logits(const void* d_logits, int32_t dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                      const int32_t* d_tokens, int32_t top_k, float* d_logprob, int32_t* d_rank, float* d_lse,
+                      float* d_entropy, int32_t* d_top_ids, float* d_top_logprobs, void* cuda_stream);
+
+/* s2d2_score_logits on the logits that the last draft pass (which = 0) or verifier pass (which = 1) of a context left
+ * behind: rows as s2d2_debug_copy_logits lists them, n_rows of them from the first one on.  Host pointers; outputs
+ * [n_rows] and [n_rows, top_k], each may be NULL as above.  Synchronous. */
+int s2d2_score_pass(s2d2_ctx* ctx, int32_t which, int32_t n_rows, const int32_t* tokens, int32_t top_k, float* logprob,
+                    int32_t* rank, float* lse, float* entropy, int32_t* top_ids, float* top_logprobs);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,4 +10,10 @@ from .binding import (  # noqa: F401
     gemm_bf16_noalloc,
     library_path,
     load_library,
+    mxfp4_dequantize,
+    mxfp4_gemm,
+    mxfp4_quantize,
+    mxfp4_sizes,
+    ops_status,
+    score_logits,
 )

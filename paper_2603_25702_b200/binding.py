@@ -81,7 +81,10 @@ EXPORTS = [
     "s2d2_get_counters", "s2d2_reset_counters", "s2d2_set_profiling", "s2d2_set_accept_override", "s2d2_get_gemm_profile", "s2d2_accept_logits", "s2d2_sample_logits", "s2d2_debug_copy_logits",
     "s2d2_debug_copy_kv", "s2d2_debug_seq_state", "s2d2_debug_gemm", "s2d2_debug_gemm2", "s2d2_debug_gemm_swiglu", "s2d2_debug_copy_expert_ids", "s2d2_debug_pass_trace", "s2d2_debug_wait_timeout",
     "s2d2_gemm_bf16_noalloc", "s2d2_noalloc_last_error",
+    "s2d2_ops_last_error", "s2d2_ops_status", "s2d2_mxfp4_sizes", "s2d2_mxfp4_quantize", "s2d2_mxfp4_dequantize",
+    "s2d2_mxfp4_gemm", "s2d2_score_logits", "s2d2_score_pass",
 ]
+_TEXTS = ("s2d2_last_error", "s2d2_noalloc_last_error", "s2d2_ops_last_error")     # these return a string
 
 
 def library_path() -> str:
@@ -101,9 +104,11 @@ def load_library() -> C.CDLL:
     lib.s2d2_last_error.argtypes = [C.c_void_p]
     lib.s2d2_noalloc_last_error.restype = C.c_char_p
     lib.s2d2_noalloc_last_error.argtypes = []
+    lib.s2d2_ops_last_error.restype = C.c_char_p
+    lib.s2d2_ops_last_error.argtypes = []
     for name in EXPORTS:
         fn = getattr(lib, name)
-        if name not in ("s2d2_last_error", "s2d2_noalloc_last_error"):
+        if name not in _TEXTS:
             fn.restype = C.c_int
     lib.s2d2_gemm_bf16_noalloc.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
     lib.s2d2_create.argtypes = [C.POINTER(ModelConfigC), C.POINTER(DecodeConfigC), C.c_void_p, C.POINTER(C.c_void_p)]
@@ -140,6 +145,13 @@ def load_library() -> C.CDLL:
     lib.s2d2_debug_copy_expert_ids.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.c_int64, C.POINTER(C.c_int32)]
     lib.s2d2_debug_wait_timeout.argtypes = [C.c_void_p, C.c_uint32, C.c_uint32]
     lib.s2d2_debug_pass_trace.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+    lib.s2d2_ops_status.argtypes = [C.c_void_p]
+    lib.s2d2_mxfp4_sizes.argtypes = [C.c_int64, C.c_int64, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
+    lib.s2d2_mxfp4_quantize.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.s2d2_mxfp4_dequantize.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]
+    lib.s2d2_mxfp4_gemm.argtypes = [C.c_void_p] * 5 + [C.c_int32] * 4 + [C.c_int64, C.c_float, C.c_void_p]
+    lib.s2d2_score_logits.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_int32] + [C.c_void_p] * 7
+    lib.s2d2_score_pass.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32] + [C.c_void_p] * 6
     _LIB = lib
     return lib
 
@@ -158,6 +170,66 @@ def gemm_bf16_noalloc(d_x: int, d_w: int, d_y: int, M: int, N: int, K: int, stre
     rc = lib.s2d2_gemm_bf16_noalloc(C.c_void_p(d_x), C.c_void_p(d_w), C.c_void_p(d_y), M, N, K, C.c_void_p(stream))
     if rc != 0:
         raise S2D2Error(rc, lib.s2d2_noalloc_last_error().decode())
+
+
+_DTYPES = {"fp32": 0, "bf16": 1}
+
+
+def _ops_check(rc: int) -> None:
+    if rc != 0:
+        raise S2D2Error(rc, _LIB.s2d2_ops_last_error().decode())
+
+
+def _dtype(name: str) -> int:
+    if name not in _DTYPES:
+        raise S2D2Error(-1, f"dtype must be 'fp32' or 'bf16', not {name!r}")
+    return _DTYPES[name]
+
+
+def ops_status(stream: int = 0) -> None:
+    """Waits for ``stream``; raises S2D2Error(-5) if a bounded wait in a kernel of the stand-alone operators ran out since
+    the last call (that kernel's outputs are NaN then)."""
+    lib = load_library()
+    _ops_check(lib.s2d2_ops_status(stream))
+
+
+def mxfp4_sizes(rows: int, cols: int):
+    """(bytes of codes, bytes of scales) of a [rows, cols] MXFP4 matrix (layout: include/s2d2.h)."""
+    lib = load_library()
+    a, b = C.c_int64(), C.c_int64()
+    _ops_check(lib.s2d2_mxfp4_sizes(rows, cols, C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def mxfp4_quantize(d_x: int, dtype: str, rows: int, cols: int, row_stride: int, d_codes: int, d_scales: int, stream: int = 0) -> None:
+    """codes, scales <- x [rows, cols] ("fp32" or "bf16", rows ``row_stride`` elements apart).  Raw device pointers;
+    asynchronous on ``stream``."""
+    lib = load_library()
+    _ops_check(lib.s2d2_mxfp4_quantize(d_x, _dtype(dtype), rows, cols, row_stride, d_codes, d_scales, stream))
+
+
+def mxfp4_dequantize(d_codes: int, d_scales: int, rows: int, cols: int, d_y: int, dtype: str, row_stride: int, stream: int = 0) -> None:
+    """y [rows, cols] <- the values that codes and scales stand for.  Asynchronous."""
+    lib = load_library()
+    _ops_check(lib.s2d2_mxfp4_dequantize(d_codes, d_scales, rows, cols, d_y, _dtype(dtype), row_stride, stream))
+
+
+def mxfp4_gemm(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int, d_y: int, y_dtype: str, M: int, N: int, K: int,
+               y_stride: Optional[int] = None, scale: float = 1.0, stream: int = 0) -> None:
+    """y[M, N] = scale * x[M, K] w[N, K]^T of two MXFP4 matrices, y "fp32" or "bf16".  Asynchronous."""
+    lib = load_library()
+    _ops_check(lib.s2d2_mxfp4_gemm(d_x_codes, d_x_scales, d_w_codes, d_w_scales, d_y, _dtype(y_dtype), M, N, K,
+                                   N if y_stride is None else y_stride, scale, stream))
+
+
+def score_logits(d_logits: int, dtype: str, n_rows: int, vocab: int, row_stride: int, d_tokens: int = 0, top_k: int = 0, *,
+                 d_logprob: int = 0, d_rank: int = 0, d_lse: int = 0, d_entropy: int = 0, d_top_ids: int = 0,
+                 d_top_logprobs: int = 0, stream: int = 0) -> None:
+    """Log probability and rank of one given token per row (int32), log-sum-exp, entropy and the ``top_k`` most probable tokens of
+    device logits ("fp32" or "bf16").  Outputs are fp32 (ids and ranks int32); 0 leaves one out.  Asynchronous."""
+    lib = load_library()
+    _ops_check(lib.s2d2_score_logits(d_logits, _dtype(dtype), n_rows, vocab, row_stride, d_tokens, top_k, d_logprob, d_rank, d_lse,
+                                     d_entropy, d_top_ids, d_top_logprobs, stream))
 
 
 class Engine:
@@ -334,6 +406,23 @@ class Engine:
                                                 rs.ctypes.data_as(C.POINTER(C.c_uint32)), stp_p,
                                                 xh.ctypes.data_as(C.POINTER(C.c_int32)), fp(cf), fp(mg), fp(en)))
         return xh, cf, mg, en
+
+    def score_pass(self, which: int, n_rows: int, tokens=None, top_k: int = 0):
+        """Scores of the first ``n_rows`` logit rows of the last draft (which = 0) or verifier pass (1): a dict with "lse",
+        "entropy", with ``tokens`` also "logprob" and "rank", with ``top_k`` also "top_ids" and "top_logprobs"."""
+        out = {"lse": np.zeros(n_rows, np.float32), "entropy": np.zeros(n_rows, np.float32)}
+        tok = None
+        if tokens is not None:
+            tok = np.ascontiguousarray(tokens, dtype=np.int32).reshape(-1)
+            if tok.size != n_rows:
+                raise ValueError("one token per row")
+            out["logprob"], out["rank"] = np.zeros(n_rows, np.float32), np.zeros(n_rows, np.int32)
+        if top_k > 0:
+            out["top_ids"], out["top_logprobs"] = np.zeros((n_rows, top_k), np.int32), np.zeros((n_rows, top_k), np.float32)
+        ptr = lambda name: out[name].ctypes.data if name in out else None
+        self._check(self.lib.s2d2_score_pass(self._h, which, n_rows, None if tok is None else tok.ctypes.data, top_k, ptr("logprob"),
+                                             ptr("rank"), ptr("lse"), ptr("entropy"), ptr("top_ids"), ptr("top_logprobs")))
+        return out
 
     def debug_copy_logits(self, which: int, max_rows: int) -> np.ndarray:
         buf = np.empty((max_rows, self.vocab), dtype=np.float32)

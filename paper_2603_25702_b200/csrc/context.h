@@ -120,6 +120,7 @@ struct s2d2_ctx {
     unsigned* acc_tickets = nullptr;               // per sequence of an acceptance launch: CTAs done so far (zero between launches)
     char* stats_h = nullptr;                       // pinned mirror of the draft statistics
     int *dsamp_h = nullptr, *dsamp_d = nullptr;    // draft sampling: per logit row position, Philox stream, step (pinned / device)
+    float* score_d = nullptr;                      // s2d2_score_pass: tokens and outputs of up to max_logit_rows rows
     int n_draft_logit_rows = 0, n_verify_logit_rows = 0;
     // The logits of a pass live in per-context buffers that the next pass of the same kind overwrites; the passes
     // are numbered so that a sequence whose rows have been overwritten is recognised (S2D2_ERR_STATE).

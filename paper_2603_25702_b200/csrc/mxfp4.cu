@@ -1,0 +1,308 @@
+// MXFP4: quantisation, its inverse, and the host side of the products (kernels in mxfp4_tc.cuh).
+#include <math.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "common.cuh"
+#include "mxfp4_tc.cuh"
+#include "ops_host.h"
+
+namespace s2d2 {
+namespace {
+
+constexpr int QT = 256;              // threads of the element-wise kernels
+constexpr int QUAD = 128;            // elements under one 32-bit word of scale bytes: 4 blocks, 16 threads x 8 elements
+
+struct QuantParams {
+    const void* x;                   // quantise: input;  dequantise: output
+    long long ld;
+    long long rows, cols;
+    int quads;                       // words of scale bytes per row
+    long long code_ld;               // bytes of codes per row
+    uint8_t* codes;
+    uint8_t* scales;
+    int vec;                         // rows of x are 16-byte aligned
+};
+
+__host__ __device__ __forceinline__ size_t scale_word(long long row, int quad, int quads) {      // byte offset of 4 scale bytes
+    return ((size_t)(row / 128) * quads + quad) * 512 + (size_t)(row % 32) * 16 + (size_t)(row % 128) / 32 * 4;
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, bool vec, long long left, float* v) {
+    if (vec && left >= 8) {
+        if (sizeof(T) == 4) {
+            const float4 a = __ldg((const float4*)p), b = __ldg((const float4*)p + 1);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 a = __ldg((const uint4*)p);
+            const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[2 * e] = __uint_as_float(u[e] << 16);
+                v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? to_f32(p[e]) : 0.f;
+    }
+}
+
+// Eight e2m1 codes, element 0 in the lowest nibble: round to nearest, ties to even, saturating.
+__device__ __forceinline__ uint32_t e2m1x8(const float* v) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+
+// 16 threads per (row, 128 elements): four threads share a block, their largest magnitude as an integer maximum of the
+// absolute bit patterns (infinities and NaN come out on top).  Scale and quotient are exact: the scale is a power of two.
+// Memory bound.  Rows that pad the last scale tile get zeros.
+template <typename T>
+__global__ void __launch_bounds__(QT) quantize_kernel(const QuantParams p) {
+    pdl_wait();
+    pdl_launch();
+    const long long rows_padded = (p.rows + 127) / 128 * 128, units = rows_padded * p.quads;
+    const int sub = threadIdx.x & 15;
+    const long long stride = (long long)gridDim.x * (QT / 16);
+    for (long long u = (long long)blockIdx.x * (QT / 16) + (threadIdx.x >> 4); u < units; u += stride) {
+        // (units is a multiple of 128: the two half warps, which exchange through shuffles, leave the loop together)
+        const long long row = u / p.quads;
+        const int quad = (int)(u - row * p.quads);
+        const long long c0 = (long long)quad * QUAD + sub * 8;
+        const bool inside = row < p.rows;
+        float v[8];
+        load8((const T*)p.x + (inside ? row * p.ld + c0 : 0), p.vec, inside ? p.cols - c0 : 0, v);
+        uint32_t a = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a = max(a, __float_as_uint(v[e]) & 0x7fffffffu);
+        a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
+        a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
+        const int exponent = (int)(a >> 23);                       // biased; 0 for zero and for subnormals
+        const bool bad = exponent == 255;
+        const int byte = bad ? 255 : max(exponent - 2, 0);
+        const float inverse = __uint_as_float((uint32_t)(254 - (bad ? 127 : byte)) << 23);       // 2^(127 - byte)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= inverse;
+        const uint32_t codes = bad ? 0u : e2m1x8(v);
+        if (inside && c0 < p.code_ld * 2) *(uint32_t*)(p.codes + row * p.code_ld + c0 / 2) = codes;
+        uint32_t word = (uint32_t)byte << (8 * (sub >> 2));
+        if (!inside || (long long)quad * QUAD + (sub >> 2) * 32 >= p.cols) word = 0;
+        word |= __shfl_xor_sync(0xffffffffu, word, 4);
+        word |= __shfl_xor_sync(0xffffffffu, word, 8);
+        if (sub == 0) *(uint32_t*)(p.scales + scale_word(row, quad, p.quads)) = word;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(QT) dequantize_kernel(const QuantParams p) {
+    pdl_wait();
+    pdl_launch();
+    const long long units = p.rows * p.quads;
+    const int sub = threadIdx.x & 15;
+    const long long stride = (long long)gridDim.x * (QT / 16);
+    for (long long u = (long long)blockIdx.x * (QT / 16) + (threadIdx.x >> 4); u < units; u += stride) {
+        const long long row = u / p.quads;
+        const int quad = (int)(u - row * p.quads);
+        const long long c0 = (long long)quad * QUAD + sub * 8;
+        if (c0 >= p.cols) continue;
+        const uint32_t codes = __ldg((const uint32_t*)(p.codes + row * p.code_ld + c0 / 2));
+        const uint32_t byte = p.scales[scale_word(row, quad, p.quads) + (sub >> 2)];
+        const float scale = __uint_as_float(byte == 255 ? 0x7fffffffu : byte ? byte << 23 : 0x00400000u);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            // e2m1 as fp32: exponent and mantissa bits moved into place, the offset of the exponent by an exact product
+            const uint32_t c = codes >> (4 * e);
+            const float mag = __uint_as_float((c & 7u) << 22) * 0x1p126f;
+            v[e] = ((c & 8u) ? -mag : mag) * scale;
+        }
+        T* y = (T*)const_cast<void*>(p.x) + row * p.ld + c0;
+        if (p.vec && c0 + 8 <= p.cols) {
+            if (sizeof(T) == 4) {
+                ((float4*)y)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                ((float4*)y)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+                    w[e] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+                *(uint4*)y = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        } else {
+            for (int e = 0; e < 8; ++e)
+                if (c0 + e < p.cols) y[e] = from_f32<T>(v[e]);
+        }
+    }
+}
+
+constexpr long long MAX_COLS = 1 << 20;
+
+int check_shape(const char* op, long long rows, long long cols) {
+    if (rows < 0 || rows > S2D2_MXFP4_MAX_DIM) return ops::fail(S2D2_ERR_INVALID, "%s: rows must be in 0..%d", op, S2D2_MXFP4_MAX_DIM);
+    if (cols < 1 || cols > MAX_COLS) return ops::fail(S2D2_ERR_INVALID, "%s: columns must be in 1..%lld", op, MAX_COLS);
+    return S2D2_OK;
+}
+
+int elementwise(const char* op, bool inverse, const void* x, int dtype, long long rows, long long cols, long long ld, const void* codes,
+                const void* scales, cudaStream_t st) {
+    ops::clear_error();
+    if (dtype != S2D2_DTYPE_F32 && dtype != S2D2_DTYPE_BF16) return ops::fail(S2D2_ERR_INVALID, "%s: dtype", op);
+    if (int rc = check_shape(op, rows, cols)) return rc;
+    if (ld < cols || ld > (1LL << 40)) return ops::fail(S2D2_ERR_INVALID, "%s: row_stride must be in cols..2^40", op);
+    const ops::Device* dev;
+    if (int rc = ops::device(&dev)) return rc;
+    if (rows == 0) return S2D2_OK;
+    const size_t size = dtype == S2D2_DTYPE_F32 ? 4 : 2;
+    if (int rc = ops::check_ptr(dev, x, size, inverse ? "y" : "x")) return rc;
+    if (int rc = ops::check_ptr(dev, codes, 16, "codes")) return rc;
+    if (int rc = ops::check_ptr(dev, scales, 16, "scales")) return rc;
+    QuantParams p;
+    p.x = x;
+    p.ld = ld;
+    p.rows = rows;
+    p.cols = cols;
+    const long long blocks = (cols + 31) / 32;
+    p.quads = (int)((blocks + 3) / 4);
+    p.code_ld = blocks * 16;
+    p.codes = (uint8_t*)const_cast<void*>(codes);
+    p.scales = (uint8_t*)const_cast<void*>(scales);
+    p.vec = ((uintptr_t)x & 15) == 0 && (ld * size) % 16 == 0;
+    const long long units = (inverse ? rows : (rows + 127) / 128 * 128) * p.quads;
+    const unsigned grid = (unsigned)std::min<long long>((units + QT / 16 - 1) / (QT / 16), (long long)dev->n_sms * 32);
+    cudaError_t e;
+    if (dtype == S2D2_DTYPE_F32) e = ops::launch(inverse ? dequantize_kernel<float> : quantize_kernel<float>, dim3(grid), QT, 0, 1, st, p);
+    else e = ops::launch(inverse ? dequantize_kernel<bf16> : quantize_kernel<bf16>, dim3(grid), QT, 0, 1, st, p);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return ops::fail(S2D2_ERR_CUDA, "%s: %s", op, cudaGetErrorString(e));
+    }
+    return S2D2_OK;
+}
+
+// Codes of a [rows, K] matrix in boxes of box_rows rows x 256 elements; what lies outside the matrix reads as zero.
+int encode_codes(const ops::Device* dev, CUtensorMap* map, const void* codes, int rows, int K, int box_rows) {
+    const cuuint64_t row_bytes = (cuuint64_t)((K + 31) / 32) * 16;
+    cuuint64_t dims[2] = {row_bytes, (cuuint64_t)rows}, strides[1] = {row_bytes};
+    cuuint32_t box[2] = {(cuuint32_t)mx::KBYTES, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    const CUresult r = dev->encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, step,
+                                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? S2D2_OK : ops::fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+int raise_limits(const ops::Device* dev) {
+    static std::atomic<bool> done[64];
+    if (done[dev->id].load(std::memory_order_acquire)) return S2D2_OK;
+    const cudaError_t e = cudaFuncSetAttribute(mx::stream_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, mx::STREAM_MAX_SMEM);
+    if (e != cudaSuccess) return ops::fail(S2D2_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+    done[dev->id].store(true, std::memory_order_release);
+    return S2D2_OK;
+}
+
+int check_product(const char* op, const ops::Device* dev, const void* xc, const void* xs, const void* wc, const void* ws, int M, int N,
+                  int K) {
+    if (M > 0) {
+        if (int rc = ops::check_ptr(dev, xc, 16, "x_codes")) return rc;
+        if (int rc = ops::check_ptr(dev, xs, 16, "x_scales")) return rc;
+        if (int rc = ops::check_ptr(dev, wc, 16, "w_codes")) return rc;
+        if (int rc = ops::check_ptr(dev, ws, 16, "w_scales")) return rc;
+    }
+    return S2D2_OK;
+}
+int check_product_shape(const char* op, int M, int N, int K) {
+    if (M < 0 || M > S2D2_MXFP4_MAX_DIM) return ops::fail(S2D2_ERR_INVALID, "%s: M must be in 0..%d", op, S2D2_MXFP4_MAX_DIM);
+    if (N < 1 || N > S2D2_MXFP4_MAX_DIM) return ops::fail(S2D2_ERR_INVALID, "%s: N must be in 1..%d", op, S2D2_MXFP4_MAX_DIM);
+    if (K < 1 || K > MAX_COLS) return ops::fail(S2D2_ERR_INVALID, "%s: K must be in 1..%lld", op, MAX_COLS);
+    return S2D2_OK;
+}
+
+int launch_stream(const ops::Device* dev, mx::GemmParams p, const void* xc, const void* wc, cudaStream_t st) {
+    p.T = std::min(128, (p.M + 15) / 16 * 16);
+    p.m_tiles = (p.M + p.T - 1) / p.T;
+    p.x_tiles = 1;                             // T divides 128, or there is one tile
+    const int n_tiles = (p.N + mx::ROWS - 1) / mx::ROWS;
+    const long long tiles = (long long)n_tiles * p.m_tiles;
+    const int sbytes = mx::stage_bytes(p.T, p.x_tiles);
+    // k splits: as many CTAs as fit at once (two per SM) while each keeps at least two k-blocks
+    p.splits = 1;
+    while (p.splits < 8 && tiles * p.splits * 2 <= 2LL * dev->n_sms && p.kb_total >= 4 * p.splits) p.splits *= 2;
+    const int room = mx::STREAM_MAX_SMEM - 1024 - (int)sizeof(mx::StreamControl);
+    p.stages = std::max(2, std::min(std::min(8, room / sbytes), (p.kb_total + p.splits - 1) / p.splits));
+    p.control_at = std::max(p.stages * sbytes, p.splits > 1 ? p.T * mx::ROWS * 4 : 0);
+    const int smem = std::max(1024 + p.control_at + (int)sizeof(mx::StreamControl), mx::stream_min_smem(p.T));
+    if (tiles * p.splits > 0x7fffffffLL) return ops::fail(S2D2_ERR_UNSUPPORTED, "mxfp4_gemm: too many tiles");
+    CUtensorMap mw, mx_;
+    if (int rc = encode_codes(dev, &mw, wc, p.N, p.K, mx::ROWS)) return rc;
+    if (int rc = encode_codes(dev, &mx_, xc, p.M, p.K, p.T)) return rc;
+    const cudaError_t e = ops::launch(mx::stream_kernel, dim3((unsigned)(tiles * p.splits)), mx::THREADS, smem, p.splits, st, mw, mx_, p);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return ops::fail(S2D2_ERR_CUDA, "mxfp4_gemm: %s", cudaGetErrorString(e));
+    }
+    return S2D2_OK;
+}
+
+}  // namespace
+}  // namespace s2d2
+
+using namespace s2d2;
+
+extern "C" int s2d2_mxfp4_sizes(int64_t rows, int64_t cols, int64_t* codes_bytes, int64_t* scales_bytes) {
+    ops::clear_error();
+    if (!codes_bytes || !scales_bytes) return ops::fail(S2D2_ERR_INVALID, "mxfp4_sizes: null pointer");
+    if (int rc = check_shape("mxfp4_sizes", rows, cols)) return rc;
+    const int64_t blocks = (cols + 31) / 32;
+    *codes_bytes = rows * blocks * 16;
+    *scales_bytes = (rows + 127) / 128 * ((blocks + 3) / 4) * 512;
+    return S2D2_OK;
+}
+
+extern "C" int s2d2_mxfp4_quantize(const void* d_x, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, void* d_codes,
+                                   void* d_scales, void* cuda_stream) {
+    return elementwise("mxfp4_quantize", false, d_x, dtype, rows, cols, row_stride, d_codes, d_scales, (cudaStream_t)cuda_stream);
+}
+
+extern "C" int s2d2_mxfp4_dequantize(const void* d_codes, const void* d_scales, int64_t rows, int64_t cols, void* d_y, int32_t dtype,
+                                     int64_t row_stride, void* cuda_stream) {
+    return elementwise("mxfp4_dequantize", true, d_y, dtype, rows, cols, row_stride, d_codes, d_scales, (cudaStream_t)cuda_stream);
+}
+
+extern "C" int s2d2_mxfp4_gemm(const void* d_x_codes, const void* d_x_scales, const void* d_w_codes, const void* d_w_scales, void* d_y,
+                               int32_t y_dtype, int32_t M, int32_t N, int32_t K, int64_t y_stride, float scale, void* cuda_stream) {
+    ops::clear_error();
+    if (y_dtype != S2D2_DTYPE_F32 && y_dtype != S2D2_DTYPE_BF16) return ops::fail(S2D2_ERR_INVALID, "mxfp4_gemm: y_dtype");
+    if (int rc = check_product_shape("mxfp4_gemm", M, N, K)) return rc;
+    if (y_stride < N || y_stride > (1LL << 40)) return ops::fail(S2D2_ERR_INVALID, "mxfp4_gemm: y_stride must be in N..2^40");
+    const ops::Device* dev;
+    if (int rc = ops::device(&dev)) return rc;
+    if (M == 0) return S2D2_OK;
+    if (int rc = check_product("mxfp4_gemm", dev, d_x_codes, d_x_scales, d_w_codes, d_w_scales, M, N, K)) return rc;
+    if (int rc = ops::check_ptr(dev, d_y, y_dtype == S2D2_DTYPE_F32 ? 4 : 2, "y")) return rc;
+    if (int rc = raise_limits(dev)) return rc;
+    mx::GemmParams p = {};
+    p.y = d_y;
+    p.y_bf16 = y_dtype == S2D2_DTYPE_BF16;
+    p.M = M;
+    p.N = N;
+    p.K = K;
+    p.ldy = y_stride;
+    p.scale = scale;
+    p.kb_total = (K + mx::KBLOCK - 1) / mx::KBLOCK;
+    p.quads = ((K + 31) / 32 + 3) / 4;
+    p.w_scales = (const uint8_t*)d_w_scales;
+    p.x_scales = (const uint8_t*)d_x_scales;
+    p.status = dev->status;
+    return launch_stream(dev, p, d_x_codes, d_w_codes, (cudaStream_t)cuda_stream);
+}

@@ -243,6 +243,7 @@ extern "C" int s2d2_create(const s2d2_model_config* m, const s2d2_decode_config*
         if ((rc = dmalloc(c, (char**)&c->attn_lo, M * nq * es))) return rc;
         if ((rc = dmalloc(c, (char**)&c->act_lo, M * f * es))) return rc;
     }
+    if ((rc = dmalloc(c, &c->score_d, (size_t)c->max_logit_rows * (5 + 2 * S2D2_SCORE_MAX_TOP)))) return rc;
     if ((rc = dmalloc(c, &c->logits_draft, (size_t)c->max_logit_rows * m->vocab))) return rc;
     if ((rc = dmalloc(c, &c->logits_verify, (size_t)c->max_logit_rows * m->vocab))) return rc;
     if (m->n_experts > 0) {
@@ -345,7 +346,7 @@ extern "C" int s2d2_destroy(s2d2_ctx* c) {
                     c->logits_draft, c->logits_verify, c->rope_cos, c->rope_sin, c->router_logits, c->moe_gates,
                     c->moe_ids, c->moe_gu, c->moe_act, c->moe_out, c->moe_ids_trace, c->meta.d, c->d_xhat, c->d_conf,
                     c->d_margin, c->d_entropy, c->d_lse, c->acc_d, c->d_status, c->chunk_d, c->chunk_v, c->rej_info,
-                    c->res_rsum, c->res_vsum, c->dsamp_d, c->acc_tickets};
+                    c->res_rsum, c->res_vsum, c->dsamp_d, c->acc_tickets, c->score_d};
     for (void* p : ptrs)
         if (p) cudaFree(p);
     if (c->meta.h) cudaFreeHost(c->meta.h);
@@ -1326,6 +1327,45 @@ extern "C" int s2d2_sample_logits(s2d2_ctx* c, const float* d_logits, int32_t n_
     CUDA_TRY(c, cudaMemcpyAsync(conf_out, c->d_conf, R * 4, cudaMemcpyDeviceToHost, c->stream));
     CUDA_TRY(c, cudaMemcpyAsync(margin_out, c->d_margin, R * 4, cudaMemcpyDeviceToHost, c->stream));
     CUDA_TRY(c, cudaMemcpyAsync(entropy_out, c->d_entropy, R * 4, cudaMemcpyDeviceToHost, c->stream));
+    CUDA_TRY(c, cudaStreamSynchronize(c->stream));
+    return S2D2_OK;
+}
+
+extern "C" int s2d2_score_pass(s2d2_ctx* c, int32_t which, int32_t n_rows, const int32_t* tokens, int32_t top_k, float* logprob,
+                               int32_t* rank, float* lse, float* entropy, int32_t* top_ids, float* top_logprobs) {
+    if (!c) return S2D2_ERR_INVALID;
+    if (which != 0 && which != 1) FAIL(c, S2D2_ERR_INVALID, "score_pass: which must be 0 (draft) or 1 (verifier)");
+    const int have = which == 0 ? c->n_draft_logit_rows : c->n_verify_logit_rows;
+    if (n_rows < 0) FAIL(c, S2D2_ERR_INVALID, "score_pass: n_rows is negative");
+    if (n_rows > have) FAIL(c, S2D2_ERR_STATE, "score_pass: the last pass of this kind has fewer logit rows");
+    if (top_k < 0 || top_k > S2D2_SCORE_MAX_TOP) FAIL(c, S2D2_ERR_INVALID, "score_pass: top_k must be in 0..32");
+    if ((logprob || rank) && !tokens) FAIL(c, S2D2_ERR_INVALID, "score_pass: log probability and rank need tokens");
+    if (n_rows == 0) return S2D2_OK;
+    const size_t R = n_rows, cap = c->max_logit_rows;
+    int32_t* d_tok = (int32_t*)c->score_d;
+    float* d_out = c->score_d + cap;      // logprob, rank, lse, entropy, ids, log probabilities of the alternatives
+    if (tokens) CUDA_TRY(c, cudaMemcpyAsync(d_tok, tokens, R * 4, cudaMemcpyHostToDevice, c->stream));
+    const bool want_top = top_k > 0 && (top_ids || top_logprobs);
+    const int rc = s2d2_score_logits(which == 0 ? c->logits_draft : c->logits_verify, S2D2_DTYPE_F32, n_rows, c->m.vocab, c->m.vocab,
+                                     tokens ? d_tok : nullptr, want_top ? top_k : 0, logprob ? d_out : nullptr,
+                                     rank ? (int32_t*)(d_out + cap) : nullptr, d_out + 2 * cap, d_out + 3 * cap,
+                                     want_top ? (int32_t*)(d_out + 4 * cap) : nullptr,
+                                     want_top ? d_out + (4 + S2D2_SCORE_MAX_TOP) * cap : nullptr, c->stream);
+    if (rc) FAIL(c, rc, s2d2_ops_last_error());
+    LAUNCHED(c);
+    if (tokens) c->cnt.h2d_bytes += R * 4;
+    const struct {
+        void* to;
+        const void* from;
+        size_t n;
+    } back[] = {{logprob, d_out, R}, {rank, d_out + cap, R}, {lse, d_out + 2 * cap, R}, {entropy, d_out + 3 * cap, R},
+                {want_top ? top_ids : nullptr, d_out + 4 * cap, R * top_k},
+                {want_top ? top_logprobs : nullptr, d_out + (4 + S2D2_SCORE_MAX_TOP) * cap, R * top_k}};
+    for (const auto& b : back)
+        if (b.to) {
+            CUDA_TRY(c, cudaMemcpyAsync(b.to, b.from, b.n * 4, cudaMemcpyDeviceToHost, c->stream));
+            c->cnt.d2h_bytes += b.n * 4;
+        }
     CUDA_TRY(c, cudaStreamSynchronize(c->stream));
     return S2D2_OK;
 }

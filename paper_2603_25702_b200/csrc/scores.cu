@@ -1,0 +1,534 @@
+// Scores of caller-supplied logits: log probability and rank of a given token, log-sum-exp, entropy, top alternatives.
+//
+// With m = max_j x_j and s = sum_j e^(x_j - m) over one row of logits:
+//   lse = m + log s        logprob = (x_t - m) - log s        entropy = log s - (1/s) sum_j (x_j - m) e^(x_j - m)
+//   rank = #{j : x_j > x_t} + #{j < t : x_j = x_t}            top: value descending, lowest id first among equals
+//
+// One pass over the row with a running maximum (per thread, one rescale per 16 elements).  Maxima, sums and moments are fp32
+// per thread over at most a few thousand terms and are merged in a fixed order.  The moment uses x - m instead of x:
+// log s - t/s then adds two non-negative terms, where lse - sum x p subtracts numbers of the size of the logits.
+//
+// The top alternatives cost nothing per element: the loop keeps the maximum of every (thread, 16 elements) tile in shared memory.
+// The k-th largest of the 256 thread maxima is a lower bound of the k-th largest element, so only tiles whose maximum reaches
+// it are read again (a little over k tiles of 16 elements), and only elements that reach it are sorted.
+//
+// A row is shared by a cluster of 1, 2, 4 or 8 CTAs, so that a few rows fill the GPU; partial results meet in the shared memory
+// of the cluster's first CTA.  Nothing is kept in global memory, no atomics on it, no workspace.
+#include <float.h>
+#include <math.h>
+
+#include <atomic>
+
+#include "common.cuh"
+#include "ops_host.h"
+
+namespace s2d2 {
+namespace {
+
+constexpr int NT = 256;            // threads
+constexpr int NW = NT / 32;
+constexpr int TILE = 16;           // elements of one thread between two rescales
+constexpr int CAP = 1024;          // candidates above the threshold held in shared memory
+constexpr int TIES = 256;          // candidates equal to it
+constexpr int MAX_CLUSTER = 8;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int MAX_SMEM = 160 * 1024;   // tile maxima of a CTA's share of the largest vocabulary
+
+struct ScoreParams {
+    const void* x;
+    long long ld;
+    int V;
+    int cluster;
+    int seg_vec;                   // 16-byte vectors of a row per CTA
+    int n_tiles;                   // tiles per CTA
+    const int* tokens;
+    int top;
+    float* logprob;
+    int* rank;
+    float* lse;
+    float* entropy;
+    int* top_ids;
+    float* top_lp;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {      // relative error 2^-22; 0 for -inf, NaN for NaN
+    float y;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Larger key = earlier in the order (value descending, id ascending).  -0 counts as +0.
+__device__ __forceinline__ unsigned long long order_key(float v, int id) {
+    const uint32_t b = __float_as_uint(v + 0.f);
+    const uint32_t o = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+    return ((unsigned long long)o << 32) | (uint32_t)~(uint32_t)id;
+}
+__device__ __forceinline__ float key_value(unsigned long long k) {
+    const uint32_t o = (uint32_t)(k >> 32);
+    return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
+}
+__device__ __forceinline__ int key_id(unsigned long long k) { return (int)~(uint32_t)k; }
+
+// The row as 16-byte vectors counted from the aligned address at or before its first element; `lead` elements in front
+// of the row belong to vector 0.  Elements outside the row read as -inf and are not touched in memory.
+template <typename T>
+struct Row {
+    static constexpr int E = 16 / (int)sizeof(T);
+    const T* p;
+    int lead, V;
+    __device__ __forceinline__ Row(const T* row, int V) : p(row), V(V) {
+        lead = (int)(((uintptr_t)row & 15) / sizeof(T));
+    }
+    __device__ __forceinline__ int first_id(int vec) const { return vec * E - lead; }
+    __device__ __forceinline__ void load(int vec, float* x) const {
+        const int i0 = first_id(vec);
+        if (i0 >= 0 && i0 + E <= V) {
+            const uint4 w = __ldg(reinterpret_cast<const uint4*>(p + i0));
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            if (sizeof(T) == 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(u[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[2 * e] = __uint_as_float(u[e] << 16);
+                    x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = (i0 + e >= 0 && i0 + e < V) ? to_f32(p[i0 + e]) : -INFINITY;
+        }
+    }
+};
+
+// 32 lanes' values sorted, largest in lane 0
+__device__ __forceinline__ float warp_sort_desc(float v, int lane) {
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1) {
+#pragma unroll
+        for (int o = size >> 1; o > 0; o >>= 1) {
+            const float w = __shfl_xor_sync(0xffffffffu, v, o);
+            const bool up = ((lane & size) == 0) == ((lane & o) == 0);    // this lane keeps the larger
+            v = up ? fmaxf(v, w) : fminf(v, w);
+        }
+    }
+    return v;
+}
+// the 32 largest of two lists of 32, both sorted with the largest first
+__device__ __forceinline__ float warp_merge_desc(float a, float b_reversed, int lane) {
+    float v = fmaxf(a, b_reversed);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float w = __shfl_xor_sync(0xffffffffu, v, o);
+        v = (lane & o) == 0 ? fmaxf(v, w) : fminf(v, w);
+    }
+    return v;
+}
+
+struct alignas(16) Partial {       // one CTA's share of a row
+    float m, s, t;
+    int before;
+};
+
+struct Shared {
+    unsigned long long top[MAX_CLUSTER][32];     // in the cluster's first CTA: every CTA's best, 0 = none
+    Partial part[MAX_CLUSTER];
+    unsigned long long cand[CAP];
+    unsigned long long tie[TIES];
+    unsigned long long best[32];                 // this CTA's best, in order
+    float list[NW][32];
+    Partial warp[NW];
+    int warp_count[NW];
+    int n_cand, n_tie;
+};
+
+// Appends, in id order, elements equal to `v` of the vectors [v0, v1) to best[n..], until `k` are there.  Whole CTA.
+template <typename T>
+__device__ int append_equal(const Row<T>& row, int v0, int v1, float v, unsigned long long* best, int n, int k, Shared& sh) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int b = v0; b < v1 && n < k; b += NT) {
+        const int vec = b + (int)threadIdx.x;
+        float x[Row<T>::E];
+        int c = 0;
+        if (vec < v1) {
+            row.load(vec, x);
+#pragma unroll
+            for (int e = 0; e < Row<T>::E; ++e) c += x[e] == v;
+        }
+        int inc = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int w = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += w;
+        }
+        if (lane == 31) sh.warp_count[warp] = inc;
+        __syncthreads();
+        int at = n + inc - c, total = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            if (w < warp) at += sh.warp_count[w];
+            total += sh.warp_count[w];
+        }
+        if (c) {
+#pragma unroll
+            for (int e = 0; e < Row<T>::E; ++e)
+                if (x[e] == v) {
+                    if (at < k) best[at] = order_key(v, row.first_id(vec) + e);
+                    ++at;
+                }
+        }
+        n += total;
+        __syncthreads();
+    }
+    return min(n, k);
+}
+
+// Largest element below `below` (strictly) among the vectors [v0, v1); -inf if there is none.  Whole CTA.
+template <typename T>
+__device__ float largest_below(const Row<T>& row, int v0, int v1, float below, Shared& sh) {
+    float m = -INFINITY;
+    for (int vec = v0 + (int)threadIdx.x; vec < v1; vec += NT) {
+        float x[Row<T>::E];
+        row.load(vec, x);
+#pragma unroll
+        for (int e = 0; e < Row<T>::E; ++e)
+            if (x[e] < below) m = fmaxf(m, x[e]);
+    }
+    m = warp_max(m);
+    if ((threadIdx.x & 31) == 0) sh.list[0][threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = sh.list[0][0];
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, sh.list[0][w]);
+    __syncthreads();
+    return m;
+}
+
+// This CTA's best `k` elements, in order, to best[0..k) (0 = none).  tile_max[tile][thread] holds the maxima, mine = the
+// largest of this thread's.
+template <typename T>
+__device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, const float* tile_max, float mine, int k,
+                                unsigned long long* best, Shared& sh) {
+    constexpr int VPT = TILE / Row<T>::E;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // k-th largest thread maximum
+    float v = warp_sort_desc(mine, lane);
+    sh.list[warp][lane] = v;
+    if (threadIdx.x < 32) best[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.n_cand = sh.n_tie = 0;
+    __syncthreads();
+#pragma unroll
+    for (int half = NW / 2; half > 0; half >>= 1) {
+        if (warp < half) {
+            v = warp_merge_desc(v, sh.list[warp + half][31 - lane], lane);
+            sh.list[warp][lane] = v;
+        }
+        __syncthreads();
+    }
+    const float thr = sh.list[0][k - 1];
+    const bool none_equal = thr == -INFINITY;                     // nothing is drawn from elements that are -inf
+    const bool many_equal = __syncthreads_count(mine == thr) > TIES / 2;
+    const bool equal_too = !none_equal && !many_equal;
+    if (mine > thr || (equal_too && mine == thr)) {
+        for (int i = 0; i < n_tiles; ++i) {
+            const float tm = tile_max[i * NT + threadIdx.x];
+            if (!(tm > thr || (equal_too && tm == thr))) continue;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                const int vec = v0 + (i * VPT + j) * NT + (int)threadIdx.x;
+                if (vec >= v1) continue;
+                float x[Row<T>::E];
+                row.load(vec, x);
+#pragma unroll
+                for (int e = 0; e < Row<T>::E; ++e) {
+                    if (x[e] > thr) {
+                        const int at = atomicAdd(&sh.n_cand, 1);
+                        if (at < CAP) sh.cand[at] = order_key(x[e], row.first_id(vec) + e);
+                    } else if (equal_too && x[e] == thr) {
+                        const int at = atomicAdd(&sh.n_tie, 1);
+                        if (at < TIES) sh.tie[at] = order_key(thr, row.first_id(vec) + e);
+                    }
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const int n = sh.n_cand, n_tie = sh.n_tie;
+    if (n > CAP) {
+        // More elements above the bound than are held here (a few threads own most of the large ones): value by value.
+        int got = 0;
+        float below = INFINITY;
+        while (got < k) {
+            const float top = largest_below(row, v0, v1, below, sh);
+            if (top == -INFINITY) break;
+            got = append_equal(row, v0, v1, top, best, got, k, sh);
+            below = top;
+        }
+        __syncthreads();
+        return;
+    }
+    // position of each candidate = how many others come before it
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const unsigned long long key = sh.cand[i];
+        int pos = 0;
+        for (int j = 0; j < n; ++j) pos += sh.cand[j] > key;
+        if (pos < k) best[pos] = key;
+    }
+    if (!none_equal && n < k) {
+        if (!many_equal && n_tie <= TIES) {
+            for (int i = threadIdx.x; i < n_tie; i += NT) {
+                const unsigned long long key = sh.tie[i];
+                int pos = n;
+                for (int j = 0; j < n_tie; ++j) pos += sh.tie[j] > key;
+                if (pos < k) best[pos] = key;
+            }
+        } else {
+            append_equal(row, v0, v1, thr, best, n, k, sh);
+        }
+    }
+    __syncthreads();
+}
+
+// Adds (m, s, t) of one part to another: sums rescaled to the common maximum.  t is kept in units of log 2.
+__device__ __forceinline__ void merge(float& m, float& s, float& t, float m2, float s2, float t2) {
+    const float M = fmaxf(m, m2);
+    const float d1 = fmaxf((m - M) * LOG2E, -300.f), d2 = fmaxf((m2 - M) * LOG2E, -300.f);      // 2^-300 is 0 in fp32
+    const float f1 = exp2_fast(d1), f2 = exp2_fast(d2);
+    t = f1 * (t + d1 * s) + f2 * (t2 + d2 * s2);
+    s = f1 * s + f2 * s2;
+    m = M;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
+    constexpr int E = Row<T>::E, VPT = TILE / E;
+    extern __shared__ float tile_max[];          // [n_tiles][NT], used when alternatives are asked for
+    __shared__ Shared sh;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int C = p.cluster;
+    const uint32_t rank = C > 1 ? cluster_rank() : 0u;
+    const long long r = blockIdx.x / (unsigned)C;
+    if (C > 1) cluster_arrive();                 // every CTA of the cluster has started: waited for before the remote stores
+    pdl_wait();
+    pdl_launch();
+
+    const Row<T> row(reinterpret_cast<const T*>(p.x) + r * p.ld, p.V);
+    const int n_vec = (row.lead + p.V + E - 1) / E;
+    const int v0 = min(n_vec, (int)rank * p.seg_vec), v1 = min(n_vec, v0 + p.seg_vec);
+
+    const int token = p.tokens ? p.tokens[r] : -1;
+    const bool has_token = token >= 0 && token < p.V;
+    const float x_t = has_token ? to_f32(row.p[token]) : 0.f;
+    const float x_next = nextafterf(x_t, INFINITY);      // x >= x_next is x > x_t
+
+    float m = -FLT_MAX, s = 0.f, t = 0.f, mine = -INFINITY;
+    int before = 0;
+    float x[TILE], nx[TILE];
+    auto fetch = [&](int i, float* to) {
+        const int vt = v0 + i * VPT * NT + (int)threadIdx.x;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            if (vt + j * NT < v1) row.load(vt + j * NT, to + j * E);
+            else
+#pragma unroll
+                for (int e = 0; e < E; ++e) to[j * E + e] = -INFINITY;
+        }
+    };
+    fetch(0, nx);
+    for (int i = 0; i < p.n_tiles; ++i) {
+#pragma unroll
+        for (int e = 0; e < TILE; ++e) x[e] = nx[e];
+        if (i + 1 < p.n_tiles) fetch(i + 1, nx);
+        float tm = x[0];
+#pragma unroll
+        for (int e = 1; e < TILE; ++e) tm = fmaxf(tm, x[e]);
+        if (p.top) tile_max[i * NT + threadIdx.x] = tm;
+        mine = fmaxf(mine, tm);
+        const float m1 = fmaxf(m, tm), d = fmaxf((m - m1) * LOG2E, -300.f), f = exp2_fast(d);
+        t = f * (t + d * s);
+        s = f * s;
+        m = m1;
+#pragma unroll
+        for (int e = 0; e < TILE; ++e) {
+            const float u = (x[e] - m) * LOG2E;
+            const float ex = exp2_fast(u);       // NaN for a NaN, and for +inf (m is +inf then): such a row is reported as NaN
+            s += ex;
+            t += fmaxf(u, -300.f) * ex;
+        }
+        if (has_token) {
+            const int vt = v0 + i * VPT * NT + (int)threadIdx.x;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                const int i0 = row.first_id(vt + j * NT);
+                if (vt + j * NT >= v1) continue;
+                if (i0 < 0 || (i0 <= token && token < i0 + E)) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) before += i0 + e >= 0 && x[j * E + e] >= (i0 + e < token ? x_t : x_next);
+                } else {
+                    // behind the row's end lie elements read as -inf: never >= x_next
+                    const float bar = i0 < token ? x_t : x_next;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) before += x[j * E + e] >= bar;
+                }
+            }
+        }
+    }
+    // the CTA's sums, merged in a fixed order
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o),
+                    t2 = __shfl_xor_sync(0xffffffffu, t, o);
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+        merge(m, s, t, m2, s2, t2);
+    }
+    if (lane == 0) sh.warp[warp] = Partial{m, s, t, before};
+    __syncthreads();
+    Partial part = sh.warp[0];
+    if (warp == 0) {
+        part = sh.warp[lane & (NW - 1)];
+#pragma unroll
+        for (int o = NW / 2; o > 0; o >>= 1) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, part.m, o), s2 = __shfl_xor_sync(0xffffffffu, part.s, o),
+                        t2 = __shfl_xor_sync(0xffffffffu, part.t, o);
+            part.before += __shfl_xor_sync(0xffffffffu, part.before, o);
+            merge(part.m, part.s, part.t, m2, s2, t2);
+        }
+    }
+    if (p.top) best_of_segment(row, v0, v1, p.n_tiles, tile_max, mine, p.top, sh.best, sh);
+
+    if (C > 1) {
+        cluster_wait();
+        const uint32_t top0 = cluster_map((uint32_t)__cvta_generic_to_shared(&sh.top[rank][0]), 0);
+        const uint32_t part0 = cluster_map((uint32_t)__cvta_generic_to_shared(&sh.part[rank]), 0);
+        if (p.top && (int)threadIdx.x < p.top)
+            asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(top0 + 8 * threadIdx.x), "l"(sh.best[threadIdx.x]) : "memory");
+        if (threadIdx.x == 0)
+            asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part0), "r"(__float_as_uint(part.m)),
+                         "r"(__float_as_uint(part.s)), "r"(__float_as_uint(part.t)), "r"(part.before)
+                         : "memory");
+        cluster_arrive();
+        cluster_wait();
+        if (rank != 0) return;
+        part = sh.part[0];
+        for (int c = 1; c < C; ++c) {
+            merge(part.m, part.s, part.t, sh.part[c].m, sh.part[c].s, sh.part[c].t);
+            part.before += sh.part[c].before;
+        }
+    } else if (threadIdx.x == 0) {
+        sh.part[0] = part;
+    }
+    if (C == 1) {
+        __syncthreads();
+        part = sh.part[0];
+    }
+    const bool undefined = isnan(part.s);
+    const float log_s = logf(part.s);
+    if (threadIdx.x == 0) {
+        const float nan = __int_as_float(0x7fffffff);
+        const bool empty = part.s == 0.f;        // every logit is -inf
+        if (p.lse) p.lse[r] = undefined ? nan : empty ? -INFINITY : part.m + log_s;
+        if (p.entropy) p.entropy[r] = undefined ? nan : empty ? 0.f : log_s - part.t * LN2 / part.s;
+        if (p.logprob) p.logprob[r] = undefined || !has_token ? nan : empty ? -INFINITY : (x_t - part.m) - log_s;
+        if (p.rank) p.rank[r] = undefined || !has_token ? -1 : part.before;
+    }
+    if (!p.top) return;
+    if (C > 1) {
+        // C lists, each in order: the position of a key is the number of keys before it in all lists
+        if (threadIdx.x < 32) sh.best[threadIdx.x] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < C * p.top; i += NT) {
+            const unsigned long long key = sh.top[i / p.top][i % p.top];
+            if (!key) continue;
+            int pos = 0;
+            for (int c = 0; c < C; ++c)
+                for (int j = 0; j < p.top && sh.top[c][j] > key; ++j) ++pos;
+            if (pos < p.top) sh.best[pos] = key;
+        }
+        __syncthreads();
+    }
+    if ((int)threadIdx.x < p.top) {
+        const unsigned long long key = sh.best[threadIdx.x];
+        const bool some = key != 0 && !undefined;
+        const long long at = r * p.top + threadIdx.x;
+        if (p.top_ids) p.top_ids[at] = some ? key_id(key) : -1;
+        if (p.top_lp)
+            p.top_lp[at] = undefined ? __int_as_float(0x7fffffff) : some ? (key_value(key) - part.m) - log_s : -INFINITY;
+    }
+}
+
+template <typename T>
+int run(const ops::Device* dev, ScoreParams p, long long rows, cudaStream_t st) {
+    constexpr int E = Row<T>::E, VPT = TILE / E;
+    // vectors of a row, whatever its alignment
+    const int n_vec = (p.V + E - 2) / E + 1;
+    const int tiles = (n_vec + VPT * NT - 1) / (VPT * NT);
+    // CTAs per row: enough rows fill the GPU by themselves; fewer rows are cut while a CTA keeps a tile of its own
+    int c = 1;
+    while (c < MAX_CLUSTER && c < tiles && (rows * c < 8LL * dev->n_sms || (p.top && (tiles + c - 1) / c > 64))) c *= 2;
+    p.cluster = c;
+    p.n_tiles = (tiles + c - 1) / c;
+    p.seg_vec = p.n_tiles * VPT * NT;
+    const size_t smem = p.top ? (size_t)p.n_tiles * NT * 4 : 0;
+    if (rows * c > 0x7fffffffLL) return ops::fail(S2D2_ERR_UNSUPPORTED, "score_logits: too many rows");
+    static std::atomic<bool> raised[64];
+    if (!raised[dev->id].load(std::memory_order_acquire)) {
+        cudaError_t e = cudaFuncSetAttribute(score_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
+        if (e != cudaSuccess) return ops::fail(S2D2_ERR_CUDA, "score_logits: %s", cudaGetErrorString(e));
+        raised[dev->id].store(true, std::memory_order_release);
+    }
+    const cudaError_t e = ops::launch(score_kernel<T>, dim3((unsigned)(rows * c)), NT, smem, c, st, p);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return ops::fail(S2D2_ERR_CUDA, "score_logits: %s", cudaGetErrorString(e));
+    }
+    return S2D2_OK;
+}
+
+}  // namespace
+}  // namespace s2d2
+
+using namespace s2d2;
+
+extern "C" int s2d2_score_logits(const void* d_logits, int32_t dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                                 const int32_t* d_tokens, int32_t top_k, float* d_logprob, int32_t* d_rank, float* d_lse,
+                                 float* d_entropy, int32_t* d_top_ids, float* d_top_logprobs, void* cuda_stream) {
+    ops::clear_error();
+    if (dtype != S2D2_DTYPE_F32 && dtype != S2D2_DTYPE_BF16) return ops::fail(S2D2_ERR_INVALID, "score_logits: dtype");
+    if (n_rows < 0) return ops::fail(S2D2_ERR_INVALID, "score_logits: n_rows is negative");
+    if (vocab < 1 || vocab > S2D2_SCORE_MAX_VOCAB)
+        return ops::fail(S2D2_ERR_INVALID, "score_logits: vocab must be in 1..%d", S2D2_SCORE_MAX_VOCAB);
+    if (row_stride < vocab) return ops::fail(S2D2_ERR_INVALID, "score_logits: row_stride is smaller than vocab");
+    if (n_rows > 0 && row_stride > (INT64_MAX >> 3) / n_rows) return ops::fail(S2D2_ERR_INVALID, "score_logits: row_stride is too large");
+    if (top_k < 0 || top_k > S2D2_SCORE_MAX_TOP)
+        return ops::fail(S2D2_ERR_INVALID, "score_logits: top_k must be in 0..%d", S2D2_SCORE_MAX_TOP);
+    if ((d_logprob || d_rank) && !d_tokens) return ops::fail(S2D2_ERR_INVALID, "score_logits: log probability and rank need tokens");
+    if (top_k > 0 && !d_top_ids && !d_top_logprobs) return ops::fail(S2D2_ERR_INVALID, "score_logits: top_k without an output for it");
+    if (top_k == 0 && (d_top_ids || d_top_logprobs)) return ops::fail(S2D2_ERR_INVALID, "score_logits: outputs for alternatives, but top_k is 0");
+    if (!d_logprob && !d_rank && !d_lse && !d_entropy && !top_k) return ops::fail(S2D2_ERR_INVALID, "score_logits: no output");
+    const ops::Device* dev;
+    if (int rc = ops::device(&dev)) return rc;
+    if (n_rows == 0) return S2D2_OK;
+    const struct {
+        const void* p;
+        size_t align;
+        const char* name;
+    } ptrs[] = {{d_logits, dtype == S2D2_DTYPE_F32 ? 4u : 2u, "logits"}, {d_tokens, 4, "tokens"}, {d_logprob, 4, "logprob"},
+                {d_rank, 4, "rank"}, {d_lse, 4, "lse"}, {d_entropy, 4, "entropy"}, {d_top_ids, 4, "top_ids"},
+                {d_top_logprobs, 4, "top_logprobs"}};
+    for (int i = 0; i < 8; ++i)
+        if (i == 0 || ptrs[i].p)
+            if (int rc = ops::check_ptr(dev, ptrs[i].p, ptrs[i].align, ptrs[i].name)) return rc;
+    ScoreParams p = {};
+    p.x = d_logits;
+    p.ld = row_stride;
+    p.V = vocab;
+    p.tokens = d_tokens;
+    p.top = top_k;
+    p.logprob = d_logprob;
+    p.rank = d_rank;
+    p.lse = d_lse;
+    p.entropy = d_entropy;
+    p.top_ids = d_top_ids;
+    p.top_lp = d_top_logprobs;
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    return dtype == S2D2_DTYPE_F32 ? run<float>(dev, p, n_rows, st) : run<bf16>(dev, p, n_rows, st);
+}

@@ -1,0 +1,206 @@
+"""MXFP4 quantisation and product on the GPU against 64-bit restatements on the CPU."""
+import numpy as np
+import pytest
+
+from tests import ops_util as ou
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def s2d2():
+    import paper_2603_25702_b200 as m
+    return m
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def quantize(s2d2, x, guard=64):
+    """codes, scales (with `guard` untouched bytes behind each) of a 2-d device tensor."""
+    name = "fp32" if x.dtype == torch.float32 else "bf16"
+    nc, ns = s2d2.mxfp4_sizes(*x.shape)
+    codes, scales = (torch.full((n + guard,), 0xA5, dtype=torch.uint8, device="cuda") for n in (nc, ns))
+    s2d2.mxfp4_quantize(x.data_ptr(), name, x.shape[0], x.shape[1], x.stride(0), codes.data_ptr(), scales.data_ptr(), stream())
+    return codes, scales
+
+
+def check_codes(x64, codes, scales):
+    want_c, want_s = ou.mxfp4_encode(x64)
+    want_s = ou.tile_scales(want_s)
+    got_c, got_s = codes.cpu().numpy(), scales.cpu().numpy()
+    assert np.array_equal(got_c[:want_c.size].reshape(want_c.shape), want_c)
+    assert np.array_equal(got_s[:want_s.size], want_s)
+    assert (got_c[want_c.size:] == 0xA5).all() and (got_s[want_s.size:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,pad,lead", [(1, 1, 0, 0), (1, 31, 1, 0), (3, 33, 0, 0), (5, 128, 0, 0), (129, 257, 7, 3),
+                                                (128, 512, 0, 1), (300, 1000, 24, 8), (1, 4096, 0, 0), (257, 40, 0, 0)])
+def test_quantize_and_back(s2d2, dtype, rows, cols, pad, lead):
+    """Every code and scale byte, padding too, and the values they stand for; odd strides and unaligned first elements."""
+    g = torch.Generator(device="cuda").manual_seed(rows * 1000 + cols)
+    buf = torch.randn(rows * (cols + pad) + lead, generator=g, device="cuda")
+    buf *= torch.exp(3 * torch.randn(buf.shape, generator=g, device="cuda"))
+    x = buf.to(DT[dtype])[lead:].view(rows, cols + pad)[:, :cols]
+    codes, scales = quantize(s2d2, x)
+    x64 = x.double().cpu().numpy()
+    check_codes(x64, codes, scales)
+    want = ou.mxfp4_values(*ou.mxfp4_encode(x64), cols)
+    for out in ("fp32", "bf16"):
+        y = torch.full((rows * (cols + pad) + lead,), 7.0, dtype=DT[out], device="cuda")
+        yv = y[lead:].view(rows, cols + pad)
+        s2d2.mxfp4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, yv.data_ptr(), out, cols + pad, stream())
+        assert np.array_equal(yv[:, :cols].double().cpu().numpy(), want)          # exact in both types
+        assert (yv[:, cols:] == 7).all() and (y[:lead] == 7).all()
+
+
+def test_quantize_special_values(s2d2):
+    big = np.finfo(np.float32).max
+    sub = 2.0 ** -149
+    rows = [[6, -6, 5, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25, -0.25, -0.75, -5], [7, 7.999, -7.5, 6.001], [0.0, -0.0], [big, -big, big / 8],
+            [sub, -sub, 3 * sub], [2.0 ** -126, 2.0 ** -127, -(2.0 ** -128)], [np.inf, 1], [np.nan, 1], [-np.inf, np.nan],
+            [1.0, 2.0 ** -30], [2.0 ** -124, 2.0 ** -127, 3 * 2.0 ** -128]]
+    x = np.zeros((len(rows), 64), np.float32)
+    for i, r in enumerate(rows):
+        x[i, :len(r)] = r
+        x[i, 40] = 1.0                                                            # a second, ordinary block
+    codes, scales = quantize(s2d2, torch.from_numpy(x).cuda())
+    check_codes(x.astype(np.float64), codes, scales)
+    y = torch.empty(x.shape, device="cuda")
+    s2d2.mxfp4_dequantize(codes.data_ptr(), scales.data_ptr(), *x.shape, y.data_ptr(), "fp32", 64, stream())
+    assert np.array_equal(y.double().cpu().numpy(), ou.mxfp4_values(*ou.mxfp4_encode(x.astype(np.float64)), 64), equal_nan=True)
+
+
+def operand(rows, K, seed, scale=1.0):
+    g = np.random.default_rng(seed)
+    x = (g.standard_normal((rows, K)) * np.exp(g.standard_normal((rows, 1)))).astype(np.float32) * np.float32(scale)
+    codes, s = ou.mxfp4_encode(x.astype(np.float64))
+    return (torch.from_numpy(codes).cuda(), torch.from_numpy(ou.tile_scales(s)).cuda()), ou.mxfp4_values(codes, s, K)
+
+
+def product_tolerance(xv, wv, scale, y_type):
+    """Products of e2m1 codes and powers of two are exact; the sum rounds (or truncates, hence 2^-23) once per 64 elements and a few
+    times where k is split; then the scale and y's type."""
+    size = (np.abs(xv) @ np.abs(wv).T) * abs(scale)
+    y = np.abs(xv @ wv.T) * abs(scale)
+    K = xv.shape[1]
+    return size * ((K + 63) // 64 + 10) * 2.0 ** -23 + y * (2.0 ** -23 + (2.0 ** -8 if y_type == "bf16" else 0.0)) + 1e-37
+
+
+SHAPES = [(1, 1, 1), (1, 128, 32), (2, 8, 33), (16, 127, 64), (17, 129, 65), (5, 256, 256), (3, 130, 257), (33, 1000, 512),
+          (64, 384, 4096), (1, 4096, 4096), (65, 200, 300), (77, 1001, 2050), (128, 256, 1024), (129, 300, 700), (200, 128, 96),
+          (256, 512, 512), (300, 640, 1000), (513, 257, 288)]
+
+
+@pytest.mark.parametrize("y_type", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_product(s2d2, M, N, K, y_type):
+    (xc, xs), xv = operand(M, K, M * 7 + K)
+    (wc, ws), wv = operand(N, K, N * 3 + K, 0.02)
+    pad, scale = 5, 0.75
+    y = torch.full((M + 1, N + pad), 7.0, dtype=DT[y_type], device="cuda")
+    s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), y_type, M, N, K, N + pad, scale, stream())
+    s2d2.ops_status(stream())
+    got = y.double().cpu().numpy()
+    want = scale * (xv @ wv.T)
+    err, tol = np.abs(got[:M, :N] - want), product_tolerance(xv, wv, scale, y_type)
+    assert np.isfinite(got).all() and (err <= tol).all(), (err.max(), (err / tol).max())
+    assert (got[:M, N:] == 7).all() and (got[M:] == 7).all()
+
+
+def test_product_of_head_rows(s2d2):
+    """A head of 100 000 rows: more tiles than CTAs fit at once; a sample of the columns is checked."""
+    M, N, K = 3, 100000, 512
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.randn(N, K, generator=g, device="cuda") * 0.02
+    wc, ws = quantize(s2d2, w, 0)
+    (xc, xs), xv = operand(M, K, 5)
+    y = torch.empty(M, N, device="cuda")
+    s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "fp32", M, N, K, stream=stream())
+    s2d2.ops_status(stream())
+    at = np.r_[0:200, 50000:50200, N - 200:N]
+    wv = ou.mxfp4_values(*ou.mxfp4_encode(w[at].double().cpu().numpy()), K)
+    err = np.abs(y[:, at].double().cpu().numpy() - xv @ wv.T)
+    assert (err <= product_tolerance(xv, wv, 1.0, "fp32")).all()
+
+
+@pytest.mark.parametrize("M", [3, 200])
+def test_nan_blocks_stay_in_their_rows(s2d2, M):
+    N, K = 140, 192
+    g = np.random.default_rng(9)
+    x, w = g.standard_normal((M, K)).astype(np.float32), g.standard_normal((N, K)).astype(np.float32)
+    x[1, 70], w[130, 5] = np.nan, np.inf
+    xc, xs = quantize(s2d2, torch.from_numpy(x).cuda(), 0)
+    wc, ws = quantize(s2d2, torch.from_numpy(w).cuda(), 0)
+    y = torch.empty(M, N, device="cuda")
+    s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "fp32", M, N, K, stream=stream())
+    bad = np.zeros((M, N), bool)
+    bad[1], bad[:, 130] = True, True
+    assert np.array_equal(np.isnan(y.cpu().numpy()), bad)
+
+
+def test_empty_batch_and_bad_pointers(s2d2):
+    y = torch.full((4,), 7.0, device="cuda")
+    s2d2.mxfp4_gemm(0, 0, 0, 0, 0, "fp32", 0, 4, 32, stream=stream())
+    s2d2.mxfp4_quantize(0, "fp32", 0, 32, 32, 0, 0, stream())
+    host = torch.zeros(64)
+    q = torch.zeros(1024, dtype=torch.uint8, device="cuda")
+    for args in [(0, q.data_ptr(), q.data_ptr()), (y.data_ptr(), 0, q.data_ptr()), (y.data_ptr(), q.data_ptr() + 8, q.data_ptr()),
+                 (host.data_ptr(), q.data_ptr(), q.data_ptr()), (y.data_ptr() + 2, q.data_ptr(), q.data_ptr())]:
+        with pytest.raises(s2d2.S2D2Error) as e:
+            s2d2.mxfp4_quantize(args[0], "fp32", 1, 4, 4, args[1], args[2], stream())
+        assert e.value.code == -1
+    assert (y == 7).all()
+
+
+def test_repeated_calls_agree_bit_for_bit(s2d2):
+    for M, N, K in [(1, 640, 4096), (40, 300, 2048), (300, 640, 1024)]:
+        (xc, xs), _ = operand(M, K, 1)
+        (wc, ws), _ = operand(N, K, 2)
+        ys = [torch.empty(M, N, device="cuda") for _ in range(4)]
+        for y in ys:
+            s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "fp32", M, N, K, stream=stream())
+        assert all(torch.equal(ys[0], y) for y in ys[1:])
+
+
+def test_captured_and_concurrent_calls(s2d2):
+    """quantise + product in two captured graphs, replayed on two streams at a time with new inputs: nothing is shared."""
+    N, K = 384, 2048
+    w = torch.randn(N, K, device="cuda") * 0.05
+    wc, ws = quantize(s2d2, w, 0)
+    wv = ou.mxfp4_values(*ou.mxfp4_encode(w.double().cpu().numpy()), K)
+    graphs = []
+    for M in (9, 260):
+        x = torch.zeros(M, K, device="cuda")
+        nc, ns = s2d2.mxfp4_sizes(M, K)
+        xc, xs = torch.empty(nc, dtype=torch.uint8, device="cuda"), torch.empty(ns, dtype=torch.uint8, device="cuda")
+        y = torch.empty(M, N, device="cuda")
+
+        def call():
+            s2d2.mxfp4_quantize(x.data_ptr(), "fp32", M, K, K, xc.data_ptr(), xs.data_ptr(), stream())
+            s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "fp32", M, N, K, stream=stream())
+
+        call()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        graphs.append((g, x, y, M, (xc, xs), torch.cuda.Stream()))
+    for trial in range(3):
+        for g, x, y, M, _, st in graphs:
+            x.copy_(torch.randn(M, K, generator=torch.Generator().manual_seed(trial * 10 + M)))
+        torch.cuda.synchronize()
+        for g, x, y, M, _, st in graphs:
+            with torch.cuda.stream(st):
+                for _ in range(3):
+                    g.replay()
+        torch.cuda.synchronize()
+        for g, x, y, M, _, st in graphs:
+            xv = ou.mxfp4_values(*ou.mxfp4_encode(x.double().cpu().numpy()), K)
+            err = np.abs(y.double().cpu().numpy() - xv @ wv.T)
+            assert (err <= product_tolerance(xv, wv, 1.0, "fp32")).all()
