@@ -437,6 +437,14 @@ int s2d2_score_logits(const void* d_logits, int32_t dtype, int64_t n_rows, int32
                       const int32_t* d_tokens, int32_t top_k, float* d_logprob, int32_t* d_rank, float* d_lse,
                       float* d_entropy, int32_t* d_top_ids, float* d_top_logprobs, void* cuda_stream);
 
+/* The same scores (without rank and alternatives) of the logits scale * x w^T, x [M, K] hidden rows and w [N, K] the head,
+ * both MXFP4; the logits never reach memory.  d_ws: at least s2d2_mxfp4_score_workspace bytes, 16-byte aligned, used by this call
+ * alone while it runs.  A row with a logit that is not finite gives NaN.  M = 0 does nothing. */
+int s2d2_mxfp4_score_workspace(int32_t M, int32_t N, int32_t K, int64_t* bytes);
+int s2d2_mxfp4_score(const void* d_x_codes, const void* d_x_scales, const void* d_w_codes, const void* d_w_scales, int32_t M,
+                     int32_t N, int32_t K, float scale, const int32_t* d_tokens, float* d_logprob, float* d_lse,
+                     float* d_entropy, void* d_ws, int64_t ws_bytes, void* cuda_stream);
+
 /* s2d2_score_logits on the logits that the last draft pass (which = 0) or verifier pass (which = 1) of a context left
  * behind: rows as s2d2_debug_copy_logits lists them, n_rows of them from the first one on.  Host pointers; outputs
  * [n_rows] and [n_rows, top_k], each may be NULL as above.  Synchronous. */

@@ -13,6 +13,8 @@ from .binding import (  # noqa: F401
     mxfp4_dequantize,
     mxfp4_gemm,
     mxfp4_quantize,
+    mxfp4_score,
+    mxfp4_score_workspace,
     mxfp4_sizes,
     ops_status,
     score_logits,

@@ -82,7 +82,7 @@ EXPORTS = [
     "s2d2_debug_copy_kv", "s2d2_debug_seq_state", "s2d2_debug_gemm", "s2d2_debug_gemm2", "s2d2_debug_gemm_swiglu", "s2d2_debug_copy_expert_ids", "s2d2_debug_pass_trace", "s2d2_debug_wait_timeout",
     "s2d2_gemm_bf16_noalloc", "s2d2_noalloc_last_error",
     "s2d2_ops_last_error", "s2d2_ops_status", "s2d2_mxfp4_sizes", "s2d2_mxfp4_quantize", "s2d2_mxfp4_dequantize",
-    "s2d2_mxfp4_gemm", "s2d2_score_logits", "s2d2_score_pass",
+    "s2d2_mxfp4_gemm", "s2d2_mxfp4_score_workspace", "s2d2_mxfp4_score", "s2d2_score_logits", "s2d2_score_pass",
 ]
 _TEXTS = ("s2d2_last_error", "s2d2_noalloc_last_error", "s2d2_ops_last_error")     # these return a string
 
@@ -150,6 +150,8 @@ def load_library() -> C.CDLL:
     lib.s2d2_mxfp4_quantize.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
     lib.s2d2_mxfp4_dequantize.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]
     lib.s2d2_mxfp4_gemm.argtypes = [C.c_void_p] * 5 + [C.c_int32] * 4 + [C.c_int64, C.c_float, C.c_void_p]
+    lib.s2d2_mxfp4_score_workspace.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
+    lib.s2d2_mxfp4_score.argtypes = [C.c_void_p] * 4 + [C.c_int32] * 3 + [C.c_float] + [C.c_void_p] * 5 + [C.c_int64, C.c_void_p]
     lib.s2d2_score_logits.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_int32] + [C.c_void_p] * 7
     lib.s2d2_score_pass.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32] + [C.c_void_p] * 6
     _LIB = lib
@@ -230,6 +232,23 @@ def score_logits(d_logits: int, dtype: str, n_rows: int, vocab: int, row_stride:
     lib = load_library()
     _ops_check(lib.s2d2_score_logits(d_logits, _dtype(dtype), n_rows, vocab, row_stride, d_tokens, top_k, d_logprob, d_rank, d_lse,
                                      d_entropy, d_top_ids, d_top_logprobs, stream))
+
+
+def mxfp4_score_workspace(M: int, N: int, K: int) -> int:
+    """Bytes of workspace that mxfp4_score needs."""
+    lib = load_library()
+    n = C.c_int64()
+    _ops_check(lib.s2d2_mxfp4_score_workspace(M, N, K, C.byref(n)))
+    return n.value
+
+
+def mxfp4_score(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int, M: int, N: int, K: int, d_tokens: int, d_ws: int,
+                ws_bytes: int, *, scale: float = 1.0, d_logprob: int = 0, d_lse: int = 0, d_entropy: int = 0, stream: int = 0) -> None:
+    """Log probability of one token per row, log-sum-exp and entropy of the logits scale * x w^T (x [M, K] hidden rows, w [N, K]
+    the head, both MXFP4) without the logits in memory.  ``d_ws``: mxfp4_score_workspace bytes.  Asynchronous."""
+    lib = load_library()
+    _ops_check(lib.s2d2_mxfp4_score(d_x_codes, d_x_scales, d_w_codes, d_w_scales, M, N, K, scale, d_tokens, d_logprob, d_lse, d_entropy,
+                                    d_ws, ws_bytes, stream))
 
 
 class Engine:

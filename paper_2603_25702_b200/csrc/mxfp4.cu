@@ -202,24 +202,23 @@ int encode_codes(const ops::Device* dev, CUtensorMap* map, const void* codes, in
     return r == CUDA_SUCCESS ? S2D2_OK : ops::fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
-int raise_limits(const ops::Device* dev) {
+constexpr int MAX_SMEM = 227 * 1024;
+
+template <int CG, bool SCORE>
+int raise_limit(const ops::Device* dev) {
     static std::atomic<bool> done[64];
     if (done[dev->id].load(std::memory_order_acquire)) return S2D2_OK;
-    const cudaError_t e = cudaFuncSetAttribute(mx::stream_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, mx::STREAM_MAX_SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(mx::product_kernel<CG, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
     if (e != cudaSuccess) return ops::fail(S2D2_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     done[dev->id].store(true, std::memory_order_release);
     return S2D2_OK;
 }
 
-int check_product(const char* op, const ops::Device* dev, const void* xc, const void* xs, const void* wc, const void* ws, int M, int N,
-                  int K) {
-    if (M > 0) {
-        if (int rc = ops::check_ptr(dev, xc, 16, "x_codes")) return rc;
-        if (int rc = ops::check_ptr(dev, xs, 16, "x_scales")) return rc;
-        if (int rc = ops::check_ptr(dev, wc, 16, "w_codes")) return rc;
-        if (int rc = ops::check_ptr(dev, ws, 16, "w_scales")) return rc;
-    }
-    return S2D2_OK;
+int check_operands(const ops::Device* dev, const void* xc, const void* xs, const void* wc, const void* ws) {
+    if (int rc = ops::check_ptr(dev, xc, 16, "x_codes")) return rc;
+    if (int rc = ops::check_ptr(dev, xs, 16, "x_scales")) return rc;
+    if (int rc = ops::check_ptr(dev, wc, 16, "w_codes")) return rc;
+    return ops::check_ptr(dev, ws, 16, "w_scales");
 }
 int check_product_shape(const char* op, int M, int N, int K) {
     if (M < 0 || M > S2D2_MXFP4_MAX_DIM) return ops::fail(S2D2_ERR_INVALID, "%s: M must be in 0..%d", op, S2D2_MXFP4_MAX_DIM);
@@ -228,30 +227,134 @@ int check_product_shape(const char* op, int M, int N, int K) {
     return S2D2_OK;
 }
 
-int launch_stream(const ops::Device* dev, mx::GemmParams p, const void* xc, const void* wc, cudaStream_t st) {
-    p.T = std::min(128, (p.M + 15) / 16 * 16);
-    p.m_tiles = (p.M + p.T - 1) / p.T;
-    p.x_tiles = 1;                             // T divides 128, or there is one tile
-    const int n_tiles = (p.N + mx::ROWS - 1) / mx::ROWS;
-    const long long tiles = (long long)n_tiles * p.m_tiles;
-    const int sbytes = mx::stage_bytes(p.T, p.x_tiles);
-    // k splits: as many CTAs as fit at once (two per SM) while each keeps at least two k-blocks
+int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// Scale tiles of a [rows, K] matrix as rows of 512 bytes, two at a time (one k-block).
+int encode_scales(const ops::Device* dev, CUtensorMap* map, const void* scales, int rows, int K) {
+    cuuint64_t dims[2] = {mx::SF_TILE / 4, (cuuint64_t)ceil_div(rows, 128) * ceil_div(ceil_div(K, 32), 4)}, strides[1] = {mx::SF_TILE};
+    cuuint32_t box[2] = {mx::SF_TILE / 4, 2}, step[2] = {1, 1};
+    const CUresult r = dev->encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(scales), dims, strides, box, step,
+                                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? S2D2_OK : ops::fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+struct Plan {
+    mx::Params p = {};
+    int cg = 1, grid = 0, smem = 0;
+};
+
+// Accumulators, tensor-memory columns, shared memory and ring depth once tiles, T, sf_tiles and splits are known.
+void finish_plan(Plan& plan, long long tiles_per_cluster, int stages_wanted) {
+    mx::Params& p = plan.p;
+    p.n_acc = tiles_per_cluster > 1 ? 2 : 1;
+    const int used = mx::used_columns(p.T, p.sf_tiles, p.n_acc);
+    p.tmem_cols = 32;
+    while ((int)p.tmem_cols < used) p.tmem_cols *= 2;
+    const int sbytes = mx::stage_bytes(plan.cg, p.a_box, p.T, p.sf_tiles), fixed = 1024 + (int)sizeof(mx::Control),
+              pad = mx::ring_bytes(plan.cg, 0, p.a_box, p.T, p.sf_tiles);
+    // one CTA's ring never needs more than half an SM's memory when the tile is small: the next kernel's set-up fits beside it
+    const int room = (p.tmem_cols <= 256 && plan.cg == 1 ? 113 * 1024 : MAX_SMEM) - fixed;
+    p.stages = std::max(2, std::min(std::min(mx::MAX_STAGES, (room - pad) / sbytes), stages_wanted));
+    p.control_at = std::max(mx::ring_bytes(plan.cg, p.stages, p.a_box, p.T, p.sf_tiles), p.splits > 1 ? p.T * mx::ROWS * 4 : 0);
+    plan.smem = std::max(fixed + p.control_at, mx::min_smem(p.tmem_cols));
+}
+
+void plan_product(Plan& plan, int n_sms, int M, int N, int K) {
+    mx::Params& p = plan.p;
+    p.a_rows = N;
+    p.b_rows = M;
+    p.K = K;
+    p.kb_total = ceil_div(K, mx::KBLOCK);
+    p.quads = ceil_div(ceil_div(K, 32), 4);
     p.splits = 1;
-    while (p.splits < 8 && tiles * p.splits * 2 <= 2LL * dev->n_sms && p.kb_total >= 4 * p.splits) p.splits *= 2;
-    const int room = mx::STREAM_MAX_SMEM - 1024 - (int)sizeof(mx::StreamControl);
-    p.stages = std::max(2, std::min(std::min(8, room / sbytes), (p.kb_total + p.splits - 1) / p.splits));
-    p.control_at = std::max(p.stages * sbytes, p.splits > 1 ? p.T * mx::ROWS * 4 : 0);
-    const int smem = std::max(1024 + p.control_at + (int)sizeof(mx::StreamControl), mx::stream_min_smem(p.T));
-    if (tiles * p.splits > 0x7fffffffLL) return ops::fail(S2D2_ERR_UNSUPPORTED, "mxfp4_gemm: too many tiles");
-    CUtensorMap mw, mx_;
-    if (int rc = encode_codes(dev, &mw, wc, p.N, p.K, mx::ROWS)) return rc;
-    if (int rc = encode_codes(dev, &mx_, xc, p.M, p.K, p.T)) return rc;
-    const cudaError_t e = ops::launch(mx::stream_kernel, dim3((unsigned)(tiles * p.splits)), mx::THREADS, smem, p.splits, st, mw, mx_, p);
-    if (e != cudaSuccess) {
-        cudaGetLastError();
-        return ops::fail(S2D2_ERR_CUDA, "mxfp4_gemm: %s", cudaGetErrorString(e));
+    p.a_box = mx::ROWS;
+    if (M > 128) {
+        // Pairs of CTAs, if the tiles occupy at least half of them: T by the number of waves times a tile's length.
+        const int pairs = n_sms / 2, a_tiles = ceil_div(N, 256);
+        auto cost = [&](int T) { return (double)ceil_div((long long)a_tiles * ceil_div(M, T), pairs) * (T + 16); };
+        p.T = cost(128) <= cost(192) ? 128 : 192;
+        if (M <= 224 && cost((M + 31) / 32 * 32) <= cost(p.T)) p.T = (M + 31) / 32 * 32;      // one tile: any width
+        p.a_tiles = a_tiles;
+        p.b_tiles = ceil_div(M, p.T);
+        if ((long long)p.a_tiles * p.b_tiles * 2 >= pairs) {
+            plan.cg = 2;
+            p.sf_tiles = p.T > 128 ? 2 : 1;        // tiles start at multiples of 128, or of 64 with T = 192
+            const long long tiles = (long long)p.a_tiles * p.b_tiles;
+            const int clusters = (int)std::min<long long>(tiles, pairs);
+            plan.grid = clusters * 2;
+            finish_plan(plan, (tiles + clusters - 1) / clusters, mx::MAX_STAGES);
+            return;
+        }
     }
-    return S2D2_OK;
+    plan.cg = 1;
+    p.T = std::min(128, (M + 15) / 16 * 16);
+    p.a_tiles = ceil_div(N, mx::ROWS);
+    p.b_tiles = ceil_div(M, p.T);
+    p.sf_tiles = 1;                            // T = 128, or one tile
+    const long long tiles = (long long)p.a_tiles * p.b_tiles;
+    // Few tiles: split k while the CTAs fit side by side (two per SM) and each keeps at least two k-blocks.
+    while (p.splits < 8 && tiles * p.splits <= n_sms && p.kb_total >= 4 * p.splits) p.splits *= 2;
+    const int clusters = (int)std::min<long long>(tiles, p.splits > 1 ? tiles : n_sms);
+    plan.grid = clusters * p.splits;
+    const long long per_cluster = (tiles + clusters - 1) / clusters;
+    finish_plan(plan, per_cluster, (int)std::min<long long>(mx::MAX_STAGES, per_cluster * ceil_div(p.kb_total, p.splits)));
+}
+
+constexpr int SCORE_MAX_ITEMS = 320;       // (A tile, range) items, unless there are more A tiles
+
+int score_cg(int M) { return M > 128 ? 2 : 1; }
+int score_max_ranges(int a_tiles, int N) { return std::max(1, std::min(ceil_div(N, 64), SCORE_MAX_ITEMS / a_tiles)); }
+
+void plan_score(Plan& plan, int n_sms, int M, int N, int K) {
+    mx::Params& p = plan.p;
+    p.a_rows = M;
+    p.b_rows = N;
+    p.K = K;
+    p.kb_total = ceil_div(K, mx::KBLOCK);
+    p.quads = ceil_div(ceil_div(K, 32), 4);
+    p.splits = 1;
+    plan.cg = score_cg(M);
+    p.a_tiles = ceil_div(M, mx::ROWS * plan.cg);
+    p.a_box = std::min(mx::ROWS, (M + 7) / 8 * 8);
+    // Ranges of the head's rows per A tile, and the tile's T: least time of the busiest cluster, in B rows; 16 rows' time for
+    // the start of a tile, 64 for that of an item.
+    const int slots = n_sms / plan.cg;
+    double best = 1e30;
+    for (int T = 64; T <= 192; T += 64) {
+        const int unit = T == 128 ? 128 : 64, units = ceil_div(N, unit);
+        for (int r = 1; r <= std::min(units, score_max_ranges(p.a_tiles, N)); ++r) {
+            const int waves = ceil_div((long long)p.a_tiles * r, slots), len = ceil_div(units, r) * unit;
+            const double cost = waves * ((double)ceil_div(len, T) * (T + 16) + 64);
+            if (cost < best) best = cost, p.ranges = r, p.T = T, p.unit = unit;
+        }
+    }
+    p.sf_tiles = p.T > 128 ? 2 : 1;            // T = 64 and 192 start at multiples of 64, T = 128 at multiples of 128
+    p.b_tiles = 0;
+    const long long items = (long long)p.a_tiles * p.ranges;
+    const int clusters = (int)std::min<long long>(items, slots);
+    plan.grid = clusters * plan.cg;
+    finish_plan(plan, 2, mx::MAX_STAGES);
+}
+
+template <int CG, bool SCORE>
+int launch_product(const ops::Device* dev, const Plan& plan, const CUtensorMap* maps, cudaStream_t st) {
+    if (int rc = raise_limit<CG, SCORE>(dev)) return rc;
+    const cudaError_t e = ops::launch(mx::product_kernel<CG, SCORE>, dim3((unsigned)plan.grid), mx::THREADS, plan.smem, CG * plan.p.splits, st,
+                                      maps[0], maps[1], maps[2], maps[3], plan.p);
+    if (e == cudaSuccess) return S2D2_OK;
+    cudaGetLastError();
+    return ops::fail(S2D2_ERR_CUDA, "mxfp4 product: %s", cudaGetErrorString(e));
+}
+
+template <bool SCORE>
+int run_product(const ops::Device* dev, Plan& plan, const void* ac, const void* as, const void* bc, const void* bs, cudaStream_t st) {
+    CUtensorMap maps[4];
+    if (int rc = encode_codes(dev, &maps[0], ac, plan.p.a_rows, plan.p.K, plan.p.a_box)) return rc;
+    if (int rc = encode_codes(dev, &maps[1], bc, plan.p.b_rows, plan.p.K, plan.p.T / plan.cg)) return rc;
+    if (int rc = encode_scales(dev, &maps[2], as, plan.p.a_rows, plan.p.K)) return rc;
+    if (int rc = encode_scales(dev, &maps[3], bs, plan.p.b_rows, plan.p.K)) return rc;
+    return plan.cg == 1 ? launch_product<1, SCORE>(dev, plan, maps, st) : launch_product<2, SCORE>(dev, plan, maps, st);
 }
 
 }  // namespace
@@ -288,21 +391,60 @@ extern "C" int s2d2_mxfp4_gemm(const void* d_x_codes, const void* d_x_scales, co
     const ops::Device* dev;
     if (int rc = ops::device(&dev)) return rc;
     if (M == 0) return S2D2_OK;
-    if (int rc = check_product("mxfp4_gemm", dev, d_x_codes, d_x_scales, d_w_codes, d_w_scales, M, N, K)) return rc;
+    if (int rc = check_operands(dev, d_x_codes, d_x_scales, d_w_codes, d_w_scales)) return rc;
     if (int rc = ops::check_ptr(dev, d_y, y_dtype == S2D2_DTYPE_F32 ? 4 : 2, "y")) return rc;
-    if (int rc = raise_limits(dev)) return rc;
-    mx::GemmParams p = {};
-    p.y = d_y;
-    p.y_bf16 = y_dtype == S2D2_DTYPE_BF16;
-    p.M = M;
-    p.N = N;
-    p.K = K;
-    p.ldy = y_stride;
-    p.scale = scale;
-    p.kb_total = (K + mx::KBLOCK - 1) / mx::KBLOCK;
-    p.quads = ((K + 31) / 32 + 3) / 4;
-    p.w_scales = (const uint8_t*)d_w_scales;
-    p.x_scales = (const uint8_t*)d_x_scales;
-    p.status = dev->status;
-    return launch_stream(dev, p, d_x_codes, d_w_codes, (cudaStream_t)cuda_stream);
+    Plan plan;
+    plan_product(plan, dev->n_sms, M, N, K);
+    plan.p.y = d_y;
+    plan.p.y_bf16 = y_dtype == S2D2_DTYPE_BF16;
+    plan.p.ldy = y_stride;
+    plan.p.scale = scale;
+    plan.p.status = dev->status;
+    return run_product<false>(dev, plan, d_w_codes, d_w_scales, d_x_codes, d_x_scales, (cudaStream_t)cuda_stream);
+}
+
+extern "C" int s2d2_mxfp4_score_workspace(int32_t M, int32_t N, int32_t K, int64_t* bytes) {
+    ops::clear_error();
+    if (!bytes) return ops::fail(S2D2_ERR_INVALID, "mxfp4_score_workspace: null pointer");
+    if (int rc = check_product_shape("mxfp4_score_workspace", M, N, K)) return rc;
+    const int rows = mx::ROWS * score_cg(M), a_tiles = ceil_div(M, rows);
+    *bytes = M ? (int64_t)a_tiles * score_max_ranges(a_tiles, N) * rows * 16 : 0;
+    return S2D2_OK;
+}
+
+extern "C" int s2d2_mxfp4_score(const void* d_x_codes, const void* d_x_scales, const void* d_w_codes, const void* d_w_scales, int32_t M,
+                                int32_t N, int32_t K, float scale, const int32_t* d_tokens, float* d_logprob, float* d_lse,
+                                float* d_entropy, void* d_ws, int64_t ws_bytes, void* cuda_stream) {
+    ops::clear_error();
+    if (int rc = check_product_shape("mxfp4_score", M, N, K)) return rc;
+    if (!d_logprob && !d_lse && !d_entropy) return ops::fail(S2D2_ERR_INVALID, "mxfp4_score: no output");
+    if (d_logprob && !d_tokens) return ops::fail(S2D2_ERR_INVALID, "mxfp4_score: log probability needs tokens");
+    int64_t need = 0;
+    if (int rc = s2d2_mxfp4_score_workspace(M, N, K, &need)) return rc;
+    if (ws_bytes < need) return ops::fail(S2D2_ERR_INVALID, "mxfp4_score: the workspace needs %lld bytes", (long long)need);
+    const ops::Device* dev;
+    if (int rc = ops::device(&dev)) return rc;
+    if (M == 0) return S2D2_OK;
+    if (int rc = check_operands(dev, d_x_codes, d_x_scales, d_w_codes, d_w_scales)) return rc;
+    const void* words[] = {d_tokens, d_logprob, d_lse, d_entropy};
+    const char* names[] = {"tokens", "logprob", "lse", "entropy"};
+    for (int i = 0; i < 4; ++i)
+        if (words[i])
+            if (int rc = ops::check_ptr(dev, words[i], 4, names[i])) return rc;
+    if (int rc = ops::check_ptr(dev, d_ws, 16, "workspace")) return rc;
+    Plan plan;
+    plan_score(plan, dev->n_sms, M, N, K);
+    plan.p.scale = scale;
+    plan.p.status = dev->status;
+    plan.p.tokens = d_tokens;
+    plan.p.parts = (float4*)d_ws;
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (int rc = run_product<true>(dev, plan, d_x_codes, d_x_scales, d_w_codes, d_w_scales, st)) return rc;
+    const cudaError_t e = ops::launch(mx::score_parts_kernel, dim3((unsigned)ceil_div(M, 4)), 128, 0, 1, st, plan.p, mx::ROWS * plan.cg,
+                                      d_logprob, d_lse, d_entropy);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return ops::fail(S2D2_ERR_CUDA, "mxfp4_score: %s", cudaGetErrorString(e));
+    }
+    return S2D2_OK;
 }

@@ -3,14 +3,14 @@
 //   Y[m, n] = scale * sum_k X[m, k] W[n, k],   X and W in blocks of 32 elements with one power-of-two scale each
 //
 // The tensor core multiplies e2m1 codes, applies both scales and sums in fp32, so nothing is widened on the way: a
-// weight costs 17/32 byte of HBM instead of 2.  As in the bf16 kernels the weights are the MMA's "M" operand (128 rows)
-// and the tokens its "N" operand (16..128 rows): the accumulator's lanes are output features, so an epilogue warp
-// stores 32 consecutive elements of one output row, whatever that row's alignment.
+// weight costs 17/32 byte of HBM instead of 2.
 //
 // One k-block of a stage is 256 elements = 128 bytes of codes per row (one 128-byte swizzle row, four MMAs of 64) and
 // 8 scales per row = two 512-byte scale tiles.  Scales go from shared memory to tensor memory by tcgen05.cp (32 lanes x 16
 // bytes, repeated for the four lane quarters): column c + r / 32 of lane r % 32 then holds the four scales of row r of that
-// tile, and an MMA of 64 elements takes the lower or the upper two of them (scale id 0 or 2).
+// tile, and an MMA of 64 elements takes the lower or the upper two of them (scale id 0 or 2).  A tile of B that starts in
+// the middle of a scale tile reads its scales from column 2 on.  The column must be even (an odd one is a misaligned address),
+// so tiles start at multiples of 64 rows.
 #pragma once
 #include "ops_host.h"
 #include "tc_ptx.cuh"
@@ -25,30 +25,58 @@ constexpr int KBLOCK = 256;          // elements of a stage's k-block
 constexpr int KBYTES = KBLOCK / 2;
 constexpr int MMA_K = 64;
 constexpr int SF_TILE = 512;         // bytes of one scale tile: 128 rows x 4 blocks
-constexpr int THREADS = 128;
+constexpr int THREADS = 192;        // producer warp, MMA warp, four epilogue warps
+constexpr int MAX_STAGES = 12;
 
-struct GemmParams {
-    void* y;
-    int y_bf16;
-    int M, N, K;
-    long long ldy;
-    float scale;
-    int T;                           // token rows per tile (multiple of 16; of 32 if there are several tiles)
-    int x_tiles;                     // scale tiles that the token rows of a tile touch (1 or 2)
+// D = A B^T; which matrix is A and which is B depends on the operator (see product_kernel).
+struct Params {
+    int a_rows, b_rows, K;           // rows of the two matrices, elements along k
+    int T;                           // B rows of a tile (multiple of 16 CG; 64, 128 or 192 if there are several tiles)
+    int a_box;                       // A rows that a CTA loads per tile: 128, or fewer (a multiple of 8) where A has fewer
+    int sf_tiles;                    // scale tiles that the B rows of a tile touch (1 or 2)
     int stages;
-    int splits;                      // k splits = CTAs per cluster
+    int n_acc;                       // accumulator buffers (2: the epilogue of a tile overlaps the next tile's MMAs)
     int kb_total;                    // k-blocks
     int quads;                       // scale tiles along k
-    int m_tiles;
-    int control_at;                  // byte offset of the barriers behind the ring
-    const uint8_t* w_scales;
-    const uint8_t* x_scales;
+    int splits;                      // CTAs of a cluster that share a tile's k-blocks (1 with CTA pairs)
+    int a_tiles, b_tiles;
+    uint32_t tmem_cols;
+    int control_at;                  // byte offset of Control behind the ring
+    float scale;
     int* status;
+    // product
+    void* y;                         // [b_rows, a_rows], rows ldy elements apart
+    long long ldy;
+    int y_bf16;
+    // scores
+    const int* tokens;
+    float4* parts;                   // [a_tile][range][A rows of a tile]: maximum, sum, moment (base 2), logit of the token
+    int ranges;                      // ranges of B per A tile, in units of `unit` rows
+    int unit;
 };
 
-__host__ __device__ __forceinline__ int stage_bytes(int T, int x_tiles) {
-    return ROWS * KBYTES + T * KBYTES + (1 + x_tiles) * 2 * SF_TILE;
+struct Control {
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full[2], acc_empty[2];
+    uint32_t tmem_slot;
+    int abort_flag;
+};
+
+// Bytes of a CTA's stage: its A rows, its share of the B rows, scales of both.
+__host__ __device__ __forceinline__ int stage_bytes(int cg, int a_box, int T, int sf_tiles) {
+    return a_box * KBYTES + T / cg * KBYTES + (1 + sf_tiles) * 2 * SF_TILE;
 }
+// An MMA reads 128 rows of A.  Where fewer are loaded, the others are whatever follows in the ring (any bits are e2m1 codes); they
+// end up in lanes that nobody reads.  Behind the last stage as many bytes are kept free.
+__host__ __device__ __forceinline__ int ring_bytes(int cg, int stages, int a_box, int T, int sf_tiles) {
+    return stages * stage_bytes(cg, a_box, T, sf_tiles) + (ROWS - a_box) * KBYTES;
+}
+__host__ __device__ __forceinline__ int scale_columns(int sf_tiles) { return 8 + 8 * sf_tiles; }      // of one of two buffers
+__host__ __device__ __forceinline__ int used_columns(int T, int sf_tiles, int n_acc) { return 2 * scale_columns(sf_tiles) + n_acc * T; }
+// Tensor memory is taken with an instruction that waits until enough columns are free.  A CTA of a cluster that waited there for
+// a CTA of another cluster, which waits for its own cluster, could wait for good.  So shared memory is asked for in
+// proportion (57 KB of an SM's 228 KB, 1 KB of it reserved per CTA, for every 128 of its 512 columns): CTAs that fit
+// on an SM by their shared memory also fit by their columns, and nobody ever waits.
+__host__ __device__ __forceinline__ int min_smem(uint32_t cols) { return cols <= 64 ? 28 * 1024 : cols <= 128 ? 56 * 1024 : cols <= 256 ? 113 * 1024 : 227 * 1024; }
 
 __device__ __forceinline__ uint64_t desc_sw128(uint32_t smem_addr) {      // K-major rows of 128 bytes, 128-byte swizzle
     return (uint64_t)((smem_addr & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
@@ -62,193 +90,427 @@ __host__ __device__ __forceinline__ uint32_t instr_desc(int rows, int T) {
 }
 __device__ __forceinline__ uint32_t scale_ids(int id) { return ((uint32_t)id << 4) | ((uint32_t)id << 29); }
 
+// The instructions come in a form for one CTA and one for a pair of CTAs (an even and an odd one of a cluster) that share
+// an MMA of 256 rows: each holds 128 rows of A, half of the rows of B, all scales of B, and 128 lanes of the accumulator.
+template <int CG>
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                          uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
-        : "memory");
+    if (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+            : "memory");
 }
+template <int CG>
 __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    if (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
-                 "l"(src), "r"(bytes), "r"(smem_u32(bar))
-                 : "memory");
+// Arrives on the barrier (of both CTAs of a pair) when the MMAs issued so far are done.
+template <int CG>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+    if (CG == 1) umma_commit(bar);
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                         smem_u32(bar)),
+                     "h"((uint16_t)3)
+                     : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void alloc(uint32_t* slot, uint32_t cols) {
+    if (CG == 1) {
+        tmem_alloc(slot, cols);
+        tmem_relinquish();
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void dealloc(uint32_t addr, uint32_t cols) {
+    if (CG == 1) tmem_dealloc(addr, cols);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+}
+// TMA tile load into this CTA that reports to a barrier of this CTA, or (pair) of the pair's first CTA
+template <int CG>
+__device__ __forceinline__ void load_2d(void* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                smem_u32(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                smem_u32(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+}
+__device__ __forceinline__ void arrive_remote(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void store_y(void* y, int y_bf16, size_t at, float v) {
     if (y_bf16) reinterpret_cast<bf16*>(y)[at] = __float2bfloat16_rn(v);
     else reinterpret_cast<float*>(y)[at] = v;
 }
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
-// ---------------------------------------------------------------------------------------------------------------------
-// The weight stream: up to 128 token rows per tile, one output tile per CTA, or per cluster whose CTAs share its k-blocks.
-//   warp 0 / lane 0  producer: codes by TMA, scale tiles by bulk copies, into a ring of stages
-//   warp 1 / lane 0  scales to tensor memory (two buffers), four MMAs per stage
-//   warps 0..3       epilogue
-// Two CTAs fit on an SM, so the set-up and the epilogue of one overlap the stream of the other.  With a cluster the partial
-// tiles meet in distributed shared memory: every CTA sums its share of the token rows over the cluster in rank order
-// (deterministic, no workspace, no tickets: nothing that two launches could share).
-// ---------------------------------------------------------------------------------------------------------------------
-struct StreamControl {
-    uint64_t full[8], empty[8], acc_ready;
-    uint32_t tmem_slot;
-    int abort_flag, issued, consumed;
+// The tiles that a cluster works on, in order.
+//   product: tile number = cluster + i * clusters; B tiles vary fastest, so that the clusters at work share the A tiles
+//   scores:  a cluster takes (A tile, range) items; inside an item the B tiles of its range
+struct Tiles {
+    int item, b, b_end;              // scores: first B row of the next tile, end of the range
+    int a0, b0, rows;                // current tile: A tile number, first B row, B rows
+    int first, last;                 // scores: first / last tile of an item
 };
-// Tensor memory is taken with an instruction that waits until enough columns are free.  A CTA of a cluster that waited there for
-// a CTA of another cluster, which waits for its own cluster, could wait for good.  So shared memory is asked for in
-// proportion (57 KB of an SM's 228 KB, 1 KB of it reserved per CTA, for every 128 of its 512 columns): the CTAs
-// that fit on an SM by their shared memory also fit by their columns, and nobody ever waits.
-__host__ __device__ __forceinline__ uint32_t stream_columns(int T) { return T <= 64 ? 128 : 256; }
-__host__ __device__ __forceinline__ int stream_min_smem(int T) { return (T <= 64 ? 56 : 113) * 1024; }
-constexpr int STREAM_MAX_SMEM = 113 * 1024;      // two CTAs per SM
+template <bool SCORE>
+__device__ __forceinline__ Tiles first_tile(int cluster) {
+    Tiles t;
+    t.item = cluster;
+    t.b = t.b_end = 0;
+    t.last = 1;
+    return t;
+}
+template <bool SCORE>
+__device__ __forceinline__ bool next_tile(const Params& p, Tiles& t, int clusters) {
+    if (!SCORE) {
+        if (t.item >= p.a_tiles * p.b_tiles) return false;
+        t.a0 = t.item / p.b_tiles;
+        t.b0 = (t.item % p.b_tiles) * p.T;
+        t.rows = p.T;
+        t.item += clusters;
+        return true;
+    }
+    t.first = t.last;
+    if (t.first) {
+        if (t.item >= p.a_tiles * p.ranges) return false;
+        t.a0 = t.item % p.a_tiles;                 // clusters next to each other read the same range of B
+        const int range = t.item / p.a_tiles;
+        const long long units = (p.b_rows + p.unit - 1) / p.unit;
+        t.b = (int)(units * range / p.ranges) * p.unit;
+        t.b_end = (int)(units * (range + 1) / p.ranges) * p.unit;
+        t.item += clusters;
+    }
+    t.b0 = t.b;
+    t.rows = min(p.T, t.b_end - t.b);
+    t.b += t.rows;
+    t.last = t.b >= t.b_end;
+    return true;
+}
 
-static __global__ void __launch_bounds__(THREADS)
-stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const GemmParams p) {
+// One kernel for both operators and for one CTA or a pair of CTAs per tile.
+//   product (SCORE = false): A = weights, B = tokens.  The accumulator's lanes are output features, so an epilogue warp stores 32
+//     consecutive elements of an output row, whatever that row's alignment.
+//   scores (SCORE = true): A = tokens, B = head.  A lane is one token's row of logits: each thread folds the logits of
+//     its token into a running maximum, sum and moment; nothing is exchanged between threads and no logit leaves the SM.
+//   warp 0     producer: codes and scale tiles by TMA into a ring of stages that runs on from tile to tile
+//   warp 1     scales to tensor memory (two buffers), four MMAs of 64 elements per stage; tensor memory
+//   warps 2-5  epilogue of the previous tile (two accumulators where a CTA has several tiles)
+// With few tiles the CTAs of a cluster (p.splits) share the k-blocks of one tile; the partial tiles meet in distributed
+// shared memory, where every CTA sums its share of the rows over the cluster in rank order: deterministic, no
+// workspace, no tickets, nothing that two launches could share.
+// Every wait on a barrier is bounded; after a time-out the outputs are NaN and the status word is raised.
+template <int CG, bool SCORE>
+__global__ void __launch_bounds__(THREADS, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb, const Params p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    StreamControl& ctl = *(StreamControl*)(ring + p.control_at);
-    uint64_t *full = ctl.full, *empty = ctl.empty, &acc_ready = ctl.acc_ready;
-    uint32_t& tmem_slot = ctl.tmem_slot;
-    volatile int &abort_flag = ctl.abort_flag, &issued = ctl.issued, &consumed = ctl.consumed;
+    Control& ctl = *(Control*)(ring + p.control_at);
+    volatile int* abort_flag = &ctl.abort_flag;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int S = p.stages, T = p.T, sbytes = stage_bytes(T, p.x_tiles);
-    const int split = p.splits > 1 ? (int)cluster_rank() : 0;
-    const int tile = blockIdx.x / (unsigned)p.splits;
-    const int m0 = (tile % p.m_tiles) * T, n_tile = tile / p.m_tiles;
+    const int S = p.stages, sbytes = stage_bytes(CG, p.a_box, p.T, p.sf_tiles);
+    const int cluster_size = CG * p.splits;
+    const uint32_t rank = cluster_size > 1 ? cluster_rank() : 0;
+    const int cluster = blockIdx.x / (unsigned)cluster_size, clusters = gridDim.x / (unsigned)cluster_size;
+    const int split = CG == 1 ? (int)rank : 0;
     const int kb0 = (int)((long long)p.kb_total * split / p.splits), kb1 = (int)((long long)p.kb_total * (split + 1) / p.splits);
-    constexpr uint32_t D_COL = 64;                                  // columns 0..47: two scale buffers of up to 24
-    const uint32_t tmem_cols = stream_columns(T);
+    const uint32_t d_col = 2 * scale_columns(p.sf_tiles);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(&full[s], 1);
-            mbar_init(&empty[s], 1);
+            mbar_init(&ctl.full[s], 1);
+            mbar_init(&ctl.empty[s], 1);
         }
-        mbar_init(&acc_ready, 1);
-        abort_flag = 0;
-        issued = 0;
-        consumed = 0;
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&ctl.acc_full[b], 1);
+            mbar_init(&ctl.acc_empty[b], 4 * CG);
+        }
+        ctl.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_sfa) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_sfb) : "memory");
     }
-    if (warp == 0) {
-        tmem_alloc(&tmem_slot, tmem_cols);
-        tmem_relinquish();
-    }
+    if (warp == 1) alloc<CG>(&ctl.tmem_slot, p.tmem_cols);
     tc_fence_before();
-    __syncthreads();
+    if (cluster_size > 1) {
+        cluster_arrive();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = ctl.tmem_slot;
     pdl_launch();
 
-    if (warp == 0 && lane == 0) {
-        pdl_wait();
-        const int x_group = m0 / ROWS, x_groups = (p.M + ROWS - 1) / ROWS;
-        for (int kb = kb0; kb < kb1; ++kb) {
-            const int i = kb - kb0, s = i % S;
-            if (i >= S && !mbar_wait(&empty[s], ((i / S) - 1) & 1, &abort_flag)) {
-                abort_flag = 1;
-                break;
+    Tiles t = first_tile<SCORE>(cluster);
+    if (warp == 0) {
+        if (lane == 0) {
+            pdl_wait();
+            const int b_half = p.T / CG;
+            const uint32_t bytes = (uint32_t)CG * ((p.a_box + b_half) * KBYTES + (1 + p.sf_tiles) * 2 * SF_TILE);
+            int it = 0;
+            while (!*abort_flag && next_tile<SCORE>(p, t, clusters)) {
+                const int a_row = (t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS;
+                const int b_row = t.b0 + (CG == 2 ? (int)rank * b_half : 0);
+                const int sfb_group = t.b0 / ROWS;
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int s = it % S;
+                    if (it >= S && !mbar_wait(&ctl.empty[s], ((it / S) - 1) & 1, abort_flag)) {
+                        *abort_flag = 1;
+                        break;
+                    }
+                    uint8_t* a = ring + (size_t)s * sbytes;
+                    uint8_t* b = a + p.a_box * KBYTES;
+                    uint8_t* sf = b + b_half * KBYTES;
+                    uint32_t bar = smem_u32(&ctl.full[s]);
+                    if (CG == 2) bar = cluster_map(bar, 0);
+                    if (CG == 1 || rank == 0) mbar_expect_tx(&ctl.full[s], bytes);
+                    load_2d<CG>(a, &map_a, kb * KBYTES, a_row, bar);
+                    load_2d<CG>(b, &map_b, kb * KBYTES, b_row, bar);
+                    load_2d<CG>(sf, &map_sfa, 0, (a_row / ROWS) * p.quads + 2 * kb, bar);
+                    for (int g = 0; g < p.sf_tiles; ++g)
+                        load_2d<CG>(sf + (1 + g) * 2 * SF_TILE, &map_sfb, 0, (sfb_group + g) * p.quads + 2 * kb, bar);
+                }
             }
-            if (abort_flag) break;
-            uint8_t* w = ring + (size_t)s * sbytes;
-            uint8_t* x = w + ROWS * KBYTES;
-            uint8_t* sf = x + T * KBYTES;
-            const uint32_t sf_bytes = (uint32_t)min(2, p.quads - 2 * kb) * SF_TILE;
-            const int xt = min(p.x_tiles, x_groups - x_group);
-            mbar_expect_tx(&full[s], (uint32_t)(ROWS + T) * KBYTES + (1 + xt) * sf_bytes);
-            tma_load_2d(w, &map_w, kb * KBYTES, n_tile * ROWS, &full[s]);
-            tma_load_2d(x, &map_x, kb * KBYTES, m0, &full[s]);
-            bulk_load(sf, p.w_scales + ((size_t)n_tile * p.quads + 2 * kb) * SF_TILE, sf_bytes, &full[s]);
-            for (int a = 0; a < xt; ++a)
-                bulk_load(sf + (1 + a) * 2 * SF_TILE, p.x_scales + ((size_t)(x_group + a) * p.quads + 2 * kb) * SF_TILE, sf_bytes,
-                          &full[s]);
-            issued = i + 1;
         }
-    } else if (warp == 1 && lane == 0) {
-        const uint32_t idesc = instr_desc(ROWS, T);
-        const int sf_cols = 8 + 8 * p.x_tiles;                      // per buffer: weights 2 x 4, tokens 2 x x_tiles x 4
-        const uint32_t x_col = (uint32_t)(m0 % ROWS) / 32;
-        for (int kb = kb0; kb < kb1; ++kb) {
-            const int i = kb - kb0, s = i % S;
-            if (!mbar_wait(&full[s], (i / S) & 1, &abort_flag)) {
-                abort_flag = 1;
-                break;
-            }
-            tc_fence_after();
-            const uint32_t w_addr = smem_u32(ring + (size_t)s * sbytes), x_addr = w_addr + ROWS * KBYTES, sf_addr = x_addr + T * KBYTES;
-            const uint32_t sfw = tmem + (i & 1) * sf_cols, sfx = sfw + 8;
-            const int steps = min(KBLOCK / MMA_K, (p.K - kb * KBLOCK + MMA_K - 1) / MMA_K), quads = (steps + 1) / 2;
-            for (int g = 0; g < quads; ++g) {
-                scales_to_tmem(sfw + g * 4, desc_scales(sf_addr + g * SF_TILE));
-                for (int a = 0; a < p.x_tiles; ++a)
-                    scales_to_tmem(sfx + (g * p.x_tiles + a) * 4, desc_scales(sf_addr + ((1 + a) * 2 + g) * SF_TILE));
-            }
-            const uint64_t wd = desc_sw128(w_addr), xd = desc_sw128(x_addr);
-            for (int k = 0; k < steps; ++k)                         // 64 elements are 32 bytes: +2 in the descriptors' address fields
-                mma_mxf4(tmem + D_COL, wd + 2 * k, xd + 2 * k, idesc | scale_ids((k & 1) * 2), sfw + (k >> 1) * 4,
-                         sfx + (k >> 1) * 4 * p.x_tiles + x_col, (i > 0 || k > 0) ? 1u : 0u);
-            umma_commit(&empty[s]);
-            consumed = i + 1;
-        }
-        umma_commit(&acc_ready);
-    }
-    __syncwarp();
-    if (!mbar_wait(&acc_ready, 0)) abort_flag = 1;
-    tc_fence_after();
-    __syncthreads();
-    const bool aborted = abort_flag != 0;
-    if (aborted && threadIdx.x == 0) {
-        atomicExch(p.status, 1);
-        for (int i = consumed; i < issued; ++i) mbar_wait(&full[i % S], (i / S) & 1);      // copies in flight land first
-    }
-    const float nan = __int_as_float(0x7fffffff);
-    const uint32_t taddr = tmem + D_COL + ((uint32_t)(warp * 32) << 16);
-    const int n_local = warp * 32 + lane, n = n_tile * ROWS + n_local, rows = min(T, p.M - m0);
-    if (p.splits == 1) {
-        for (int c = 0; c < rows; c += 16) {
-            float v[16];
-            tmem_ld16(taddr + c, v);
-            if (n < p.N) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (c + j < rows) store_y(p.y, p.y_bf16, (size_t)(m0 + c + j) * p.ldy + n, aborted ? nan : p.scale * v[j]);
+    } else if (warp == 1) {
+        if (lane == 0 && (CG == 1 || rank == 0)) {
+            int it = 0, n = 0;
+            while (!*abort_flag && next_tile<SCORE>(p, t, clusters)) {
+                const int acc = n % p.n_acc;
+                if (n >= p.n_acc && !mbar_wait(&ctl.acc_empty[acc], ((n / p.n_acc) - 1) & 1, abort_flag)) {
+                    *abort_flag = 1;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t idesc = instr_desc(ROWS * CG, p.T);      // of a tile cut short at the end of a range, the last columns go unread
+                const uint32_t d = tmem + d_col + acc * p.T;
+                const uint32_t b_col = (uint32_t)(t.b0 % ROWS) / 32;
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int s = it % S;
+                    if (!mbar_wait(&ctl.full[s], (it / S) & 1, abort_flag)) {
+                        *abort_flag = 1;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t a_addr = smem_u32(ring + (size_t)s * sbytes), b_addr = a_addr + p.a_box * KBYTES,
+                                   sf_addr = b_addr + p.T / CG * KBYTES;
+                    const uint32_t sfa = tmem + (it & 1) * scale_columns(p.sf_tiles), sfb = sfa + 8;
+                    const int steps = min(KBLOCK / MMA_K, (p.K - kb * KBLOCK + MMA_K - 1) / MMA_K), quads = (steps + 1) / 2;
+                    for (int q = 0; q < quads; ++q) {
+                        scales_to_tmem<CG>(sfa + q * 4, desc_scales(sf_addr + q * SF_TILE));
+                        for (int g = 0; g < p.sf_tiles; ++g)
+                            scales_to_tmem<CG>(sfb + (q * p.sf_tiles + g) * 4, desc_scales(sf_addr + ((1 + g) * 2 + q) * SF_TILE));
+                    }
+                    const uint64_t ad = desc_sw128(a_addr), bd = desc_sw128(b_addr);
+                    for (int k = 0; k < steps; ++k)          // 64 elements are 32 bytes: +2 in the descriptors' address fields
+                        mma_mxf4<CG>(d, ad + 2 * k, bd + 2 * k, idesc | scale_ids((k & 1) * 2), sfa + (k >> 1) * 4,
+                                     sfb + (k >> 1) * 4 * p.sf_tiles + b_col, (kb > kb0 || k > 0) ? 1u : 0u);
+                    commit<CG>(&ctl.empty[s]);
+                }
+                commit<CG>(&ctl.acc_full[acc]);
+                ++n;
             }
         }
     } else {
-        float* part = reinterpret_cast<float*>(ring);               // [T][128]; the ring is idle
-        __syncthreads();                                            // ... once thread 0 has seen the last copies land
-        for (int c = 0; c < rows; c += 16) {
-            float v[16];
-            tmem_ld16(taddr + c, v);
+        const int quarter = warp & 3;                        // the lanes of tensor memory that this warp may read
+        const int row = quarter * 32 + lane;
+        const float nan = __int_as_float(0x7fffffff);
+        int n = 0;
+        // scores
+        float m = 0.f, s = 0.f, mo = 0.f, x_t = 0.f;
+        int token = -1;
+        const float c2 = p.scale * 1.4426950408889634f;
+        if (SCORE) pdl_wait();
+        while (next_tile<SCORE>(p, t, clusters)) {
+            const int acc = n % p.n_acc;
+            bool ok = !*abort_flag && mbar_wait(&ctl.acc_full[acc], (n / p.n_acc) & 1, abort_flag);
+            if (!ok) *abort_flag = 1;
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            const uint32_t taddr = tmem + d_col + acc * p.T + ((uint32_t)(quarter * 32) << 16);
+            const int a = (t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS + row;
+            if (!SCORE) {
+                const int rows = min(t.rows, p.b_rows - t.b0);
+                if (p.splits == 1) {
+                    for (int c = 0; c < rows; c += 16) {
+                        float v[16];
+                        tmem_ld16(taddr + c, v);
+                        if (a < p.a_rows) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (c + j < rows) part[(c + j) * ROWS + n_local] = aborted ? nan : v[j];
+                            for (int j = 0; j < 16; ++j)
+                                if (c + j < rows) store_y(p.y, p.y_bf16, (size_t)(t.b0 + c + j) * p.ldy + a, ok ? p.scale * v[j] : nan);
+                        }
+                    }
+                } else {
+                    // the ring is idle: a cluster that shares a tile has no other, and all its loads have been multiplied
+                    float* part = reinterpret_cast<float*>(ring);
+                    for (int c = 0; c < rows; c += 16) {
+                        float v[16];
+                        tmem_ld16(taddr + c, v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (c + j < rows) part[(c + j) * ROWS + row] = ok ? v[j] : nan;
+                    }
+                }
+            } else {
+                if (t.first) {
+                    m = -3.402823466e38f;
+                    s = mo = x_t = 0.f;
+                    token = p.tokens && a < p.a_rows ? p.tokens[a] : -1;
+                }
+                if ((t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS + quarter * 32 < p.a_rows) {
+                    for (int c = 0; c < t.rows; c += 32) {
+                        const int left = p.b_rows - (t.b0 + c);
+                        if (left <= 0) break;
+                        float v[32];
+                        tmem_ld32(taddr + c, v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= c2;
+                        if (left < 32) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j >= left) v[j] = -3.402823466e38f;
+                        }
+                        float top = v[0];
+#pragma unroll
+                        for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
+                        const float m1 = fmaxf(m, top), dm = fmaxf(m - m1, -300.f), f = exp2_fast(dm);
+                        mo = f * (mo + dm * s);
+                        s *= f;
+                        m = m1;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float u = v[j] - m, e = exp2_fast(u);
+                            s += e;
+                            mo += u * e;
+                        }
+                        const int at = token - (t.b0 + c);
+                        if (at >= 0 && at < 32) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j == at) x_t = v[j];
+                        }
+                    }
+                }
+                if (t.last && a < p.a_rows) {
+                    const int range = (t.item - clusters) / p.a_tiles;
+                    p.parts[((size_t)t.a0 * p.ranges + range) * (ROWS * CG) + (CG == 2 ? rank * ROWS : 0) + row] =
+                        ok && !*abort_flag ? make_float4(m, s, mo, x_t) : make_float4(nan, nan, nan, nan);
+                }
+            }
+            // the accumulator may be overwritten (by the pair's first CTA, which issues the MMAs)
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&ctl.acc_empty[acc])) : "memory");
+                else arrive_remote(cluster_map(smem_u32(&ctl.acc_empty[acc]), 0));
+            }
+            ++n;
         }
+    }
+    __syncwarp();
+    if (CG == 1 && p.splits > 1) {
+        // sum of the partial tiles over the cluster
         cluster_arrive();
         cluster_wait();
-        const uint32_t mine = smem_u32(part) + 4 * n_local;
-        for (int t = split; t < rows; t += p.splits) {
-            float sum = 0.f;
-            for (int q = 0; q < p.splits; ++q) {
-                float v;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_map(mine + t * ROWS * 4, q)) : "memory");
-                sum += v;
+        if (warp >= 2) {
+            Tiles u = first_tile<SCORE>(cluster);
+            next_tile<SCORE>(p, u, clusters);
+            const int rows = min(u.rows, p.b_rows - u.b0), row = (warp & 3) * 32 + lane, a = u.a0 * ROWS + row;
+            const uint32_t mine = smem_u32(ring) + 4 * row;
+            for (int b = split; b < rows; b += p.splits) {
+                float sum = 0.f;
+                for (int q = 0; q < p.splits; ++q) {
+                    float v;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_map(mine + b * ROWS * 4, q)) : "memory");
+                    sum += v;
+                }
+                if (a < p.a_rows) store_y(p.y, p.y_bf16, (size_t)(u.b0 + b) * p.ldy + a, p.scale * sum);
             }
-            if (n < p.N) store_y(p.y, p.y_bf16, (size_t)(m0 + t) * p.ldy + n, p.scale * sum);
         }
-        cluster_arrive();                                           // nobody leaves while others read its partial tile
-        cluster_wait();
+    }
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) atomicExch(p.status, 1);
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);       // copies in flight land before shared memory is given back
     }
     tc_fence_before();
-    __syncthreads();
-    if (warp == 0) tmem_dealloc(tmem, tmem_cols);
+    if (cluster_size > 1) {
+        // nobody leaves while others read its shared memory, signal its barriers or multiply into its tensor memory
+        cluster_arrive();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
+    if (warp == 1) dealloc<CG>(tmem, p.tmem_cols);
+}
+
+// Scores from the partial results of a row's ranges: one warp per row, ranges in a fixed order.
+static __global__ void __launch_bounds__(128)
+score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse, float* entropy) {
+    pdl_wait();
+    pdl_launch();
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (r >= p.a_rows) return;
+    const float4* parts = p.parts + (size_t)(r / rows_per_tile) * p.ranges * rows_per_tile + r % rows_per_tile;
+    const int token = p.tokens ? p.tokens[r] : -1;
+    const bool has_token = token >= 0 && token < p.b_rows;
+    const long long units = (p.b_rows + p.unit - 1) / p.unit;
+    float m = -3.402823466e38f, s = 0.f, mo = 0.f, x_t = 0.f;
+    auto add = [&](float m2, float s2, float mo2) {
+        const float M = fmaxf(m, m2), d1 = fmaxf(m - M, -300.f), d2 = fmaxf(m2 - M, -300.f);
+        const float f1 = exp2_fast(d1), f2 = exp2_fast(d2);
+        mo = f1 * (mo + d1 * s) + f2 * (mo2 + d2 * s2);
+        s = f1 * s + f2 * s2;
+        m = M;
+    };
+    for (int i = lane; i < p.ranges; i += 32) {
+        const float4 v = parts[(size_t)i * rows_per_tile];
+        add(v.x, v.y, v.z);
+        if (has_token && token / p.unit >= units * i / p.ranges && token / p.unit < units * (i + 1) / p.ranges) x_t = v.w;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o),
+                    mo2 = __shfl_xor_sync(0xffffffffu, mo, o);
+        x_t += __shfl_xor_sync(0xffffffffu, x_t, o);          // one lane has it, the others zero
+        add(m2, s2, mo2);
+    }
+    if (lane) return;
+    const float ln2 = 0.6931471805599453f, log_s = log2f(s), nan = __int_as_float(0x7fffffff);
+    const bool undefined = !(s > 0.f) || isinf(m);
+    if (lse) lse[r] = undefined ? nan : (m + log_s) * ln2;
+    if (entropy) entropy[r] = undefined ? nan : (log_s - mo / s) * ln2;
+    if (logprob) logprob[r] = undefined || !has_token ? nan : ((x_t - m) - log_s) * ln2;
 }
 
 }  // namespace mx

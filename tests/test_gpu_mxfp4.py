@@ -94,7 +94,10 @@ def product_tolerance(xv, wv, scale, y_type):
 
 SHAPES = [(1, 1, 1), (1, 128, 32), (2, 8, 33), (16, 127, 64), (17, 129, 65), (5, 256, 256), (3, 130, 257), (33, 1000, 512),
           (64, 384, 4096), (1, 4096, 4096), (65, 200, 300), (77, 1001, 2050), (128, 256, 1024), (129, 300, 700), (200, 128, 96),
-          (256, 512, 512), (300, 640, 1000), (513, 257, 288)]
+          (256, 512, 512), (300, 640, 1000), (513, 257, 288),
+          # enough tiles for pairs of CTAs: one or several tiles per pair, every tile width and start inside a scale tile
+          (150, 9500, 96), (300, 6001, 320), (1000, 2500, 257), (1025, 2999, 64), (210, 19000, 600), (450, 10000, 1024),
+          (1400, 1537, 1000)]
 
 
 @pytest.mark.parametrize("y_type", ["fp32", "bf16"])

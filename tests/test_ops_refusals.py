@@ -68,6 +68,16 @@ def test_score_refusals(s2d2):
     refused(s2d2, -1, "no output", f, P, "fp32", 1, 8, 8, P)
 
 
+def test_hidden_score_refusals(s2d2):
+    f, need = s2d2.mxfp4_score, s2d2.mxfp4_score_workspace(4, 1000, 64)
+    assert need > 0 and need % 16 == 0 and s2d2.mxfp4_score_workspace(0, 1000, 64) == 0
+    refused(s2d2, -1, "N must", s2d2.mxfp4_score_workspace, 1, 0, 32)
+    refused(s2d2, -1, "M must", f, P, P, P, P, -1, 1000, 64, P, P, need, d_lse=P)
+    refused(s2d2, -1, "no output", f, P, P, P, P, 4, 1000, 64, P, P, need)
+    refused(s2d2, -1, "tokens", f, P, P, P, P, 4, 1000, 64, 0, P, need, d_logprob=P)
+    refused(s2d2, -1, "workspace", f, P, P, P, P, 4, 1000, 64, P, P, need - 1, d_lse=P)
+
+
 def test_no_gpu_fails_loudly(s2d2):
     import torch
     if torch.cuda.is_available():
