@@ -25,7 +25,7 @@ constexpr int KBLOCK = 256;          // elements of a stage's k-block
 constexpr int KBYTES = KBLOCK / 2;
 constexpr int MMA_K = 64;
 constexpr int SF_TILE = 512;         // bytes of one scale tile: 128 rows x 4 blocks
-constexpr int THREADS = 192;        // producer warp, MMA warp, four epilogue warps
+constexpr int THREADS = 224;        // warps: codes, MMA, four of the epilogue, scales
 constexpr int MAX_STAGES = 12;
 
 // D = A B^T; which matrix is A and which is B depends on the operator (see product_kernel).
@@ -142,17 +142,17 @@ __device__ __forceinline__ void dealloc(uint32_t addr, uint32_t cols) {
 }
 // TMA tile load into this CTA that reports to a barrier of this CTA, or (pair) of the pair's first CTA
 template <int CG>
-__device__ __forceinline__ void load_2d(void* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+__device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     if (CG == 1)
         asm volatile(
             "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-                smem_u32(dst)),
+                dst),
             "l"(map), "r"(x), "r"(y), "r"(bar)
             : "memory");
     else
         asm volatile(
             "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-                smem_u32(dst)),
+                dst),
             "l"(map), "r"(x), "r"(y), "r"(bar)
             : "memory");
 }
@@ -168,6 +168,22 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+// One lane of a converged warp.  The warps that feed the tensor core and the copy engine run their loops with all lanes, so
+// that addresses and descriptors stay in uniform registers; only the instruction itself is left to one lane.
+__device__ __forceinline__ bool elect() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
+}
+// Position in the ring: stage and the parity of its current use.
+struct Ring {
+    int s = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++s == stages) s = 0, parity ^= 1;
+    }
+};
 
 // The tiles that a cluster works on, in order.
 //   product: tile number = cluster + i * clusters; B tiles vary fastest, so that the clusters at work share the A tiles
@@ -217,7 +233,8 @@ __device__ __forceinline__ bool next_tile(const Params& p, Tiles& t, int cluster
 //     consecutive elements of an output row, whatever that row's alignment.
 //   scores (SCORE = true): A = tokens, B = head.  A lane is one token's row of logits: each thread folds the logits of
 //     its token into a running maximum, sum and moment; nothing is exchanged between threads and no logit leaves the SM.
-//   warp 0     producer: codes and scale tiles by TMA into a ring of stages that runs on from tile to tile
+//   warp 0     producer of the codes: TMA into a ring of stages that runs on from tile to tile
+//   warp 6     producer of the scale tiles of the same stages
 //   warp 1     scales to tensor memory (two buffers), four MMAs of 64 elements per stage; tensor memory
 //   warps 2-5  epilogue of the previous tile (two accumulators where a CTA has several tiles)
 // With few tiles the CTAs of a cluster (p.splits) share the k-blocks of one tile; the partial tiles meet in distributed
@@ -271,74 +288,89 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     pdl_launch();
 
     Tiles t = first_tile<SCORE>(cluster);
-    if (warp == 0) {
-        if (lane == 0) {
-            pdl_wait();
-            const int b_half = p.T / CG;
-            const uint32_t bytes = (uint32_t)CG * ((p.a_box + b_half) * KBYTES + (1 + p.sf_tiles) * 2 * SF_TILE);
-            int it = 0;
-            while (!*abort_flag && next_tile<SCORE>(p, t, clusters)) {
-                const int a_row = (t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS;
-                const int b_row = t.b0 + (CG == 2 ? (int)rank * b_half : 0);
-                const int sfb_group = t.b0 / ROWS;
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = it % S;
-                    if (it >= S && !mbar_wait(&ctl.empty[s], ((it / S) - 1) & 1, abort_flag)) {
-                        *abort_flag = 1;
-                        break;
+    const int b_half = p.T / CG, a_bytes = p.a_box * KBYTES, b_bytes = b_half * KBYTES;
+    if (warp == 0 || warp == 6) {
+        // Producers: codes (warp 0) and scales (warp 6) of the same stage, reported to one barrier.
+        pdl_wait();
+        const uint32_t bytes = (uint32_t)CG * (a_bytes + b_bytes + (1 + p.sf_tiles) * 2 * SF_TILE);
+        Ring r;
+        r.parity = 1;                                        // a fresh barrier passes a wait for the phase before its first
+        bool ok = true;
+        while (ok && next_tile<SCORE>(p, t, clusters)) {
+            const int a_row = (t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS;
+            const int b_row = t.b0 + (CG == 2 ? (int)rank * b_half : 0);
+            const int sfa_row = a_row / ROWS * p.quads, sfb_row = t.b0 / ROWS * p.quads;
+            for (int kb = kb0; kb < kb1; ++kb, r.next(S)) {
+                ok = __all_sync(0xffffffffu, mbar_wait(&ctl.empty[r.s], r.parity, abort_flag));
+                if (!ok) break;
+                const uint32_t a = smem_u32(ring) + r.s * sbytes;
+                uint32_t bar = smem_u32(&ctl.full[r.s]);
+                if (CG == 2) bar = cluster_map(bar, 0);
+                if (elect()) {
+                    if (warp == 0) {
+                        if (CG == 1 || rank == 0) mbar_expect_tx(&ctl.full[r.s], bytes);
+                        load_2d<CG>(a, &map_a, kb * KBYTES, a_row, bar);
+                        load_2d<CG>(a + a_bytes, &map_b, kb * KBYTES, b_row, bar);
+                    } else {
+                        const uint32_t sf = a + a_bytes + b_bytes;
+                        load_2d<CG>(sf, &map_sfa, 0, sfa_row + 2 * kb, bar);
+                        load_2d<CG>(sf + 2 * SF_TILE, &map_sfb, 0, sfb_row + 2 * kb, bar);
+                        if (p.sf_tiles > 1) load_2d<CG>(sf + 4 * SF_TILE, &map_sfb, 0, sfb_row + p.quads + 2 * kb, bar);
                     }
-                    uint8_t* a = ring + (size_t)s * sbytes;
-                    uint8_t* b = a + p.a_box * KBYTES;
-                    uint8_t* sf = b + b_half * KBYTES;
-                    uint32_t bar = smem_u32(&ctl.full[s]);
-                    if (CG == 2) bar = cluster_map(bar, 0);
-                    if (CG == 1 || rank == 0) mbar_expect_tx(&ctl.full[s], bytes);
-                    load_2d<CG>(a, &map_a, kb * KBYTES, a_row, bar);
-                    load_2d<CG>(b, &map_b, kb * KBYTES, b_row, bar);
-                    load_2d<CG>(sf, &map_sfa, 0, (a_row / ROWS) * p.quads + 2 * kb, bar);
-                    for (int g = 0; g < p.sf_tiles; ++g)
-                        load_2d<CG>(sf + (1 + g) * 2 * SF_TILE, &map_sfb, 0, (sfb_group + g) * p.quads + 2 * kb, bar);
                 }
+                __syncwarp();
             }
         }
+        if (!ok) *abort_flag = 1;
     } else if (warp == 1) {
-        if (lane == 0 && (CG == 1 || rank == 0)) {
-            int it = 0, n = 0;
-            while (!*abort_flag && next_tile<SCORE>(p, t, clusters)) {
-                const int acc = n % p.n_acc;
-                if (n >= p.n_acc && !mbar_wait(&ctl.acc_empty[acc], ((n / p.n_acc) - 1) & 1, abort_flag)) {
-                    *abort_flag = 1;
-                    break;
-                }
+        if (CG == 1 || rank == 0) {
+            const uint32_t idesc = instr_desc(ROWS * CG, p.T);      // of a tile cut short at the end of a range, the last columns go unread
+            const int sf_cols = scale_columns(p.sf_tiles), sfb_step = 4 * p.sf_tiles;
+            Ring r;
+            int acc = 0, odd = 0;
+            uint32_t acc_parity = 1;
+            bool ok = true;
+            while (ok && next_tile<SCORE>(p, t, clusters)) {
+                ok = __all_sync(0xffffffffu, mbar_wait(&ctl.acc_empty[acc], acc_parity, abort_flag));
+                if (!ok) break;
                 tc_fence_after();
-                const uint32_t idesc = instr_desc(ROWS * CG, p.T);      // of a tile cut short at the end of a range, the last columns go unread
                 const uint32_t d = tmem + d_col + acc * p.T;
                 const uint32_t b_col = (uint32_t)(t.b0 % ROWS) / 32;
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = it % S;
-                    if (!mbar_wait(&ctl.full[s], (it / S) & 1, abort_flag)) {
-                        *abort_flag = 1;
-                        break;
-                    }
+                for (int kb = kb0; kb < kb1; ++kb, r.next(S), odd ^= 1) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&ctl.full[r.s], r.parity, abort_flag));
+                    if (!ok) break;
                     tc_fence_after();
-                    const uint32_t a_addr = smem_u32(ring + (size_t)s * sbytes), b_addr = a_addr + p.a_box * KBYTES,
-                                   sf_addr = b_addr + p.T / CG * KBYTES;
-                    const uint32_t sfa = tmem + (it & 1) * scale_columns(p.sf_tiles), sfb = sfa + 8;
-                    const int steps = min(KBLOCK / MMA_K, (p.K - kb * KBLOCK + MMA_K - 1) / MMA_K), quads = (steps + 1) / 2;
-                    for (int q = 0; q < quads; ++q) {
-                        scales_to_tmem<CG>(sfa + q * 4, desc_scales(sf_addr + q * SF_TILE));
-                        for (int g = 0; g < p.sf_tiles; ++g)
-                            scales_to_tmem<CG>(sfb + (q * p.sf_tiles + g) * 4, desc_scales(sf_addr + ((1 + g) * 2 + q) * SF_TILE));
+                    const uint32_t a_addr = smem_u32(ring) + r.s * sbytes, sf_addr = a_addr + a_bytes + b_bytes;
+                    const uint32_t sfa = tmem + odd * sf_cols, sfb = sfa + 8;
+                    const uint64_t ad = desc_sw128(a_addr), bd = desc_sw128(a_addr + a_bytes), sd = desc_scales(sf_addr);
+                    const int left = p.K - kb * KBLOCK;
+                    if (elect()) {
+                        // a scale tile is 512 bytes: +32 in a descriptor's address field; 64 elements are 32 bytes: +2
+                        auto scales = [&](int q) {
+                            scales_to_tmem<CG>(sfa + q * 4, sd + q * 32);
+                            scales_to_tmem<CG>(sfb + q * sfb_step, sd + 64 + q * 32);
+                            if (p.sf_tiles > 1) scales_to_tmem<CG>(sfb + q * sfb_step + 4, sd + 128 + q * 32);
+                        };
+                        auto multiply = [&](int k) {
+                            mma_mxf4<CG>(d, ad + 2 * k, bd + 2 * k, idesc | scale_ids((k & 1) * 2), sfa + (k >> 1) * 4,
+                                         sfb + (k >> 1) * sfb_step + b_col, (kb > kb0 || k > 0) ? 1u : 0u);
+                        };
+                        scales(0);
+                        if (left > KBLOCK / 2) scales(1);
+                        if (left > KBLOCK - MMA_K) {
+#pragma unroll
+                            for (int k = 0; k < KBLOCK / MMA_K; ++k) multiply(k);
+                        } else {
+                            for (int k = 0; k * MMA_K < left; ++k) multiply(k);
+                        }
+                        commit<CG>(&ctl.empty[r.s]);
+                        if (kb == kb1 - 1) commit<CG>(&ctl.acc_full[acc]);
                     }
-                    const uint64_t ad = desc_sw128(a_addr), bd = desc_sw128(b_addr);
-                    for (int k = 0; k < steps; ++k)          // 64 elements are 32 bytes: +2 in the descriptors' address fields
-                        mma_mxf4<CG>(d, ad + 2 * k, bd + 2 * k, idesc | scale_ids((k & 1) * 2), sfa + (k >> 1) * 4,
-                                     sfb + (k >> 1) * 4 * p.sf_tiles + b_col, (kb > kb0 || k > 0) ? 1u : 0u);
-                    commit<CG>(&ctl.empty[s]);
+                    __syncwarp();
                 }
-                commit<CG>(&ctl.acc_full[acc]);
-                ++n;
+                if (++acc == p.n_acc) acc = 0, acc_parity ^= 1;
             }
+            if (!ok) *abort_flag = 1;
         }
     } else {
         const int quarter = warp & 3;                        // the lanes of tensor memory that this warp may read
@@ -442,7 +474,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // sum of the partial tiles over the cluster
         cluster_arrive();
         cluster_wait();
-        if (warp >= 2) {
+        if (warp >= 2 && warp < 6) {
             Tiles u = first_tile<SCORE>(cluster);
             next_tile<SCORE>(p, u, clusters);
             const int rows = min(u.rows, p.b_rows - u.b0), row = (warp & 3) * 32 + lane, a = u.a0 * ROWS + row;
