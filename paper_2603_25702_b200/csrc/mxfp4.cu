@@ -204,16 +204,6 @@ int encode_codes(const ops::Device* dev, CUtensorMap* map, const void* codes, in
 
 constexpr int MAX_SMEM = 227 * 1024;
 
-template <int CG, bool SCORE>
-int raise_limit(const ops::Device* dev) {
-    static std::atomic<bool> done[64];
-    if (done[dev->id].load(std::memory_order_acquire)) return S2D2_OK;
-    const cudaError_t e = cudaFuncSetAttribute(mx::product_kernel<CG, SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
-    if (e != cudaSuccess) return ops::fail(S2D2_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
-    done[dev->id].store(true, std::memory_order_release);
-    return S2D2_OK;
-}
-
 int check_operands(const ops::Device* dev, const void* xc, const void* xs, const void* wc, const void* ws) {
     if (int rc = ops::check_ptr(dev, xc, 16, "x_codes")) return rc;
     if (int rc = ops::check_ptr(dev, xs, 16, "x_scales")) return rc;
@@ -244,20 +234,30 @@ struct Plan {
     int cg = 1, grid = 0, smem = 0;
 };
 
+bool two_accumulators(int T, int sf_tiles) { return mx::used_columns(T, sf_tiles, 2) <= 512; }
+
 // Accumulators, tensor-memory columns, shared memory and ring depth once tiles, T, sf_tiles and splits are known.
 void finish_plan(Plan& plan, long long tiles_per_cluster, int stages_wanted) {
     mx::Params& p = plan.p;
-    p.n_acc = tiles_per_cluster > 1 ? 2 : 1;
+    p.n_acc = tiles_per_cluster > 1 && two_accumulators(p.T, p.sf_tiles) ? 2 : 1;
     const int used = mx::used_columns(p.T, p.sf_tiles, p.n_acc);
     p.tmem_cols = 32;
     while ((int)p.tmem_cols < used) p.tmem_cols *= 2;
     const int sbytes = mx::stage_bytes(plan.cg, p.a_box, p.T, p.sf_tiles), fixed = 1024 + (int)sizeof(mx::Control),
               pad = mx::ring_bytes(plan.cg, 0, p.a_box, p.T, p.sf_tiles);
-    // one CTA's ring never needs more than half an SM's memory when the tile is small: the next kernel's set-up fits beside it
-    const int room = (p.tmem_cols <= 256 && plan.cg == 1 ? 113 * 1024 : MAX_SMEM) - fixed;
+    // CTAs that share k-blocks may be two to an SM
+    const int room = (p.splits > 1 ? 113 * 1024 : MAX_SMEM) - fixed;
     p.stages = std::max(2, std::min(std::min(mx::MAX_STAGES, (room - pad) / sbytes), stages_wanted));
     p.control_at = std::max(mx::ring_bytes(plan.cg, p.stages, p.a_box, p.T, p.sf_tiles), p.splits > 1 ? p.T * mx::ROWS * 4 : 0);
     plan.smem = std::max(fixed + p.control_at, mx::min_smem(p.tmem_cols));
+}
+
+// Clock cycles of a tile, for choosing T.  A k-block costs the larger of what the SM takes in (64 bytes a cycle) and what its tensor
+// core multiplies (2 T cycles for 128 x T x 256); without a second accumulator the next tile waits for the read of this one.
+double tile_cycles(int cg, int a_box, int T, int kb_total) {
+    const int sf_tiles = T > 128 ? 2 : 1;
+    const double in = mx::stage_bytes(cg, a_box, T, sf_tiles) / 64.0;
+    return kb_total * std::max(in, 2.0 * T) + 400 + (two_accumulators(T, sf_tiles) ? 0 : 600);
 }
 
 void plan_product(Plan& plan, int n_sms, int M, int N, int K) {
@@ -272,9 +272,12 @@ void plan_product(Plan& plan, int n_sms, int M, int N, int K) {
     if (M > 128) {
         // Pairs of CTAs, if the tiles occupy at least half of them: T by the number of waves times a tile's length.
         const int pairs = n_sms / 2, a_tiles = ceil_div(N, 256);
-        auto cost = [&](int T) { return (double)ceil_div((long long)a_tiles * ceil_div(M, T), pairs) * (T + 16); };
-        p.T = cost(128) <= cost(192) ? 128 : 192;
-        if (M <= 224 && cost((M + 31) / 32 * 32) <= cost(p.T)) p.T = (M + 31) / 32 * 32;      // one tile: any width
+        double best = 1e30;
+        for (int T = 128; T <= 256; T += 64) {
+            const int width = M < T ? (M + 31) / 32 * 32 : T;                                  // one tile: any width
+            const double cost = (double)ceil_div((long long)a_tiles * ceil_div(M, T), pairs) * tile_cycles(2, mx::ROWS, width, p.kb_total);
+            if (cost < best) best = cost, p.T = width;
+        }
         p.a_tiles = a_tiles;
         p.b_tiles = ceil_div(M, p.T);
         if ((long long)p.a_tiles * p.b_tiles * 2 >= pairs) {
@@ -293,8 +296,8 @@ void plan_product(Plan& plan, int n_sms, int M, int N, int K) {
     p.b_tiles = ceil_div(M, p.T);
     p.sf_tiles = 1;                            // T = 128, or one tile
     const long long tiles = (long long)p.a_tiles * p.b_tiles;
-    // Few tiles: split k while the CTAs fit side by side (two per SM) and each keeps at least two k-blocks.
-    while (p.splits < 8 && tiles * p.splits <= n_sms && p.kb_total >= 4 * p.splits) p.splits *= 2;
+    // Few tiles: split k while the CTAs fit side by side (two per SM with narrow tiles) and each keeps at least two k-blocks.
+    while (p.splits < 8 && tiles * p.splits * (p.T <= 64 ? 1 : 2) <= n_sms && p.kb_total >= 4 * p.splits) p.splits *= 2;
     const int clusters = (int)std::min<long long>(tiles, p.splits > 1 ? tiles : n_sms);
     plan.grid = clusters * p.splits;
     const long long per_cluster = (tiles + clusters - 1) / clusters;
@@ -317,19 +320,22 @@ void plan_score(Plan& plan, int n_sms, int M, int N, int K) {
     plan.cg = score_cg(M);
     p.a_tiles = ceil_div(M, mx::ROWS * plan.cg);
     p.a_box = std::min(mx::ROWS, (M + 7) / 8 * 8);
-    // Ranges of the head's rows per A tile, and the tile's T: least time of the busiest cluster, in B rows; 16 rows' time for
-    // the start of a tile, 64 for that of an item.
+    // Ranges of the head's rows per A tile, and the tile's T, by the time of the busiest cluster.
     const int slots = n_sms / plan.cg;
     double best = 1e30;
-    for (int T = 64; T <= 192; T += 64) {
-        const int unit = T == 128 ? 128 : 64, units = ceil_div(N, unit);
+    for (int T = 64; T <= 256; T += 64) {
+        const int unit = T % 128 ? 64 : 128, units = ceil_div(N, unit);
+        if (plan.cg == 1 && T > 192) break;
+        const double full = tile_cycles(plan.cg, p.a_box, T, p.kb_total);
         for (int r = 1; r <= std::min(units, score_max_ranges(p.a_tiles, N)); ++r) {
             const int waves = ceil_div((long long)p.a_tiles * r, slots), len = ceil_div(units, r) * unit;
-            const double cost = waves * ((double)ceil_div(len, T) * (T + 16) + 64);
+            // a single CTA loads no more of its last tile than the range holds
+            const int rest = plan.cg == 1 && len % T ? len % T : T;
+            const double cost = waves * ((ceil_div(len, T) - 1) * full + tile_cycles(plan.cg, p.a_box, rest, p.kb_total) + 1000);
             if (cost < best) best = cost, p.ranges = r, p.T = T, p.unit = unit;
         }
     }
-    p.sf_tiles = p.T > 128 ? 2 : 1;            // T = 64 and 192 start at multiples of 64, T = 128 at multiples of 128
+    p.sf_tiles = p.T > 128 ? 2 : 1;            // T = 64 and 192 start at multiples of 64, T = 128 and 256 at multiples of 128
     p.b_tiles = 0;
     const long long items = (long long)p.a_tiles * p.ranges;
     const int clusters = (int)std::min<long long>(items, slots);
@@ -337,11 +343,18 @@ void plan_score(Plan& plan, int n_sms, int M, int N, int K) {
     finish_plan(plan, 2, mx::MAX_STAGES);
 }
 
-template <int CG, bool SCORE>
+template <int CG, bool SCORE, int NQ>
 int launch_product(const ops::Device* dev, const Plan& plan, const CUtensorMap* maps, cudaStream_t st) {
-    if (int rc = raise_limit<CG, SCORE>(dev)) return rc;
-    const cudaError_t e = ops::launch(mx::product_kernel<CG, SCORE>, dim3((unsigned)plan.grid), mx::THREADS, plan.smem, CG * plan.p.splits, st,
-                                      maps[0], maps[1], maps[2], maps[3], plan.p);
+    const auto kernel = mx::product_kernel<CG, SCORE, NQ>;
+    static std::atomic<bool> raised[64];
+    cudaError_t e = cudaSuccess;
+    if (!raised[dev->id].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
+        if (e == cudaSuccess) raised[dev->id].store(true, std::memory_order_release);
+    }
+    if (e == cudaSuccess)
+        e = ops::launch(kernel, dim3((unsigned)plan.grid), mx::THREADS, plan.smem, CG * plan.p.splits, st, maps[0], maps[1], maps[2], maps[3],
+                        maps[4], plan.p);
     if (e == cudaSuccess) return S2D2_OK;
     cudaGetLastError();
     return ops::fail(S2D2_ERR_CUDA, "mxfp4 product: %s", cudaGetErrorString(e));
@@ -349,12 +362,19 @@ int launch_product(const ops::Device* dev, const Plan& plan, const CUtensorMap* 
 
 template <bool SCORE>
 int run_product(const ops::Device* dev, Plan& plan, const void* ac, const void* as, const void* bc, const void* bs, cudaStream_t st) {
-    CUtensorMap maps[4];
-    if (int rc = encode_codes(dev, &maps[0], ac, plan.p.a_rows, plan.p.K, plan.p.a_box)) return rc;
-    if (int rc = encode_codes(dev, &maps[1], bc, plan.p.b_rows, plan.p.K, plan.p.T / plan.cg)) return rc;
-    if (int rc = encode_scales(dev, &maps[2], as, plan.p.a_rows, plan.p.K)) return rc;
-    if (int rc = encode_scales(dev, &maps[3], bs, plan.p.b_rows, plan.p.K)) return rc;
-    return plan.cg == 1 ? launch_product<1, SCORE>(dev, plan, maps, st) : launch_product<2, SCORE>(dev, plan, maps, st);
+    const mx::Params& p = plan.p;
+    CUtensorMap maps[5];
+    if (int rc = encode_codes(dev, &maps[0], ac, p.a_rows, p.K, p.a_box)) return rc;
+    if (int rc = encode_codes(dev, &maps[1], bc, p.b_rows, p.K, p.T / plan.cg)) return rc;
+    if (SCORE && plan.cg == 1) {
+        if (int rc = encode_codes(dev, &maps[2], bc, p.b_rows, p.K, mx::CUT)) return rc;
+    } else {
+        maps[2] = maps[1];
+    }
+    if (int rc = encode_scales(dev, &maps[3], as, p.a_rows, p.K)) return rc;
+    if (int rc = encode_scales(dev, &maps[4], bs, p.b_rows, p.K)) return rc;
+    if (plan.cg == 1) return p.T <= 64 ? launch_product<1, SCORE, 1>(dev, plan, maps, st) : launch_product<1, SCORE, 3>(dev, plan, maps, st);
+    return p.T <= 192 ? launch_product<2, SCORE, 3>(dev, plan, maps, st) : launch_product<2, SCORE, 4>(dev, plan, maps, st);
 }
 
 }  // namespace
@@ -408,7 +428,7 @@ extern "C" int s2d2_mxfp4_score_workspace(int32_t M, int32_t N, int32_t K, int64
     if (!bytes) return ops::fail(S2D2_ERR_INVALID, "mxfp4_score_workspace: null pointer");
     if (int rc = check_product_shape("mxfp4_score_workspace", M, N, K)) return rc;
     const int rows = mx::ROWS * score_cg(M), a_tiles = ceil_div(M, rows);
-    *bytes = M ? (int64_t)a_tiles * score_max_ranges(a_tiles, N) * rows * 16 : 0;
+    *bytes = M ? (int64_t)a_tiles * score_max_ranges(a_tiles, N) * 2 * rows * 16 : 0;
     return S2D2_OK;
 }
 

@@ -25,13 +25,14 @@ constexpr int KBLOCK = 256;          // elements of a stage's k-block
 constexpr int KBYTES = KBLOCK / 2;
 constexpr int MMA_K = 64;
 constexpr int SF_TILE = 512;         // bytes of one scale tile: 128 rows x 4 blocks
-constexpr int THREADS = 224;        // warps: codes, MMA, four of the epilogue, scales
+constexpr int THREADS = 352;        // warps: codes, MMA, eight of the epilogue, scales
 constexpr int MAX_STAGES = 12;
+constexpr int CUT = 64;              // B rows of a load of a tile that is cut short
 
 // D = A B^T; which matrix is A and which is B depends on the operator (see product_kernel).
 struct Params {
     int a_rows, b_rows, K;           // rows of the two matrices, elements along k
-    int T;                           // B rows of a tile (multiple of 16 CG; 64, 128 or 192 if there are several tiles)
+    int T;                           // B rows of a tile (multiple of 16 CG; of 64 if there are several tiles)
     int a_box;                       // A rows that a CTA loads per tile: 128, or fewer (a multiple of 8) where A has fewer
     int sf_tiles;                    // scale tiles that the B rows of a tile touch (1 or 2)
     int stages;
@@ -50,7 +51,7 @@ struct Params {
     int y_bf16;
     // scores
     const int* tokens;
-    float4* parts;                   // [a_tile][range][A rows of a tile]: maximum, sum, moment (base 2), logit of the token
+    float4* parts;                   // [a_tile][range][column half][A rows of a tile]: maximum, sum, moment (base 2), the token's logit or 0
     int ranges;                      // ranges of B per A tile, in units of `unit` rows
     int unit;
 };
@@ -71,7 +72,9 @@ __host__ __device__ __forceinline__ int ring_bytes(int cg, int stages, int a_box
     return stages * stage_bytes(cg, a_box, T, sf_tiles) + (ROWS - a_box) * KBYTES;
 }
 __host__ __device__ __forceinline__ int scale_columns(int sf_tiles) { return 8 + 8 * sf_tiles; }      // of one of two buffers
-__host__ __device__ __forceinline__ int used_columns(int T, int sf_tiles, int n_acc) { return 2 * scale_columns(sf_tiles) + n_acc * T; }
+// Accumulators are read 32 columns at a time.
+__host__ __device__ __forceinline__ int acc_columns(int T) { return (T + 31) / 32 * 32; }
+__host__ __device__ __forceinline__ int used_columns(int T, int sf_tiles, int n_acc) { return 2 * scale_columns(sf_tiles) + n_acc * acc_columns(T); }
 // Tensor memory is taken with an instruction that waits until enough columns are free.  A CTA of a cluster that waited there for
 // a CTA of another cluster, which waits for its own cluster, could wait for good.  So shared memory is asked for in
 // proportion (57 KB of an SM's 228 KB, 1 KB of it reserved per CTA, for every 128 of its 512 columns): CTAs that fit
@@ -156,6 +159,15 @@ __device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap* map, in
             "l"(map), "r"(x), "r"(y), "r"(bar)
             : "memory");
 }
+// 32 columns of this warp's 32 lanes; several loads may be in flight before load_wait()
+__device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void arrive_remote(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -163,10 +175,45 @@ __device__ __forceinline__ void store_y(void* y, int y_bf16, size_t at, float v)
     if (y_bf16) reinterpret_cast<bf16*>(y)[at] = __float2bfloat16_rn(v);
     else reinterpret_cast<float*>(y)[at] = v;
 }
+// A thread's column of the accumulator: `cols` elements, one in each row of y from `y` on.
+template <typename T, int NQ>
+__device__ __forceinline__ void store_columns(T* y, long long ldy, const uint32_t (&v)[NQ][32], int cols, float scale) {
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        if (q * 32 + 32 <= cols) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, y += ldy) *y = from_f32<T>(scale * __uint_as_float(v[q][j]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, y += ldy)
+                if (q * 32 + j < cols) *y = from_f32<T>(scale * __uint_as_float(v[q][j]));
+        }
+    }
+}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Folds up to 32 logits (accumulators times c, base 2) into a running maximum, sum and moment.
+template <bool FULL>
+__device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float c, float& m, float& s, float& mo) {
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (FULL || j < n) top = fmaxf(top, __uint_as_float(v[j]) * c);
+    const float dm = fmaxf(m - top, -300.f), f = exp2_fast(dm);
+    mo = f * (mo + dm * s);
+    s *= f;
+    m = top;
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (FULL || j < n) {
+            const float u = fmaf(__uint_as_float(v[j]), c, -m), e = exp2_fast(u);
+            s += e;
+            mo += u * e;
+        }
 }
 
 // One lane of a converged warp.  The warps that feed the tensor core and the copy engine run their loops with all lanes, so
@@ -234,17 +281,21 @@ __device__ __forceinline__ bool next_tile(const Params& p, Tiles& t, int cluster
 //   scores (SCORE = true): A = tokens, B = head.  A lane is one token's row of logits: each thread folds the logits of
 //     its token into a running maximum, sum and moment; nothing is exchanged between threads and no logit leaves the SM.
 //   warp 0     producer of the codes: TMA into a ring of stages that runs on from tile to tile
-//   warp 6     producer of the scale tiles of the same stages
+//   warp 10    producer of the scale tiles of the same stages
 //   warp 1     scales to tensor memory (two buffers), four MMAs of 64 elements per stage; tensor memory
-//   warps 2-5  epilogue of the previous tile (two accumulators where a CTA has several tiles)
+//   warps 2-9  epilogue: four lane quarters, two warps for the halves of the columns.  A warp takes its part of the
+//              accumulator (up to 128 columns) into registers at once and gives tensor memory back before it computes
+//              and stores, so the next tile's MMAs wait for a short read only, even with one accumulator.
 // With few tiles the CTAs of a cluster (p.splits) share the k-blocks of one tile; the partial tiles meet in distributed
 // shared memory, where every CTA sums its share of the rows over the cluster in rank order: deterministic, no
 // workspace, no tickets, nothing that two launches could share.
 // Every wait on a barrier is bounded; after a time-out the outputs are NaN and the status word is raised.
-template <int CG, bool SCORE>
-__global__ void __launch_bounds__(THREADS, 1)
+// NQ: groups of 32 columns that an epilogue warp holds; with one (T <= 64) two CTAs fit on an SM by their registers.
+template <int CG, bool SCORE, int NQ>
+__global__ void __launch_bounds__(THREADS, NQ == 1 ? 2 : 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb, const Params p) {
+               const __grid_constant__ CUtensorMap map_cut, const __grid_constant__ CUtensorMap map_sfa,
+               const __grid_constant__ CUtensorMap map_sfb, const Params p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     Control& ctl = *(Control*)(ring + p.control_at);
@@ -266,7 +317,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&ctl.acc_full[b], 1);
-            mbar_init(&ctl.acc_empty[b], 4 * CG);
+            mbar_init(&ctl.acc_empty[b], 8 * CG);
         }
         ctl.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -289,10 +340,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     Tiles t = first_tile<SCORE>(cluster);
     const int b_half = p.T / CG, a_bytes = p.a_box * KBYTES, b_bytes = b_half * KBYTES;
-    if (warp == 0 || warp == 6) {
-        // Producers: codes (warp 0) and scales (warp 6) of the same stage, reported to one barrier.
+    if (warp == 0 || warp == 10) {
+        // Producers: codes (warp 0) and scales (warp 10) of the same stage, reported to one barrier.
         pdl_wait();
-        const uint32_t bytes = (uint32_t)CG * (a_bytes + b_bytes + (1 + p.sf_tiles) * 2 * SF_TILE);
+        const uint32_t fixed_bytes = (uint32_t)CG * (a_bytes + (1 + p.sf_tiles) * 2 * SF_TILE);
         Ring r;
         r.parity = 1;                                        // a fresh barrier passes a wait for the phase before its first
         bool ok = true;
@@ -300,6 +351,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const int a_row = (t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS;
             const int b_row = t.b0 + (CG == 2 ? (int)rank * b_half : 0);
             const int sfa_row = a_row / ROWS * p.quads, sfb_row = t.b0 / ROWS * p.quads;
+            const bool cut = SCORE && CG == 1 && t.rows < p.T;          // a single CTA loads no more of it than the range holds
+            const uint32_t bytes = fixed_bytes + (uint32_t)CG * (cut ? (t.rows + CUT - 1) / CUT * CUT : b_half) * KBYTES;
             for (int kb = kb0; kb < kb1; ++kb, r.next(S)) {
                 ok = __all_sync(0xffffffffu, mbar_wait(&ctl.empty[r.s], r.parity, abort_flag));
                 if (!ok) break;
@@ -310,7 +363,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     if (warp == 0) {
                         if (CG == 1 || rank == 0) mbar_expect_tx(&ctl.full[r.s], bytes);
                         load_2d<CG>(a, &map_a, kb * KBYTES, a_row, bar);
-                        load_2d<CG>(a + a_bytes, &map_b, kb * KBYTES, b_row, bar);
+                        if (!cut) load_2d<CG>(a + a_bytes, &map_b, kb * KBYTES, b_row, bar);
+                        else
+                            for (int i = 0; i < t.rows; i += CUT) load_2d<CG>(a + a_bytes + i * KBYTES, &map_cut, kb * KBYTES, b_row + i, bar);
                     } else {
                         const uint32_t sf = a + a_bytes + b_bytes;
                         load_2d<CG>(sf, &map_sfa, 0, sfa_row + 2 * kb, bar);
@@ -334,7 +389,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 ok = __all_sync(0xffffffffu, mbar_wait(&ctl.acc_empty[acc], acc_parity, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t d = tmem + d_col + acc * p.T;
+                const uint32_t d = tmem + d_col + acc * acc_columns(p.T);
                 const uint32_t b_col = (uint32_t)(t.b0 % ROWS) / 32;
                 for (int kb = kb0; kb < kb1; ++kb, r.next(S), odd ^= 1) {
                     ok = __all_sync(0xffffffffu, mbar_wait(&ctl.full[r.s], r.parity, abort_flag));
@@ -373,91 +428,34 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             if (!ok) *abort_flag = 1;
         }
     } else {
-        const int quarter = warp & 3;                        // the lanes of tensor memory that this warp may read
-        const int row = quarter * 32 + lane;
+        const int quarter = warp & 3, half = (warp - 2) >> 2;      // the lanes of tensor memory that this warp may read; its columns
+        const int row = quarter * 32 + lane, row0 = (CG == 2 ? (int)rank * ROWS : 0) + row;
+        const int half_cols = (p.T / 2 + 31) / 32 * 32;
+        const int col0 = half * half_cols, col1 = half ? p.T : min(half_cols, p.T);
         const float nan = __int_as_float(0x7fffffff);
-        int n = 0;
+        int acc = 0;
+        uint32_t parity = 0;
         // scores
         float m = 0.f, s = 0.f, mo = 0.f, x_t = 0.f;
         int token = -1;
         const float c2 = p.scale * 1.4426950408889634f;
         if (SCORE) pdl_wait();
         while (next_tile<SCORE>(p, t, clusters)) {
-            const int acc = n % p.n_acc;
-            bool ok = !*abort_flag && mbar_wait(&ctl.acc_full[acc], (n / p.n_acc) & 1, abort_flag);
+            bool ok = !*abort_flag && mbar_wait(&ctl.acc_full[acc], parity, abort_flag);
             if (!ok) *abort_flag = 1;
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
-            const uint32_t taddr = tmem + d_col + acc * p.T + ((uint32_t)(quarter * 32) << 16);
-            const int a = (t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS + row;
-            if (!SCORE) {
-                const int rows = min(t.rows, p.b_rows - t.b0);
-                if (p.splits == 1) {
-                    for (int c = 0; c < rows; c += 16) {
-                        float v[16];
-                        tmem_ld16(taddr + c, v);
-                        if (a < p.a_rows) {
+            const uint32_t taddr = tmem + d_col + acc * acc_columns(p.T) + col0 + ((uint32_t)(quarter * 32) << 16);
+            const int a = t.a0 * CG * ROWS + row0;
+            // columns of the tile that are rows of B; lanes that are rows of A
+            const int cols = min(col1, min(t.rows, p.b_rows - t.b0)) - col0;
+            const bool any = a - lane < p.a_rows && cols > 0;
+            uint32_t v[NQ][32];
+            if (any) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                if (c + j < rows) store_y(p.y, p.y_bf16, (size_t)(t.b0 + c + j) * p.ldy + a, ok ? p.scale * v[j] : nan);
-                        }
-                    }
-                } else {
-                    // the ring is idle: a cluster that shares a tile has no other, and all its loads have been multiplied
-                    float* part = reinterpret_cast<float*>(ring);
-                    for (int c = 0; c < rows; c += 16) {
-                        float v[16];
-                        tmem_ld16(taddr + c, v);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (c + j < rows) part[(c + j) * ROWS + row] = ok ? v[j] : nan;
-                    }
-                }
-            } else {
-                if (t.first) {
-                    m = -3.402823466e38f;
-                    s = mo = x_t = 0.f;
-                    token = p.tokens && a < p.a_rows ? p.tokens[a] : -1;
-                }
-                if ((t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS + quarter * 32 < p.a_rows) {
-                    for (int c = 0; c < t.rows; c += 32) {
-                        const int left = p.b_rows - (t.b0 + c);
-                        if (left <= 0) break;
-                        float v[32];
-                        tmem_ld32(taddr + c, v);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] *= c2;
-                        if (left < 32) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j >= left) v[j] = -3.402823466e38f;
-                        }
-                        float top = v[0];
-#pragma unroll
-                        for (int j = 1; j < 32; ++j) top = fmaxf(top, v[j]);
-                        const float m1 = fmaxf(m, top), dm = fmaxf(m - m1, -300.f), f = exp2_fast(dm);
-                        mo = f * (mo + dm * s);
-                        s *= f;
-                        m = m1;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float u = v[j] - m, e = exp2_fast(u);
-                            s += e;
-                            mo += u * e;
-                        }
-                        const int at = token - (t.b0 + c);
-                        if (at >= 0 && at < 32) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j == at) x_t = v[j];
-                        }
-                    }
-                }
-                if (t.last && a < p.a_rows) {
-                    const int range = (t.item - clusters) / p.a_tiles;
-                    p.parts[((size_t)t.a0 * p.ranges + range) * (ROWS * CG) + (CG == 2 ? rank * ROWS : 0) + row] =
-                        ok && !*abort_flag ? make_float4(m, s, mo, x_t) : make_float4(nan, nan, nan, nan);
-                }
+                for (int q = 0; q < NQ; ++q)
+                    if (q * 32 < cols) tmem_ld32_issue(taddr + q * 32, v[q]);
+                tmem_ld_wait();
             }
             // the accumulator may be overwritten (by the pair's first CTA, which issues the MMAs)
             tc_fence_before();
@@ -466,7 +464,46 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&ctl.acc_empty[acc])) : "memory");
                 else arrive_remote(cluster_map(smem_u32(&ctl.acc_empty[acc]), 0));
             }
-            ++n;
+            if (++acc == p.n_acc) acc = 0, parity ^= 1;
+            if (!SCORE) {
+                if (!any) continue;
+                const int b = t.b0 + col0;
+                if (p.splits > 1) {
+                    // the ring is idle: a cluster that shares a tile has no other, and all its loads have been multiplied
+                    float* part = reinterpret_cast<float*>(ring) + (size_t)col0 * ROWS + row;
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (q * 32 + j < cols) part[(q * 32 + j) * ROWS] = ok ? __uint_as_float(v[q][j]) : nan;
+                } else if (a < p.a_rows) {
+                    if (p.y_bf16) store_columns(reinterpret_cast<bf16*>(p.y) + (size_t)b * p.ldy + a, p.ldy, v, cols, ok ? p.scale : nan);
+                    else store_columns(reinterpret_cast<float*>(p.y) + (size_t)b * p.ldy + a, p.ldy, v, cols, ok ? p.scale : nan);
+                }
+            } else {
+                if (t.first) {
+                    m = -3.402823466e38f;
+                    s = mo = x_t = 0.f;
+                    token = p.tokens && a < p.a_rows ? p.tokens[a] : -1;
+                }
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    if (!any || q * 32 >= cols) break;
+                    if (cols - q * 32 >= 32) fold<true>(v[q], 32, c2, m, s, mo);
+                    else fold<false>(v[q], cols - q * 32, c2, m, s, mo);
+                    const int at = token - (t.b0 + col0 + q * 32);
+                    if (at >= 0 && at < 32) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (j == at) x_t = __uint_as_float(v[q][j]) * c2;
+                    }
+                }
+                if (!ok) s = nan;
+                if (t.last && a < p.a_rows) {
+                    const int range = (t.item - clusters) / p.a_tiles;
+                    p.parts[(((size_t)t.a0 * p.ranges + range) * 2 + half) * (ROWS * CG) + row0] = make_float4(m, s, mo, x_t);
+                }
+            }
         }
     }
     __syncwarp();
@@ -474,12 +511,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // sum of the partial tiles over the cluster
         cluster_arrive();
         cluster_wait();
-        if (warp >= 2 && warp < 6) {
+        if (warp >= 2 && warp < 10) {
             Tiles u = first_tile<SCORE>(cluster);
             next_tile<SCORE>(p, u, clusters);
             const int rows = min(u.rows, p.b_rows - u.b0), row = (warp & 3) * 32 + lane, a = u.a0 * ROWS + row;
             const uint32_t mine = smem_u32(ring) + 4 * row;
-            for (int b = split; b < rows; b += p.splits) {
+            for (int b = split + p.splits * ((warp - 2) >> 2); b < rows; b += 2 * p.splits) {
                 float sum = 0.f;
                 for (int q = 0; q < p.splits; ++q) {
                     float v;
@@ -513,7 +550,7 @@ score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse
     pdl_launch();
     const int r = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (r >= p.a_rows) return;
-    const float4* parts = p.parts + (size_t)(r / rows_per_tile) * p.ranges * rows_per_tile + r % rows_per_tile;
+    const float4* parts = p.parts + (size_t)(r / rows_per_tile) * p.ranges * 2 * rows_per_tile + r % rows_per_tile;
     const int token = p.tokens ? p.tokens[r] : -1;
     const bool has_token = token >= 0 && token < p.b_rows;
     const long long units = (p.b_rows + p.unit - 1) / p.unit;
@@ -526,9 +563,10 @@ score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse
         m = M;
     };
     for (int i = lane; i < p.ranges; i += 32) {
-        const float4 v = parts[(size_t)i * rows_per_tile];
+        const float4 v = parts[(size_t)(2 * i) * rows_per_tile], w = parts[(size_t)(2 * i + 1) * rows_per_tile];
         add(v.x, v.y, v.z);
-        if (has_token && token / p.unit >= units * i / p.ranges && token / p.unit < units * (i + 1) / p.ranges) x_t = v.w;
+        add(w.x, w.y, w.z);
+        if (has_token && token / p.unit >= units * i / p.ranges && token / p.unit < units * (i + 1) / p.ranges) x_t = v.w + w.w;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
