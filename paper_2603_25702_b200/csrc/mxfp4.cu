@@ -460,7 +460,7 @@ extern "C" int s2d2_mxfp4_score(const void* d_x_codes, const void* d_x_scales, c
     plan.p.parts = (float4*)d_ws;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     if (int rc = run_product<true>(dev, plan, d_x_codes, d_x_scales, d_w_codes, d_w_scales, st)) return rc;
-    const cudaError_t e = ops::launch(mx::score_parts_kernel, dim3((unsigned)ceil_div(M, 4)), 128, 0, 1, st, plan.p, mx::ROWS * plan.cg,
+    const cudaError_t e = ops::launch(mx::score_parts_kernel, dim3((unsigned)M), 128, 0, 1, st, plan.p, mx::ROWS * plan.cg,
                                       d_logprob, d_lse, d_entropy);
     if (e != cudaSuccess) {
         cudaGetLastError();

@@ -190,9 +190,9 @@ __device__ __forceinline__ void store_columns(T* y, long long ldy, const uint32_
         }
     }
 }
-__device__ __forceinline__ float exp2_fast(float x) {
+__device__ __forceinline__ float exp2_fast(float x) {      // relative error 2^-22; below 2^-126 zero
     float y;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -543,44 +543,42 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (warp == 1) dealloc<CG>(tmem, p.tmem_cols);
 }
 
-// Scores from the partial results of a row's ranges: one warp per row, ranges in a fixed order.
+// Scores from the partial results of a row: one block per row, a thread per part (or several), merged in a fixed order.
 static __global__ void __launch_bounds__(128)
 score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse, float* entropy) {
+    __shared__ float4 sh[4];
     pdl_wait();
     pdl_launch();
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (r >= p.a_rows) return;
+    const int r = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float4* parts = p.parts + (size_t)(r / rows_per_tile) * p.ranges * 2 * rows_per_tile + r % rows_per_tile;
     const int token = p.tokens ? p.tokens[r] : -1;
     const bool has_token = token >= 0 && token < p.b_rows;
     const long long units = (p.b_rows + p.unit - 1) / p.unit;
-    float m = -3.402823466e38f, s = 0.f, mo = 0.f, x_t = 0.f;
-    auto add = [&](float m2, float s2, float mo2) {
-        const float M = fmaxf(m, m2), d1 = fmaxf(m - M, -300.f), d2 = fmaxf(m2 - M, -300.f);
+    float4 a = make_float4(-3.402823466e38f, 0.f, 0.f, 0.f);      // maximum, sum, moment; logit of the token (zero in all parts but one)
+    auto add = [&](const float4 b) {
+        const float M = fmaxf(a.x, b.x), d1 = fmaxf(a.x - M, -300.f), d2 = fmaxf(b.x - M, -300.f);
         const float f1 = exp2_fast(d1), f2 = exp2_fast(d2);
-        mo = f1 * (mo + d1 * s) + f2 * (mo2 + d2 * s2);
-        s = f1 * s + f2 * s2;
-        m = M;
+        a = make_float4(M, f1 * a.y + f2 * b.y, f1 * (a.z + d1 * a.y) + f2 * (b.z + d2 * b.y), a.w + b.w);
     };
-    for (int i = lane; i < p.ranges; i += 32) {
-        const float4 v = parts[(size_t)(2 * i) * rows_per_tile], w = parts[(size_t)(2 * i + 1) * rows_per_tile];
-        add(v.x, v.y, v.z);
-        add(w.x, w.y, w.z);
-        if (has_token && token / p.unit >= units * i / p.ranges && token / p.unit < units * (i + 1) / p.ranges) x_t = v.w + w.w;
+    for (int i = threadIdx.x; i < 2 * p.ranges; i += 128) {
+        float4 b = parts[(size_t)i * rows_per_tile];
+        const int range = i / 2;
+        if (!has_token || token / p.unit < units * range / p.ranges || token / p.unit >= units * (range + 1) / p.ranges) b.w = 0.f;
+        add(b);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o),
-                    mo2 = __shfl_xor_sync(0xffffffffu, mo, o);
-        x_t += __shfl_xor_sync(0xffffffffu, x_t, o);          // one lane has it, the others zero
-        add(m2, s2, mo2);
-    }
-    if (lane) return;
-    const float ln2 = 0.6931471805599453f, log_s = log2f(s), nan = __int_as_float(0x7fffffff);
-    const bool undefined = !(s > 0.f) || isinf(m);
-    if (lse) lse[r] = undefined ? nan : (m + log_s) * ln2;
-    if (entropy) entropy[r] = undefined ? nan : (log_s - mo / s) * ln2;
-    if (logprob) logprob[r] = undefined || !has_token ? nan : ((x_t - m) - log_s) * ln2;
+    for (int o = 16; o > 0; o >>= 1)
+        add(make_float4(__shfl_xor_sync(0xffffffffu, a.x, o), __shfl_xor_sync(0xffffffffu, a.y, o), __shfl_xor_sync(0xffffffffu, a.z, o),
+                        __shfl_xor_sync(0xffffffffu, a.w, o)));
+    if (lane == 0) sh[warp] = a;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 4; ++w) add(sh[w]);
+    const float ln2 = 0.6931471805599453f, log_s = log2f(a.y), nan = __int_as_float(0x7fffffff);
+    const bool undefined = !(a.y > 0.f) || isinf(a.x);
+    if (lse) lse[r] = undefined ? nan : (a.x + log_s) * ln2;
+    if (entropy) entropy[r] = undefined ? nan : (log_s - a.z / a.y) * ln2;
+    if (logprob) logprob[r] = undefined || !has_token ? nan : ((a.w - a.x) - log_s) * ln2;
 }
 
 }  // namespace mx

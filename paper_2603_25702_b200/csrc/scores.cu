@@ -51,10 +51,46 @@ struct ScoreParams {
     float* top_lp;
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {      // relative error 2^-22; 0 for -inf, NaN for NaN
+// Relative error 2^-22; 0 for -inf, NaN for NaN.  Results below 2^-126 become zero (they are next to sums of at least one), which
+// saves the scaling of subnormal results: three instructions of about ten per element.
+__device__ __forceinline__ float exp2_fast(float x) {
     float y;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Two fp32 operations per instruction, each rounded as the scalar one.
+struct Pair {
+    unsigned long long v;
+};
+__device__ __forceinline__ Pair pair(float a, float b) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ float lo(Pair p) {
+    float a, b;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v));
+    return a;
+}
+__device__ __forceinline__ float hi(Pair p) {
+    float a, b;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v));
+    return b;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+    Pair p;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(p.v) : "l"(a.v), "l"(b.v));
+    return p;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    Pair p;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p.v) : "l"(a.v), "l"(b.v));
+    return p;
+}
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c) {
+    Pair p;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(p.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return p;
 }
 // Larger key = earlier in the order (value descending, id ascending).  -0 counts as +0.
 __device__ __forceinline__ unsigned long long order_key(float v, int id) {
@@ -79,26 +115,37 @@ struct Row {
         lead = (int)(((uintptr_t)row & 15) / sizeof(T));
     }
     __device__ __forceinline__ int first_id(int vec) const { return vec * E - lead; }
-    __device__ __forceinline__ void load(int vec, float* x) const {
-        const int i0 = first_id(vec);
-        if (i0 >= 0 && i0 + E <= V) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4*>(p + i0));
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-            if (sizeof(T) == 4) {
+    static __device__ __forceinline__ void widen(const uint4 w, float* x) {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        if (sizeof(T) == 4) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(u[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[2 * e] = __uint_as_float(u[e] << 16);
-                    x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-                }
-            }
+            for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(u[e]);
         } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = (i0 + e >= 0 && i0 + e < V) ? to_f32(p[i0 + e]) : -INFINITY;
+            for (int e = 0; e < 4; ++e) {
+                x[2 * e] = __uint_as_float(u[e] << 16);
+                x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+            }
         }
     }
+    // a vector as it stands in memory; `inside`: all of it lies in the row
+    __device__ __forceinline__ uint4 raw(int vec, bool inside) const {
+        const int i0 = first_id(vec);
+        if (inside || (i0 >= 0 && i0 + E <= V)) return __ldg(reinterpret_cast<const uint4*>(p + i0));
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < E; e += 4 / (int)sizeof(T)) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
+                const float f = (i0 + e + h >= 0 && i0 + e + h < V) ? to_f32(p[i0 + e + h]) : -INFINITY;
+                w |= sizeof(T) == 4 ? __float_as_uint(f) : (__float_as_uint(f) >> 16) << (16 * h);
+            }
+            u[e * (int)sizeof(T) / 4] = w;
+        }
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    __device__ __forceinline__ void load(int vec, float* x) const { widen(raw(vec, false), x); }
 };
 
 // 32 lanes' values sorted, largest in lane 0
@@ -315,46 +362,60 @@ __global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
     const int n_vec = (row.lead + p.V + E - 1) / E;
     const int v0 = min(n_vec, (int)rank * p.seg_vec), v1 = min(n_vec, v0 + p.seg_vec);
 
+    // Two tiles in flight per thread.  All vectors of a tile lie inside the row, except in the first (elements in front of
+    // the row) and from last_full on.
+    uint4 buf[2][VPT];
+    const int first_full = row.lead ? 1 : 0, last_full = (min(v1 * E, row.lead + p.V) / E - v0) / (VPT * NT);
+    auto fetch = [&](int i, uint4 (&to)[VPT]) {
+        const int vt = v0 + i * VPT * NT + (int)threadIdx.x;
+        if (i >= first_full && i < last_full) {
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) to[j] = row.raw(vt + j * NT, true);
+        } else {
+            const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) to[j] = vt + j * NT < v1 ? row.raw(vt + j * NT, false) : make_uint4(none, none, none, none);
+        }
+    };
+    if (p.n_tiles > 0) fetch(0, buf[0]);
+    if (p.n_tiles > 1) fetch(1, buf[1]);
+
     const int token = p.tokens ? p.tokens[r] : -1;
     const bool has_token = token >= 0 && token < p.V;
     const float x_t = has_token ? to_f32(row.p[token]) : 0.f;
     const float x_next = nextafterf(x_t, INFINITY);      // x >= x_next is x > x_t
 
-    float m = -FLT_MAX, s = 0.f, t = 0.f, mine = -INFINITY;
+    float m = -FLT_MAX, mine = -INFINITY;
+    Pair s2 = pair(0.f, 0.f), t2 = pair(0.f, 0.f);       // t2: sum of u 2^u, in units of log 2
     int before = 0;
-    float x[TILE], nx[TILE];
-    auto fetch = [&](int i, float* to) {
-        const int vt = v0 + i * VPT * NT + (int)threadIdx.x;
+    auto fold = [&](int i, const uint4 (&from)[VPT]) {
+        float x[TILE];
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            if (vt + j * NT < v1) row.load(vt + j * NT, to + j * E);
-            else
-#pragma unroll
-                for (int e = 0; e < E; ++e) to[j * E + e] = -INFINITY;
-        }
-    };
-    fetch(0, nx);
-    for (int i = 0; i < p.n_tiles; ++i) {
-#pragma unroll
-        for (int e = 0; e < TILE; ++e) x[e] = nx[e];
-        if (i + 1 < p.n_tiles) fetch(i + 1, nx);
+        for (int j = 0; j < VPT; ++j) Row<T>::widen(from[j], x + j * E);
         float tm = x[0];
 #pragma unroll
         for (int e = 1; e < TILE; ++e) tm = fmaxf(tm, x[e]);
         if (p.top) tile_max[i * NT + threadIdx.x] = tm;
         mine = fmaxf(mine, tm);
-        const float m1 = fmaxf(m, tm), d = fmaxf((m - m1) * LOG2E, -300.f), f = exp2_fast(d);
-        t = f * (t + d * s);
-        s = f * s;
-        m = m1;
-#pragma unroll
-        for (int e = 0; e < TILE; ++e) {
-            const float u = (x[e] - m) * LOG2E;
-            const float ex = exp2_fast(u);       // NaN for a NaN, and for +inf (m is +inf then): such a row is reported as NaN
-            s += ex;
-            t += fmaxf(u, -300.f) * ex;
+        if (tm > m) {
+            const float d = fmaxf((m - tm) * LOG2E, -300.f), f = exp2_fast(d);
+            const Pair ff = pair(f, f);
+            t2 = ff * fma(pair(d, d), s2, t2);
+            s2 = ff * s2;
+            m = tm;
         }
-        if (has_token) {
+        const Pair minus_m = pair(-m, -m), log2e = pair(LOG2E, LOG2E);
+#pragma unroll
+        for (int e = 0; e < TILE; e += 2) {
+            const Pair u = (pair(x[e], x[e + 1]) + minus_m) * log2e;
+            const float u0 = lo(u), u1 = hi(u);
+            // NaN for a NaN, and for +inf (m is +inf then): such a row is reported as NaN
+            const Pair ex = pair(exp2_fast(u0), exp2_fast(u1));
+            s2 = s2 + ex;
+            t2 = fma(pair(fmaxf(u0, -300.f), fmaxf(u1, -300.f)), ex, t2);
+        }
+        // tokens that come before the given one: of most tiles not even the largest does
+        if (has_token && tm >= x_t) {
             const int vt = v0 + i * VPT * NT + (int)threadIdx.x;
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
@@ -371,7 +432,14 @@ __global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
                 }
             }
         }
+    };
+    for (int i = 0; i < p.n_tiles; i += 2) {
+        fold(i, buf[0]);
+        if (i + 2 < p.n_tiles) fetch(i + 2, buf[0]);
+        if (i + 1 < p.n_tiles) fold(i + 1, buf[1]);
+        if (i + 3 < p.n_tiles) fetch(i + 3, buf[1]);
     }
+    float s = lo(s2) + hi(s2), t = lo(t2) + hi(t2);
     // the CTA's sums, merged in a fixed order
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
