@@ -9,8 +9,9 @@
 // log s - t/s then adds two non-negative terms, where lse - sum x p subtracts numbers of the size of the logits.
 //
 // The top alternatives cost nothing per element: the loop keeps the maximum of every (thread, 16 elements) tile in shared memory.
-// The k-th largest of the 256 thread maxima is a lower bound of the k-th largest element, so only tiles whose maximum reaches
-// it are read again (a little over k tiles of 16 elements), and only elements that reach it are sorted.
+// If every one of the eight warps has at least ceil(k / 8) threads whose maximum is t or more, t is a lower bound of the k-th
+// largest element.  So only tiles whose maximum reaches the least of the warps' ceil(k / 8)-th largest thread maxima are read
+// again (two to three tiles of 16 elements per alternative), and only elements that reach it are ordered.
 //
 // A row is shared by a cluster of 1, 2, 4 or 8 CTAs, so that a few rows fill the GPU; partial results meet in the shared memory
 // of the cluster's first CTA.  Nothing is kept in global memory, no atomics on it, no workspace.
@@ -30,6 +31,7 @@ constexpr int NW = NT / 32;
 constexpr int TILE = 16;           // elements of one thread between two rescales
 constexpr int CAP = 1024;          // candidates above the threshold held in shared memory
 constexpr int TIES = 256;          // candidates equal to it
+constexpr int TILES = 768;         // tiles that may be read again
 constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int MAX_SMEM = 160 * 1024;   // tile maxima of a CTA's share of the largest vocabulary
@@ -68,14 +70,10 @@ __device__ __forceinline__ Pair pair(float a, float b) {
     return p;
 }
 __device__ __forceinline__ float lo(Pair p) {
-    float a, b;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v));
-    return a;
+    return __uint_as_float((uint32_t)p.v);
 }
 __device__ __forceinline__ float hi(Pair p) {
-    float a, b;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v));
-    return b;
+    return __uint_as_float((uint32_t)(p.v >> 32));
 }
 __device__ __forceinline__ Pair operator+(Pair a, Pair b) {
     Pair p;
@@ -148,46 +146,37 @@ struct Row {
     __device__ __forceinline__ void load(int vec, float* x) const { widen(raw(vec, false), x); }
 };
 
-// 32 lanes' values sorted, largest in lane 0
-__device__ __forceinline__ float warp_sort_desc(float v, int lane) {
-#pragma unroll
-    for (int size = 2; size <= 32; size <<= 1) {
-#pragma unroll
-        for (int o = size >> 1; o > 0; o >>= 1) {
-            const float w = __shfl_xor_sync(0xffffffffu, v, o);
-            const bool up = ((lane & size) == 0) == ((lane & o) == 0);    // this lane keeps the larger
-            v = up ? fmaxf(v, w) : fminf(v, w);
-        }
-    }
-    return v;
-}
-// the 32 largest of two lists of 32, both sorted with the largest first
-__device__ __forceinline__ float warp_merge_desc(float a, float b_reversed, int lane) {
-    float v = fmaxf(a, b_reversed);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float w = __shfl_xor_sync(0xffffffffu, v, o);
-        v = (lane & o) == 0 ? fmaxf(v, w) : fminf(v, w);
-    }
-    return v;
-}
-
 struct alignas(16) Partial {       // one CTA's share of a row
     float m, s, t;
     int before;
 };
 
 struct Shared {
-    unsigned long long top[MAX_CLUSTER][32];     // in the cluster's first CTA: every CTA's best, 0 = none
-    Partial part[MAX_CLUSTER];
-    unsigned long long cand[CAP];
-    unsigned long long tie[TIES];
+    unsigned long long cand[CAP + 8];
+    unsigned long long tie[TIES + 8];
+    unsigned long long top[MAX_CLUSTER][32];     // in the cluster's first CTA: every CTA's best, in order, 0 = none
     unsigned long long best[32];                 // this CTA's best, in order
-    float list[NW][32];
-    Partial warp[NW];
+    Partial part[MAX_CLUSTER * NW];              // in the cluster's first CTA: every warp's sums
+    float bound[NW];
     int warp_count[NW];
-    int n_cand, n_tie;
+    int tile[TILES];                             // tiles that are read again
+    int n_cand, n_tie, n_tile;
+    float m, s;
 };
+
+// Position of `key` among the n keys of `list`, which is padded to a multiple of eight with zeros.
+__device__ __forceinline__ int count_above(const unsigned long long* list, int n, unsigned long long key) {
+    int pos = 0;
+    for (int j = 0; j < n; j += 8) {
+#pragma unroll
+        for (int h = 0; h < 8; h += 2) {
+            const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(list + j + h);
+            pos += w.x > key;
+            pos += w.y > key;
+        }
+    }
+    return pos;
+}
 
 // Appends, in id order, elements equal to `v` of the vectors [v0, v1) to best[n..], until `k` are there.  Whole CTA.
 template <typename T>
@@ -242,65 +231,71 @@ __device__ float largest_below(const Row<T>& row, int v0, int v1, float below, S
             if (x[e] < below) m = fmaxf(m, x[e]);
     }
     m = warp_max(m);
-    if ((threadIdx.x & 31) == 0) sh.list[0][threadIdx.x >> 5] = m;
+    if ((threadIdx.x & 31) == 0) sh.bound[threadIdx.x >> 5] = m;
     __syncthreads();
-    m = sh.list[0][0];
-    for (int w = 1; w < NW; ++w) m = fmaxf(m, sh.list[0][w]);
+    m = sh.bound[0];
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, sh.bound[w]);
     __syncthreads();
     return m;
 }
 
-// This CTA's best `k` elements, in order, to best[0..k) (0 = none).  tile_max[tile][thread] holds the maxima, mine = the
+// This CTA's best `k` elements, in order, to sh.best[0..k) (0 = none).  tile_max[tile][thread] holds the maxima, mine = the
 // largest of this thread's.
 template <typename T>
-__device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, const float* tile_max, float mine, int k,
-                                unsigned long long* best, Shared& sh) {
-    constexpr int VPT = TILE / Row<T>::E;
+__device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, const float* tile_max, float mine, int k, Shared& sh) {
+    constexpr int E = Row<T>::E, VPT = TILE / E;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    // k-th largest thread maximum
-    float v = warp_sort_desc(mine, lane);
-    sh.list[warp][lane] = v;
-    if (threadIdx.x < 32) best[threadIdx.x] = 0;
-    if (threadIdx.x == 0) sh.n_cand = sh.n_tie = 0;
-    __syncthreads();
-#pragma unroll
-    for (int half = NW / 2; half > 0; half >>= 1) {
-        if (warp < half) {
-            v = warp_merge_desc(v, sh.list[warp + half][31 - lane], lane);
-            sh.list[warp][lane] = v;
-        }
-        __syncthreads();
+    unsigned long long* best = sh.best;
+    // the warp's ceil(k / 8)-th largest thread maximum
+    float rest = mine, bound = -INFINITY;
+    for (int i = 0; i < (k + NW - 1) / NW; ++i) {
+        bound = warp_max(rest);
+        const unsigned who = __ballot_sync(0xffffffffu, rest == bound);
+        if (lane == __ffs(who) - 1) rest = -INFINITY;
     }
-    const float thr = sh.list[0][k - 1];
+    if (lane == 0) sh.bound[warp] = bound;
+    if (threadIdx.x < 32) best[threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.n_cand = sh.n_tie = sh.n_tile = 0;
+    __syncthreads();
+    float thr = sh.bound[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) thr = fminf(thr, sh.bound[w]);
     const bool none_equal = thr == -INFINITY;                     // nothing is drawn from elements that are -inf
     const bool many_equal = __syncthreads_count(mine == thr) > TIES / 2;
     const bool equal_too = !none_equal && !many_equal;
     if (mine > thr || (equal_too && mine == thr)) {
+#pragma unroll 4
         for (int i = 0; i < n_tiles; ++i) {
             const float tm = tile_max[i * NT + threadIdx.x];
-            if (!(tm > thr || (equal_too && tm == thr))) continue;
+            if (tm > thr || (equal_too && tm == thr)) {
+                const int at = atomicAdd(&sh.n_tile, 1);
+                if (at < TILES) sh.tile[at] = i * NT + (int)threadIdx.x;
+            }
+        }
+    }
+    __syncthreads();
+    const int n_again = sh.n_tile;
+    if (n_again <= TILES) {
+        for (int i = threadIdx.x; i < n_again * VPT; i += NT) {
+            const int which = sh.tile[i / VPT], vec = v0 + (which / NT * VPT + i % VPT) * NT + which % NT;
+            if (vec >= v1) continue;
+            float x[E];
+            row.load(vec, x);
 #pragma unroll
-            for (int j = 0; j < VPT; ++j) {
-                const int vec = v0 + (i * VPT + j) * NT + (int)threadIdx.x;
-                if (vec >= v1) continue;
-                float x[Row<T>::E];
-                row.load(vec, x);
-#pragma unroll
-                for (int e = 0; e < Row<T>::E; ++e) {
-                    if (x[e] > thr) {
-                        const int at = atomicAdd(&sh.n_cand, 1);
-                        if (at < CAP) sh.cand[at] = order_key(x[e], row.first_id(vec) + e);
-                    } else if (equal_too && x[e] == thr) {
-                        const int at = atomicAdd(&sh.n_tie, 1);
-                        if (at < TIES) sh.tie[at] = order_key(thr, row.first_id(vec) + e);
-                    }
+            for (int e = 0; e < E; ++e) {
+                if (x[e] > thr) {
+                    const int at = atomicAdd(&sh.n_cand, 1);
+                    if (at < CAP) sh.cand[at] = order_key(x[e], row.first_id(vec) + e);
+                } else if (equal_too && x[e] == thr) {
+                    const int at = atomicAdd(&sh.n_tie, 1);
+                    if (at < TIES) sh.tie[at] = order_key(thr, row.first_id(vec) + e);
                 }
             }
         }
     }
     __syncthreads();
     const int n = sh.n_cand, n_tie = sh.n_tie;
-    if (n > CAP) {
+    if (n_again > TILES || n > CAP) {
         // More elements above the bound than are held here (a few threads own most of the large ones): value by value.
         int got = 0;
         float below = INFINITY;
@@ -313,19 +308,23 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
         __syncthreads();
         return;
     }
-    // position of each candidate = how many others come before it
+    // position of each candidate = how many others come before it; elements equal to the bound follow those above it
+    const bool ties_held = !many_equal && n_tie <= TIES;
+    if (threadIdx.x < 8) {
+        sh.cand[n + threadIdx.x] = 0;
+        if (ties_held) sh.tie[n_tie + threadIdx.x] = 0;
+    }
+    __syncthreads();
     for (int i = threadIdx.x; i < n; i += NT) {
         const unsigned long long key = sh.cand[i];
-        int pos = 0;
-        for (int j = 0; j < n; ++j) pos += sh.cand[j] > key;
+        const int pos = count_above(sh.cand, n, key);
         if (pos < k) best[pos] = key;
     }
     if (!none_equal && n < k) {
-        if (!many_equal && n_tie <= TIES) {
+        if (ties_held) {
             for (int i = threadIdx.x; i < n_tie; i += NT) {
                 const unsigned long long key = sh.tie[i];
-                int pos = n;
-                for (int j = 0; j < n_tie; ++j) pos += sh.tie[j] > key;
+                const int pos = n + count_above(sh.tie, n_tie, key);
                 if (pos < k) best[pos] = key;
             }
         } else {
@@ -416,19 +415,18 @@ __global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
         }
         // tokens that come before the given one: of most tiles not even the largest does
         if (has_token && tm >= x_t) {
-            const int vt = v0 + i * VPT * NT + (int)threadIdx.x;
+            const int vt = v0 + i * VPT * NT + (int)threadIdx.x, i0 = row.first_id(vt), i1 = row.first_id(vt + (VPT - 1) * NT) + E;
+            if (i0 >= 0 && (i1 <= token || (i0 > token && vt + (VPT - 1) * NT < v1))) {
+                const float bar = i1 <= token ? x_t : x_next;      // (behind the row's end lie elements read as -inf: never >= x_next)
 #pragma unroll
-            for (int j = 0; j < VPT; ++j) {
-                const int i0 = row.first_id(vt + j * NT);
-                if (vt + j * NT >= v1) continue;
-                if (i0 < 0 || (i0 <= token && token < i0 + E)) {
+                for (int e = 0; e < TILE; ++e) before += x[e] >= bar;
+            } else {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) before += i0 + e >= 0 && x[j * E + e] >= (i0 + e < token ? x_t : x_next);
-                } else {
-                    // behind the row's end lie elements read as -inf: never >= x_next
-                    const float bar = i0 < token ? x_t : x_next;
+                for (int j = 0; j < VPT; ++j) {
+                    if (vt + j * NT >= v1) continue;
+                    const int id = row.first_id(vt + j * NT);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) before += x[j * E + e] >= bar;
+                    for (int e = 0; e < E; ++e) before += id + e >= 0 && id + e < p.V && x[j * E + e] >= (id + e < token ? x_t : x_next);
                 }
             }
         }
@@ -440,86 +438,89 @@ __global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
         if (i + 3 < p.n_tiles) fetch(i + 3, buf[1]);
     }
     float s = lo(s2) + hi(s2), t = lo(t2) + hi(t2);
-    // the CTA's sums, merged in a fixed order
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o),
-                    t2 = __shfl_xor_sync(0xffffffffu, t, o);
-        before += __shfl_xor_sync(0xffffffffu, before, o);
-        merge(m, s, t, m2, s2, t2);
+    // the warp's sums, brought to its maximum; they meet in the cluster's first CTA
+    Partial part;
+    part.m = warp_max(m);
+    {
+        const float d = fmaxf((m - part.m) * LOG2E, -300.f), f = exp2_fast(d);
+        part.t = warp_sum(f * (t + d * s));
+        part.s = warp_sum(f * s);
+        part.before = __reduce_add_sync(0xffffffffu, before);
     }
-    if (lane == 0) sh.warp[warp] = Partial{m, s, t, before};
-    __syncthreads();
-    Partial part = sh.warp[0];
-    if (warp == 0) {
-        part = sh.warp[lane & (NW - 1)];
-#pragma unroll
-        for (int o = NW / 2; o > 0; o >>= 1) {
-            const float m2 = __shfl_xor_sync(0xffffffffu, part.m, o), s2 = __shfl_xor_sync(0xffffffffu, part.s, o),
-                        t2 = __shfl_xor_sync(0xffffffffu, part.t, o);
-            part.before += __shfl_xor_sync(0xffffffffu, part.before, o);
-            merge(part.m, part.s, part.t, m2, s2, t2);
-        }
-    }
-    if (p.top) best_of_segment(row, v0, v1, p.n_tiles, tile_max, mine, p.top, sh.best, sh);
+    if (p.top) best_of_segment(row, v0, v1, p.n_tiles, tile_max, mine, p.top, sh);
 
     if (C > 1) {
         cluster_wait();
         const uint32_t top0 = cluster_map((uint32_t)__cvta_generic_to_shared(&sh.top[rank][0]), 0);
-        const uint32_t part0 = cluster_map((uint32_t)__cvta_generic_to_shared(&sh.part[rank]), 0);
-        if (p.top && (int)threadIdx.x < p.top)
+        const uint32_t part0 = cluster_map((uint32_t)__cvta_generic_to_shared(&sh.part[rank * NW + warp]), 0);
+        if (p.top && threadIdx.x < 32)
             asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(top0 + 8 * threadIdx.x), "l"(sh.best[threadIdx.x]) : "memory");
-        if (threadIdx.x == 0)
+        if (lane == 0)
             asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part0), "r"(__float_as_uint(part.m)),
                          "r"(__float_as_uint(part.s)), "r"(__float_as_uint(part.t)), "r"(part.before)
                          : "memory");
         cluster_arrive();
         cluster_wait();
         if (rank != 0) return;
-        part = sh.part[0];
-        for (int c = 1; c < C; ++c) {
-            merge(part.m, part.s, part.t, sh.part[c].m, sh.part[c].s, sh.part[c].t);
-            part.before += sh.part[c].before;
-        }
-    } else if (threadIdx.x == 0) {
-        sh.part[0] = part;
-    }
-    if (C == 1) {
+    } else {
+        if (lane == 0) sh.part[warp] = part;
         __syncthreads();
-        part = sh.part[0];
     }
-    const bool undefined = isnan(part.s);
-    const float log_s = logf(part.s);
-    if (threadIdx.x == 0) {
-        const float nan = __int_as_float(0x7fffffff);
-        const bool empty = part.s == 0.f;        // every logit is -inf
-        if (p.lse) p.lse[r] = undefined ? nan : empty ? -INFINITY : part.m + log_s;
-        if (p.entropy) p.entropy[r] = undefined ? nan : empty ? 0.f : log_s - part.t * LN2 / part.s;
-        if (p.logprob) p.logprob[r] = undefined || !has_token ? nan : empty ? -INFINITY : (x_t - part.m) - log_s;
-        if (p.rank) p.rank[r] = undefined || !has_token ? -1 : part.before;
+    if (warp == 0) {
+        // C * 8 parts, two per lane at most
+        float pm = -FLT_MAX, ps = 0.f, pt = 0.f;
+        int pb = 0;
+        for (int i = lane; i < C * NW; i += 32) {
+            const Partial q = sh.part[i];
+            merge(pm, ps, pt, q.m, q.s, q.t);
+            pb += q.before;
+        }
+        const float M = warp_max(pm), d = fmaxf((pm - M) * LOG2E, -300.f), f = exp2_fast(d);
+        const float S = warp_sum(f * ps), U = warp_sum(f * (pt + d * ps));
+        pb = __reduce_add_sync(0xffffffffu, pb);
+        if (lane == 0) {
+            const float nan = __int_as_float(0x7fffffff), log_s = logf(S);
+            const bool undefined = isnan(S), empty = S == 0.f;         // empty: every logit is -inf
+            if (p.lse) p.lse[r] = undefined ? nan : empty ? -INFINITY : M + log_s;
+            if (p.entropy) p.entropy[r] = undefined ? nan : empty ? 0.f : log_s - U * LN2 / S;
+            if (p.logprob) p.logprob[r] = undefined || !has_token ? nan : empty ? -INFINITY : (x_t - M) - log_s;
+            if (p.rank) p.rank[r] = undefined || !has_token ? -1 : pb;
+            sh.m = M;
+            sh.s = S;
+        }
     }
     if (!p.top) return;
+    unsigned long long key = 0;
+    int pos = 32;
     if (C > 1) {
-        // C lists, each in order: the position of a key is the number of keys before it in all lists
-        if (threadIdx.x < 32) sh.best[threadIdx.x] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < C * p.top; i += NT) {
-            const unsigned long long key = sh.top[i / p.top][i % p.top];
-            if (!key) continue;
-            int pos = 0;
-            for (int c = 0; c < C; ++c)
-                for (int j = 0; j < p.top && sh.top[c][j] > key; ++j) ++pos;
-            if (pos < p.top) sh.best[pos] = key;
+        // C lists, each in order: a key's position is the number of keys before it in all lists (found by bisection)
+        if (threadIdx.x >= NT - 32) sh.best[threadIdx.x & 31] = 0;
+        if ((int)threadIdx.x < C * 32) key = sh.top[warp][lane];
+        if (key) {
+            int at[MAX_CLUSTER];
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c) at[c] = 0;
+#pragma unroll
+            for (int step = 16; step > 0; step >>= 1)
+#pragma unroll
+                for (int c = 0; c < MAX_CLUSTER; ++c)
+                    if (c < C && sh.top[c][at[c] + step - 1] > key) at[c] += step;
+            pos = 0;
+#pragma unroll
+            for (int c = 0; c < MAX_CLUSTER; ++c)
+                if (c < C) pos += at[c] + (at[c] == 31 && sh.top[c][31] > key);
         }
         __syncthreads();
+        if (pos < p.top) sh.best[pos] = key;
     }
+    __syncthreads();
     if ((int)threadIdx.x < p.top) {
-        const unsigned long long key = sh.best[threadIdx.x];
-        const bool some = key != 0 && !undefined;
+        key = sh.best[threadIdx.x];
+        const bool undefined = isnan(sh.s), some = key != 0 && !undefined;
         const long long at = r * p.top + threadIdx.x;
         if (p.top_ids) p.top_ids[at] = some ? key_id(key) : -1;
         if (p.top_lp)
-            p.top_lp[at] = undefined ? __int_as_float(0x7fffffff) : some ? (key_value(key) - part.m) - log_s : -INFINITY;
+            p.top_lp[at] = undefined ? __int_as_float(0x7fffffff) : some ? (key_value(key) - sh.m) - logf(sh.s) : -INFINITY;
     }
 }
 
