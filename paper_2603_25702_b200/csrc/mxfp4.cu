@@ -13,6 +13,7 @@ namespace {
 
 constexpr int QT = 256;              // threads of the element-wise kernels
 constexpr int QUAD = 128;            // elements under one 32-bit word of scale bytes: 4 blocks, 16 threads x 8 elements
+constexpr int QROWS = QT / 32;       // rows of a block
 
 struct QuantParams {
     const void* x;                   // quantise: input;  dequantise: output
@@ -29,26 +30,42 @@ __host__ __device__ __forceinline__ size_t scale_word(long long row, int quad, i
     return ((size_t)(row / 128) * quads + quad) * 512 + (size_t)(row % 32) * 16 + (size_t)(row % 128) / 32 * 4;
 }
 
+// Eight elements from p on, `left` of which exist, as they stand in memory (zeros behind them).
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool vec, long long left, float* v) {
-    if (vec && left >= 8) {
-        if (sizeof(T) == 4) {
-            const float4 a = __ldg((const float4*)p), b = __ldg((const float4*)p + 1);
-            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+struct Eight {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p, bool vec, long long left) {
+        if (vec && left >= 8) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldg((const uint4*)p + i);
         } else {
-            const uint4 a = __ldg((const uint4*)p);
-            const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+            uint32_t u[2 * sizeof(T)];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t f = e < left ? __float_as_uint(to_f32(p[e])) : 0u;
+                if (sizeof(T) == 4) u[e % (2 * sizeof(T))] = f;
+                else u[e / 2] = e & 1 ? u[e / 2] | (f & 0xffff0000u) : f >> 16;
+            }
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+        }
+    }
+    __device__ __forceinline__ void values(float* v) const {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[2 * e] = __uint_as_float(u[e] << 16);
-                v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+                if (sizeof(T) == 4) {
+                    v[4 * i + e] = __uint_as_float(u[e]);
+                } else {
+                    v[2 * e] = __uint_as_float(u[e] << 16);
+                    v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+                }
             }
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < left ? to_f32(p[e]) : 0.f;
     }
-}
+};
 
 // Eight e2m1 codes, element 0 in the lowest nibble: round to nearest, ties to even, saturating.
 __device__ __forceinline__ uint32_t e2m1x8(const float* v) {
@@ -64,24 +81,30 @@ __device__ __forceinline__ uint32_t e2m1x8(const float* v) {
     return r;
 }
 
-// 16 threads per (row, 128 elements): four threads share a block, their largest magnitude as an integer maximum of the
-// absolute bit patterns (infinities and NaN come out on top).  Scale and quotient are exact: the scale is a power of two.
-// Memory bound.  Rows that pad the last scale tile get zeros.
-template <typename T>
+// A warp takes STEPS x 256 elements of a row, all of its loads in flight at once, 16 threads per 128 elements: four threads share a block, their largest magnitude is an
+// integer maximum of the absolute bit patterns (infinities and NaN come out on top).  Scale and quotient are exact: the scale is a
+// power of two.  Memory bound; rows that pad the last scale tile get zeros.
+template <typename T, int STEPS>
 __global__ void __launch_bounds__(QT) quantize_kernel(const QuantParams p) {
     pdl_wait();
     pdl_launch();
-    const long long rows_padded = (p.rows + 127) / 128 * 128, units = rows_padded * p.quads;
-    const int sub = threadIdx.x & 15;
-    const long long stride = (long long)gridDim.x * (QT / 16);
-    for (long long u = (long long)blockIdx.x * (QT / 16) + (threadIdx.x >> 4); u < units; u += stride) {
-        // (units is a multiple of 128: the two half warps, which exchange through shuffles, leave the loop together)
-        const long long row = u / p.quads;
-        const int quad = (int)(u - row * p.quads);
+    const int lane = threadIdx.x & 31, sub = lane & 15;
+    const long long row = (long long)blockIdx.x * QROWS + (threadIdx.x >> 5);
+    const int quad0 = (int)blockIdx.y * (2 * STEPS) + (lane >> 4);
+    const bool inside = row < p.rows;
+    const T* x = (const T*)p.x + (inside ? row * p.ld : 0);
+    Eight<T> in[STEPS];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        const long long c0 = (long long)(quad0 + 2 * i) * QUAD + sub * 8;
+        in[i].load(x + c0, p.vec, inside ? p.cols - c0 : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        const int quad = quad0 + 2 * i;
         const long long c0 = (long long)quad * QUAD + sub * 8;
-        const bool inside = row < p.rows;
         float v[8];
-        load8((const T*)p.x + (inside ? row * p.ld + c0 : 0), p.vec, inside ? p.cols - c0 : 0, v);
+        in[i].values(v);
         uint32_t a = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) a = max(a, __float_as_uint(v[e]) & 0x7fffffffu);
@@ -99,30 +122,39 @@ __global__ void __launch_bounds__(QT) quantize_kernel(const QuantParams p) {
         if (!inside || (long long)quad * QUAD + (sub >> 2) * 32 >= p.cols) word = 0;
         word |= __shfl_xor_sync(0xffffffffu, word, 4);
         word |= __shfl_xor_sync(0xffffffffu, word, 8);
-        if (sub == 0) *(uint32_t*)(p.scales + scale_word(row, quad, p.quads)) = word;
+        if (sub == 0 && quad < p.quads) *(uint32_t*)(p.scales + scale_word(row, quad, p.quads)) = word;
     }
 }
 
-template <typename T>
+template <typename T, int STEPS>
 __global__ void __launch_bounds__(QT) dequantize_kernel(const QuantParams p) {
     pdl_wait();
     pdl_launch();
-    const long long units = p.rows * p.quads;
-    const int sub = threadIdx.x & 15;
-    const long long stride = (long long)gridDim.x * (QT / 16);
-    for (long long u = (long long)blockIdx.x * (QT / 16) + (threadIdx.x >> 4); u < units; u += stride) {
-        const long long row = u / p.quads;
-        const int quad = (int)(u - row * p.quads);
+    const int lane = threadIdx.x & 31, sub = lane & 15;
+    const long long row = (long long)blockIdx.x * QROWS + (threadIdx.x >> 5);
+    const int quad0 = (int)blockIdx.y * (2 * STEPS) + (lane >> 4);
+    if (row >= p.rows) return;
+    uint32_t codes[STEPS], byte[STEPS];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        const int quad = quad0 + 2 * i;
         const long long c0 = (long long)quad * QUAD + sub * 8;
-        if (c0 >= p.cols) continue;
-        const uint32_t codes = __ldg((const uint32_t*)(p.codes + row * p.code_ld + c0 / 2));
-        const uint32_t byte = p.scales[scale_word(row, quad, p.quads) + (sub >> 2)];
-        const float scale = __uint_as_float(byte == 255 ? 0x7fffffffu : byte ? byte << 23 : 0x00400000u);
+        codes[i] = byte[i] = 0;
+        if (c0 < p.cols) {
+            codes[i] = __ldg((const uint32_t*)(p.codes + row * p.code_ld + c0 / 2));
+            byte[i] = __ldg(p.scales + scale_word(row, quad, p.quads) + (sub >> 2));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        const long long c0 = (long long)(quad0 + 2 * i) * QUAD + sub * 8;
+        if (c0 >= p.cols) break;
+        const float scale = __uint_as_float(byte[i] == 255 ? 0x7fffffffu : byte[i] ? byte[i] << 23 : 0x00400000u);
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             // e2m1 as fp32: exponent and mantissa bits moved into place, the offset of the exponent by an exact product
-            const uint32_t c = codes >> (4 * e);
+            const uint32_t c = codes[i] >> (4 * e);
             const float mag = __uint_as_float((c & 7u) << 22) * 0x1p126f;
             v[e] = ((c & 8u) ? -mag : mag) * scale;
         }
@@ -179,11 +211,19 @@ int elementwise(const char* op, bool inverse, const void* x, int dtype, long lon
     p.codes = (uint8_t*)const_cast<void*>(codes);
     p.scales = (uint8_t*)const_cast<void*>(scales);
     p.vec = ((uintptr_t)x & 15) == 0 && (ld * size) % 16 == 0;
-    const long long units = (inverse ? rows : (rows + 127) / 128 * 128) * p.quads;
-    const unsigned grid = (unsigned)std::min<long long>((units + QT / 16 - 1) / (QT / 16), (long long)dev->n_sms * 32);
-    cudaError_t e;
-    if (dtype == S2D2_DTYPE_F32) e = ops::launch(inverse ? dequantize_kernel<float> : quantize_kernel<float>, dim3(grid), QT, 0, 1, st, p);
-    else e = ops::launch(inverse ? dequantize_kernel<bf16> : quantize_kernel<bf16>, dim3(grid), QT, 0, 1, st, p);
+    const long long row_blocks = ((inverse ? rows : (rows + 127) / 128 * 128) + QROWS - 1) / QROWS;      // at most 2^19
+    // four steps per warp once that many blocks fill the GPU (12288 x 4096 bf16: 27.5 us each way, 42 us with one step);
+    // one step for small matrices (333 x 2049 fp32, both ways: 6 us, 11 us with four)
+    const int steps = row_blocks * ((p.quads + 7) / 8) >= 8LL * dev->n_sms ? 4 : 1;
+    const dim3 grid((unsigned)row_blocks, (unsigned)((p.quads + 2 * steps - 1) / (2 * steps)));           // at most 2^12 along y
+    void (*kernel)(QuantParams);
+    if (dtype == S2D2_DTYPE_F32)
+        kernel = inverse ? (steps == 4 ? dequantize_kernel<float, 4> : dequantize_kernel<float, 1>)
+                         : (steps == 4 ? quantize_kernel<float, 4> : quantize_kernel<float, 1>);
+    else
+        kernel = inverse ? (steps == 4 ? dequantize_kernel<bf16, 4> : dequantize_kernel<bf16, 1>)
+                         : (steps == 4 ? quantize_kernel<bf16, 4> : quantize_kernel<bf16, 1>);
+    const cudaError_t e = ops::launch(kernel, grid, QT, 0, 1, st, p);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return ops::fail(S2D2_ERR_CUDA, "%s: %s", op, cudaGetErrorString(e));

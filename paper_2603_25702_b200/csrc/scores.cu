@@ -29,8 +29,8 @@ namespace {
 constexpr int NT = 256;            // threads
 constexpr int NW = NT / 32;
 constexpr int TILE = 16;           // elements of one thread between two rescales
-constexpr int CAP = 1024;          // candidates above the threshold held in shared memory
-constexpr int TIES = 256;          // candidates equal to it
+constexpr int CAP = 1024;          // candidates held in shared memory
+constexpr int MANY_EQUAL = 128;    // threads whose maximum equals the bound: more, and equal elements are taken in id order instead
 constexpr int TILES = 768;         // tiles that may be read again
 constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -153,15 +153,14 @@ struct alignas(16) Partial {       // one CTA's share of a row
 
 struct Shared {
     unsigned long long cand[CAP + 8];
-    unsigned long long tie[TIES + 8];
     unsigned long long top[MAX_CLUSTER][32];     // in the cluster's first CTA: every CTA's best, in order, 0 = none
     unsigned long long best[32];                 // this CTA's best, in order
     Partial part[MAX_CLUSTER * NW];              // in the cluster's first CTA: every warp's sums
     float bound[NW];
     int warp_count[NW];
     int tile[TILES];                             // tiles that are read again
-    int n_cand, n_tie, n_tile;
-    float m, s;
+    int n_cand, n_tile;
+    float m, log_s;
 };
 
 // Position of `key` among the n keys of `list`, which is padded to a multiple of eight with zeros.
@@ -176,6 +175,20 @@ __device__ __forceinline__ int count_above(const unsigned long long* list, int n
         }
     }
     return pos;
+}
+
+// Places for `n` entries of every lane behind *count, taken by the warp at once; the first of this lane's.  Converged warp.
+__device__ __forceinline__ int warp_places(int n, int* count) {
+    const int lane = threadIdx.x & 31;
+    int end = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int w = __shfl_up_sync(0xffffffffu, end, o);
+        if (lane >= o) end += w;
+    }
+    int base = 0;
+    if (lane == 31) base = atomicAdd(count, end);
+    return __shfl_sync(0xffffffffu, base, 31) + end - n;
 }
 
 // Appends, in id order, elements equal to `v` of the vectors [v0, v1) to best[n..], until `k` are there.  Whole CTA.
@@ -255,48 +268,53 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
     }
     if (lane == 0) sh.bound[warp] = bound;
     if (threadIdx.x < 32) best[threadIdx.x] = 0;
-    if (threadIdx.x == 0) sh.n_cand = sh.n_tie = sh.n_tile = 0;
+    if (threadIdx.x == 0) sh.n_cand = sh.n_tile = 0;
     __syncthreads();
     float thr = sh.bound[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) thr = fminf(thr, sh.bound[w]);
-    const bool none_equal = thr == -INFINITY;                     // nothing is drawn from elements that are -inf
-    const bool many_equal = __syncthreads_count(mine == thr) > TIES / 2;
-    const bool equal_too = !none_equal && !many_equal;
-    if (mine > thr || (equal_too && mine == thr)) {
+    // Candidates are the elements from `bar` on: equal ones too, unless there are many of them, or they are -inf (which are never
+    // drawn).
+    const bool many_equal = __syncthreads_count(mine == thr) > MANY_EQUAL && thr > -INFINITY;
+    const float bar = many_equal || thr == -INFINITY ? nextafterf(thr, INFINITY) : thr;
+    // the tiles to read again: each thread marks its own (at most 64), a warp takes places for all of its at once
+    unsigned long long marks = 0;
+    if (mine >= bar) {
 #pragma unroll 4
-        for (int i = 0; i < n_tiles; ++i) {
-            const float tm = tile_max[i * NT + threadIdx.x];
-            if (tm > thr || (equal_too && tm == thr)) {
-                const int at = atomicAdd(&sh.n_tile, 1);
-                if (at < TILES) sh.tile[at] = i * NT + (int)threadIdx.x;
-            }
-        }
+        for (int i = 0; i < n_tiles; ++i) marks |= (unsigned long long)(tile_max[i * NT + threadIdx.x] >= bar) << i;
+    }
+    if (__any_sync(0xffffffffu, marks != 0)) {
+        for (int at = warp_places(__popcll(marks), &sh.n_tile); marks; ++at, marks &= marks - 1)
+            if (at < TILES) sh.tile[at] = (__ffsll(marks) - 1) * NT + (int)threadIdx.x;
     }
     __syncthreads();
     const int n_again = sh.n_tile;
     if (n_again <= TILES) {
-        for (int i = threadIdx.x; i < n_again * VPT; i += NT) {
-            const int which = sh.tile[i / VPT], vec = v0 + (which / NT * VPT + i % VPT) * NT + which % NT;
-            if (vec >= v1) continue;
+        for (int i0 = 0; i0 < n_again * VPT; i0 += NT) {
+            const int i = i0 + (int)threadIdx.x, which = i < n_again * VPT ? sh.tile[i / VPT] : 0;
+            const int vec = v0 + (which / NT * VPT + i % VPT) * NT + which % NT;
             float x[E];
-            row.load(vec, x);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (x[e] > thr) {
-                    const int at = atomicAdd(&sh.n_cand, 1);
-                    if (at < CAP) sh.cand[at] = order_key(x[e], row.first_id(vec) + e);
-                } else if (equal_too && x[e] == thr) {
-                    const int at = atomicAdd(&sh.n_tie, 1);
-                    if (at < TIES) sh.tie[at] = order_key(thr, row.first_id(vec) + e);
-                }
+            for (int e = 0; e < E; ++e) x[e] = -INFINITY;
+            if (i < n_again * VPT && vec < v1) row.load(vec, x);
+            int count = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) count += x[e] >= bar;
+            if (__any_sync(0xffffffffu, count > 0)) {
+                int at = warp_places(count, &sh.n_cand);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (x[e] >= bar) {
+                        if (at < CAP) sh.cand[at] = order_key(x[e], row.first_id(vec) + e);
+                        ++at;
+                    }
             }
         }
     }
     __syncthreads();
-    const int n = sh.n_cand, n_tie = sh.n_tie;
+    const int n = sh.n_cand;
     if (n_again > TILES || n > CAP) {
-        // More elements above the bound than are held here (a few threads own most of the large ones): value by value.
+        // More candidates than are held here (a few threads own most of the large elements): value by value.
         int got = 0;
         float below = INFINITY;
         while (got < k) {
@@ -308,29 +326,15 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
         __syncthreads();
         return;
     }
-    // position of each candidate = how many others come before it; elements equal to the bound follow those above it
-    const bool ties_held = !many_equal && n_tie <= TIES;
-    if (threadIdx.x < 8) {
-        sh.cand[n + threadIdx.x] = 0;
-        if (ties_held) sh.tie[n_tie + threadIdx.x] = 0;
-    }
+    // position of each candidate = how many others come before it
+    if (threadIdx.x < 8) sh.cand[n + threadIdx.x] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += NT) {
         const unsigned long long key = sh.cand[i];
         const int pos = count_above(sh.cand, n, key);
         if (pos < k) best[pos] = key;
     }
-    if (!none_equal && n < k) {
-        if (ties_held) {
-            for (int i = threadIdx.x; i < n_tie; i += NT) {
-                const unsigned long long key = sh.tie[i];
-                const int pos = n + count_above(sh.tie, n_tie, key);
-                if (pos < k) best[pos] = key;
-            }
-        } else {
-            append_equal(row, v0, v1, thr, best, n, k, sh);
-        }
-    }
+    if (many_equal && n < k) append_equal(row, v0, v1, thr, best, n, k, sh);
     __syncthreads();
 }
 
@@ -466,7 +470,7 @@ __global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
         if (lane == 0) sh.part[warp] = part;
         __syncthreads();
     }
-    if (warp == 0) {
+    if (warp == NW - 1) {                        // (the first C warps order the alternatives meanwhile)
         // C * 8 parts, two per lane at most
         float pm = -FLT_MAX, ps = 0.f, pt = 0.f;
         int pb = 0;
@@ -486,21 +490,20 @@ __global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
             if (p.logprob) p.logprob[r] = undefined || !has_token ? nan : empty ? -INFINITY : (x_t - M) - log_s;
             if (p.rank) p.rank[r] = undefined || !has_token ? -1 : pb;
             sh.m = M;
-            sh.s = S;
+            sh.log_s = undefined ? nan : log_s;
         }
     }
     if (!p.top) return;
     unsigned long long key = 0;
-    int pos = 32;
+    int pos = threadIdx.x;
     if (C > 1) {
         // C lists, each in order: a key's position is the number of keys before it in all lists (found by bisection)
-        if (threadIdx.x >= NT - 32) sh.best[threadIdx.x & 31] = 0;
         if ((int)threadIdx.x < C * 32) key = sh.top[warp][lane];
         if (key) {
             int at[MAX_CLUSTER];
 #pragma unroll
             for (int c = 0; c < MAX_CLUSTER; ++c) at[c] = 0;
-#pragma unroll
+#pragma unroll 1
             for (int step = 16; step > 0; step >>= 1)
 #pragma unroll
                 for (int c = 0; c < MAX_CLUSTER; ++c)
@@ -510,17 +513,20 @@ __global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
             for (int c = 0; c < MAX_CLUSTER; ++c)
                 if (c < C) pos += at[c] + (at[c] == 31 && sh.top[c][31] > key);
         }
-        __syncthreads();
-        if (pos < p.top) sh.best[pos] = key;
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < p.top) {
+    } else if ((int)threadIdx.x < p.top) {
         key = sh.best[threadIdx.x];
-        const bool undefined = isnan(sh.s), some = key != 0 && !undefined;
-        const long long at = r * p.top + threadIdx.x;
-        if (p.top_ids) p.top_ids[at] = some ? key_id(key) : -1;
-        if (p.top_lp)
-            p.top_lp[at] = undefined ? __int_as_float(0x7fffffff) : some ? (key_value(key) - sh.m) - logf(sh.s) : -INFINITY;
+    }
+    const int found = __syncthreads_count(key != 0);
+    const float log_s = sh.log_s;                // NaN: undefined row
+    const long long at = r * p.top;
+    if (key && pos < p.top) {
+        if (p.top_ids) p.top_ids[at + pos] = isnan(log_s) ? -1 : key_id(key);
+        if (p.top_lp) p.top_lp[at + pos] = isnan(log_s) ? log_s : (key_value(key) - sh.m) - log_s;
+    }
+    pos = threadIdx.x;
+    if (pos < p.top && pos >= found) {
+        if (p.top_ids) p.top_ids[at + pos] = -1;
+        if (p.top_lp) p.top_lp[at + pos] = isnan(log_s) ? log_s : -INFINITY;
     }
 }
 
@@ -530,9 +536,12 @@ int run(const ops::Device* dev, ScoreParams p, long long rows, cudaStream_t st) 
     // vectors of a row, whatever its alignment
     const int n_vec = (p.V + E - 2) / E + 1;
     const int tiles = (n_vec + VPT * NT - 1) / (VPT * NT);
-    // CTAs per row: enough rows fill the GPU by themselves; fewer rows are cut while a CTA keeps a tile of its own
+    // CTAs per row: rows are cut, while a CTA keeps a tile of its own, until the CTAs are three per SM; and once where that
+    // fills the GPU more evenly than whole rows do.
     int c = 1;
-    while (c < MAX_CLUSTER && c < tiles && (rows * c < 8LL * dev->n_sms || (p.top && (tiles + c - 1) / c > 64))) c *= 2;
+    while (c < MAX_CLUSTER && c < tiles && (rows * c < 3LL * dev->n_sms || (p.top && (tiles + c - 1) / c > 64))) c *= 2;
+    const long long slots = 4LL * dev->n_sms;
+    if (c == 1 && tiles > 8 && rows < 8 * slots) c = 2;
     p.cluster = c;
     p.n_tiles = (tiles + c - 1) / c;
     p.seg_vec = p.n_tiles * VPT * NT;
