@@ -37,7 +37,7 @@ struct Eight {
     __device__ __forceinline__ void load(const T* p, bool vec, long long left) {
         if (vec && left >= 8) {
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldg((const uint4*)p + i);
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldcs((const uint4*)p + i);
         } else {
             uint32_t u[2 * sizeof(T)];
 #pragma unroll
@@ -161,8 +161,8 @@ __global__ void __launch_bounds__(QT) dequantize_kernel(const QuantParams p) {
         T* y = (T*)const_cast<void*>(p.x) + row * p.ld + c0;
         if (p.vec && c0 + 8 <= p.cols) {
             if (sizeof(T) == 4) {
-                ((float4*)y)[0] = make_float4(v[0], v[1], v[2], v[3]);
-                ((float4*)y)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                __stcs((float4*)y, make_float4(v[0], v[1], v[2], v[3]));
+                __stcs((float4*)y + 1, make_float4(v[4], v[5], v[6], v[7]));
             } else {
                 uint32_t w[4];
 #pragma unroll
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(QT) dequantize_kernel(const QuantParams p) {
                     const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
                     w[e] = *reinterpret_cast<const uint32_t*>(&h);
                 }
-                *(uint4*)y = make_uint4(w[0], w[1], w[2], w[3]);
+                __stcs((uint4*)y, make_uint4(w[0], w[1], w[2], w[3]));
             }
         } else {
             for (int e = 0; e < 8; ++e)
@@ -242,7 +242,7 @@ int encode_codes(const ops::Device* dev, CUtensorMap* map, const void* codes, in
     return r == CUDA_SUCCESS ? S2D2_OK : ops::fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
-constexpr int MAX_SMEM = 227 * 1024;
+constexpr int MAX_SMEM = 224 * 1024;     // 3 KB of an SM are left to kernels without tensor memory
 
 int check_operands(const ops::Device* dev, const void* xc, const void* xs, const void* wc, const void* ws) {
     if (int rc = ops::check_ptr(dev, xc, 16, "x_codes")) return rc;

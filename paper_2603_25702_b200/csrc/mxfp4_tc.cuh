@@ -77,9 +77,10 @@ __host__ __device__ __forceinline__ int acc_columns(int T) { return (T + 31) / 3
 __host__ __device__ __forceinline__ int used_columns(int T, int sf_tiles, int n_acc) { return 2 * scale_columns(sf_tiles) + n_acc * acc_columns(T); }
 // Tensor memory is taken with an instruction that waits until enough columns are free.  A CTA of a cluster that waited there for
 // a CTA of another cluster, which waits for its own cluster, could wait for good.  So shared memory is asked for in
-// proportion (57 KB of an SM's 228 KB, 1 KB of it reserved per CTA, for every 128 of its 512 columns): CTAs that fit
-// on an SM by their shared memory also fit by their columns, and nobody ever waits.
-__host__ __device__ __forceinline__ int min_smem(uint32_t cols) { return cols <= 64 ? 28 * 1024 : cols <= 128 ? 56 * 1024 : cols <= 256 ? 113 * 1024 : 227 * 1024; }
+// proportion (57 KB of an SM's 228 KB, 1 KB of it reserved per CTA, for every 128 of its 512 columns; with all columns so much
+// that no other CTA of these kernels fits): CTAs that fit on an SM by their shared memory also fit by their columns, and
+// nobody ever waits.
+__host__ __device__ __forceinline__ int min_smem(uint32_t cols) { return cols <= 64 ? 28 * 1024 : cols <= 128 ? 56 * 1024 : cols <= 256 ? 113 * 1024 : 200 * 1024; }
 
 __device__ __forceinline__ uint64_t desc_sw128(uint32_t smem_addr) {      // K-major rows of 128 bytes, 128-byte swizzle
     return (uint64_t)((smem_addr & 0x3FFFF) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
@@ -544,7 +545,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 }
 
 // Scores from the partial results of a row: one block per row, a thread per part (or several), merged in a fixed order.
-static __global__ void __launch_bounds__(128)
+// Few registers and little shared memory: it waits on the SMs while the product still runs.
+static __global__ void __launch_bounds__(128, 10)
 score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse, float* entropy) {
     __shared__ float4 sh[4];
     pdl_wait();
@@ -553,18 +555,15 @@ score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse
     const float4* parts = p.parts + (size_t)(r / rows_per_tile) * p.ranges * 2 * rows_per_tile + r % rows_per_tile;
     const int token = p.tokens ? p.tokens[r] : -1;
     const bool has_token = token >= 0 && token < p.b_rows;
-    const long long units = (p.b_rows + p.unit - 1) / p.unit;
     float4 a = make_float4(-3.402823466e38f, 0.f, 0.f, 0.f);      // maximum, sum, moment; logit of the token (zero in all parts but one)
     auto add = [&](const float4 b) {
         const float M = fmaxf(a.x, b.x), d1 = fmaxf(a.x - M, -300.f), d2 = fmaxf(b.x - M, -300.f);
         const float f1 = exp2_fast(d1), f2 = exp2_fast(d2);
         a = make_float4(M, f1 * a.y + f2 * b.y, f1 * (a.z + d1 * a.y) + f2 * (b.z + d2 * b.y), a.w + b.w);
     };
+#pragma unroll 4
     for (int i = threadIdx.x; i < 2 * p.ranges; i += 128) {
-        float4 b = parts[(size_t)i * rows_per_tile];
-        const int range = i / 2;
-        if (!has_token || token / p.unit < units * range / p.ranges || token / p.unit >= units * (range + 1) / p.ranges) b.w = 0.f;
-        add(b);
+        add(parts[(size_t)i * rows_per_tile]);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
