@@ -385,8 +385,10 @@ const char* s2d2_noalloc_last_error(void);
  *
  * All pointers with d_ are device (or managed) memory of the current device, owned by the caller; `cuda_stream` is a
  * stream of that device.  The calls are ASYNCHRONOUS, keep nothing between calls, allocate nothing and may be captured
- * into CUDA graphs (make the first call of each on a device outside any capture); calls on different streams may overlap.  They return S2D2_OK or a negative
- * s2d2_status before anything is launched, with the text in s2d2_ops_last_error() (per host thread).
+ * into CUDA graphs; calls on different streams or from different host threads may overlap.  The first call of any of them on a
+ * device loads all of their kernels: make it (s2d2_ops_status will do) outside any capture.  Arguments are checked
+ * before anything is launched; a call returns S2D2_OK or a negative s2d2_status, with the text in s2d2_ops_last_error()
+ * (per host thread).  Outputs must not overlap inputs or one another.
  *
  * MXFP4 (microscaling, block size 32): the elements of a row are cut into blocks of 32; a block has one scale 2^e, held
  * as the byte e + 127 (255: the whole block is NaN), and 32 e2m1 codes (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3,
@@ -397,7 +399,7 @@ const char* s2d2_noalloc_last_error(void);
  *           (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4 of tile (r / 128) * ceil(ceil(cols / 32) / 4) + b / 4.  The tiles are
  *           whole; bytes of rows and blocks that do not exist are zero.  16-byte aligned. */
 #define S2D2_SCORE_MAX_TOP 32
-#define S2D2_SCORE_MAX_VOCAB 2097152
+#define S2D2_SCORE_MAX_VOCAB 2000000
 #define S2D2_MXFP4_MAX_DIM 4194304       /* rows, N and M of an MXFP4 matrix; columns and K: 1048576 */
 
 const char* s2d2_ops_last_error(void);

@@ -2,7 +2,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "common.cuh"
 #include "mxfp4_tc.cuh"
@@ -384,17 +383,9 @@ void plan_score(Plan& plan, int n_sms, int M, int N, int K) {
 }
 
 template <int CG, bool SCORE, int NQ>
-int launch_product(const ops::Device* dev, const Plan& plan, const CUtensorMap* maps, cudaStream_t st) {
-    const auto kernel = mx::product_kernel<CG, SCORE, NQ>;
-    static std::atomic<bool> raised[64];
-    cudaError_t e = cudaSuccess;
-    if (!raised[dev->id].load(std::memory_order_acquire)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
-        if (e == cudaSuccess) raised[dev->id].store(true, std::memory_order_release);
-    }
-    if (e == cudaSuccess)
-        e = ops::launch(kernel, dim3((unsigned)plan.grid), mx::THREADS, plan.smem, CG * plan.p.splits, st, maps[0], maps[1], maps[2], maps[3],
-                        maps[4], plan.p);
+int launch_product(const Plan& plan, const CUtensorMap* maps, cudaStream_t st) {
+    const cudaError_t e = ops::launch(mx::product_kernel<CG, SCORE, NQ>, dim3((unsigned)plan.grid), mx::THREADS, plan.smem,
+                                      CG * plan.p.splits, st, maps[0], maps[1], maps[2], maps[3], maps[4], plan.p);
     if (e == cudaSuccess) return S2D2_OK;
     cudaGetLastError();
     return ops::fail(S2D2_ERR_CUDA, "mxfp4 product: %s", cudaGetErrorString(e));
@@ -413,11 +404,25 @@ int run_product(const ops::Device* dev, Plan& plan, const void* ac, const void* 
     }
     if (int rc = encode_scales(dev, &maps[3], as, p.a_rows, p.K)) return rc;
     if (int rc = encode_scales(dev, &maps[4], bs, p.b_rows, p.K)) return rc;
-    if (plan.cg == 1) return p.T <= 64 ? launch_product<1, SCORE, 1>(dev, plan, maps, st) : launch_product<1, SCORE, 3>(dev, plan, maps, st);
-    return p.T <= 192 ? launch_product<2, SCORE, 3>(dev, plan, maps, st) : launch_product<2, SCORE, 4>(dev, plan, maps, st);
+    if (plan.cg == 1) return p.T <= 64 ? launch_product<1, SCORE, 1>(plan, maps, st) : launch_product<1, SCORE, 3>(plan, maps, st);
+    return p.T <= 192 ? launch_product<2, SCORE, 3>(plan, maps, st) : launch_product<2, SCORE, 4>(plan, maps, st);
 }
 
 }  // namespace
+
+cudaError_t ops::load_mxfp4_kernels() {
+    const cudaError_t all[] = {load(quantize_kernel<float, 1>), load(quantize_kernel<float, 4>), load(quantize_kernel<bf16, 1>),
+                               load(quantize_kernel<bf16, 4>), load(dequantize_kernel<float, 1>), load(dequantize_kernel<float, 4>),
+                               load(dequantize_kernel<bf16, 1>), load(dequantize_kernel<bf16, 4>),
+                               load(mx::product_kernel<1, false, 1>, MAX_SMEM), load(mx::product_kernel<1, false, 3>, MAX_SMEM),
+                               load(mx::product_kernel<2, false, 3>, MAX_SMEM), load(mx::product_kernel<2, false, 4>, MAX_SMEM),
+                               load(mx::product_kernel<1, true, 1>, MAX_SMEM), load(mx::product_kernel<1, true, 3>, MAX_SMEM),
+                               load(mx::product_kernel<2, true, 3>, MAX_SMEM), load(mx::product_kernel<2, true, 4>, MAX_SMEM),
+                               load(mx::score_parts_kernel)};
+    for (cudaError_t e : all)
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
 }  // namespace s2d2
 
 using namespace s2d2;

@@ -51,6 +51,10 @@ int device(const Device** out) {
             if ((e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q)) != cudaSuccess || !fn)
                 return fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
             d.encode = (EncodeTiledFn)fn;
+            if ((e = load_score_kernels()) != cudaSuccess || (e = load_mxfp4_kernels()) != cudaSuccess) {
+                cudaGetLastError();
+                return fail(S2D2_ERR_CUDA, "loading the kernels: %s", cudaGetErrorString(e));
+            }
             g_dev[id] = d;
             g_ready[id].store(true, std::memory_order_release);
         }

@@ -28,8 +28,20 @@ struct Device {
     int* status = nullptr;            // device word a kernel raises when a bounded wait runs out
     EncodeTiledFn encode = nullptr;
 };
-// The current device, set up on first use; S2D2_OK or a failure with its text.
+// The current device, set up on first use; S2D2_OK or a failure with its text.  The set-up loads every kernel of these operators
+// (kernels are otherwise loaded at their first launch, which a stream capture may not allow) and raises its limits.
 int device(const Device** out);
+cudaError_t load_score_kernels();      // scores.cu
+cudaError_t load_mxfp4_kernels();      // mxfp4.cu
+
+// Loads a kernel and allows it `smem` bytes of dynamic shared memory.
+template <typename... P>
+inline cudaError_t load(void (*kernel)(P...), int smem = 0) {
+    cudaFuncAttributes a;
+    cudaError_t e = cudaFuncGetAttributes(&a, kernel);
+    if (e == cudaSuccess && smem) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return e;
+}
 
 // `p` must be device (or managed) memory of the current device, aligned to `align` bytes.
 int check_ptr(const Device* d, const void* p, size_t align, const char* what);

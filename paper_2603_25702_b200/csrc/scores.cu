@@ -18,7 +18,6 @@
 #include <float.h>
 #include <math.h>
 
-#include <atomic>
 
 #include "common.cuh"
 #include "ops_host.h"
@@ -33,8 +32,10 @@ constexpr int CAP = 1024;          // candidates held in shared memory
 constexpr int MANY_EQUAL = 128;    // threads whose maximum equals the bound: more, and equal elements are taken in id order instead
 constexpr int TILES = 768;         // tiles that may be read again
 constexpr int MAX_CLUSTER = 8;
+constexpr int MAX_TILES = 64;      // tiles of a CTA with alternatives: one bit each when they are marked
+static_assert(S2D2_SCORE_MAX_VOCAB + 64 <= MAX_CLUSTER * MAX_TILES * NT * TILE, "a vocabulary fits a cluster's tiles");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int MAX_SMEM = 160 * 1024;   // tile maxima of a CTA's share of the largest vocabulary
+constexpr int MAX_SMEM = MAX_TILES * NT * 4;   // tile maxima
 
 struct ScoreParams {
     const void* x;
@@ -277,7 +278,7 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
     // drawn).
     const bool many_equal = __syncthreads_count(mine == thr) > MANY_EQUAL && thr > -INFINITY;
     const float bar = many_equal || thr == -INFINITY ? nextafterf(thr, INFINITY) : thr;
-    // the tiles to read again: each thread marks its own (at most 64), a warp takes places for all of its at once
+    // the tiles to read again: each thread marks its own (at most MAX_TILES), a warp takes places for all of its at once
     unsigned long long marks = 0;
     if (mine >= bar) {
 #pragma unroll 4
@@ -539,7 +540,7 @@ int run(const ops::Device* dev, ScoreParams p, long long rows, cudaStream_t st) 
     // CTAs per row: rows are cut, while a CTA keeps a tile of its own, until the CTAs are three per SM; and once where that
     // fills the GPU more evenly than whole rows do.
     int c = 1;
-    while (c < MAX_CLUSTER && c < tiles && (rows * c < 3LL * dev->n_sms || (p.top && (tiles + c - 1) / c > 64))) c *= 2;
+    while (c < MAX_CLUSTER && c < tiles && (rows * c < 3LL * dev->n_sms || (p.top && (tiles + c - 1) / c > MAX_TILES))) c *= 2;
     const long long slots = 4LL * dev->n_sms;
     if (c == 1 && tiles > 8 && rows < 8 * slots) c = 2;
     p.cluster = c;
@@ -547,12 +548,6 @@ int run(const ops::Device* dev, ScoreParams p, long long rows, cudaStream_t st) 
     p.seg_vec = p.n_tiles * VPT * NT;
     const size_t smem = p.top ? (size_t)p.n_tiles * NT * 4 : 0;
     if (rows * c > 0x7fffffffLL) return ops::fail(S2D2_ERR_UNSUPPORTED, "score_logits: too many rows");
-    static std::atomic<bool> raised[64];
-    if (!raised[dev->id].load(std::memory_order_acquire)) {
-        cudaError_t e = cudaFuncSetAttribute(score_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SMEM);
-        if (e != cudaSuccess) return ops::fail(S2D2_ERR_CUDA, "score_logits: %s", cudaGetErrorString(e));
-        raised[dev->id].store(true, std::memory_order_release);
-    }
     const cudaError_t e = ops::launch(score_kernel<T>, dim3((unsigned)(rows * c)), NT, smem, c, st, p);
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -562,6 +557,11 @@ int run(const ops::Device* dev, ScoreParams p, long long rows, cudaStream_t st) 
 }
 
 }  // namespace
+
+cudaError_t ops::load_score_kernels() {
+    cudaError_t e = load(score_kernel<float>, MAX_SMEM);
+    return e != cudaSuccess ? e : load(score_kernel<bf16>, MAX_SMEM);
+}
 }  // namespace s2d2
 
 using namespace s2d2;

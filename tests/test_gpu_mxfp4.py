@@ -207,3 +207,80 @@ def test_captured_and_concurrent_calls(s2d2):
             xv = ou.mxfp4_values(*ou.mxfp4_encode(x.double().cpu().numpy()), K)
             err = np.abs(y.double().cpu().numpy() - xv @ wv.T)
             assert (err <= product_tolerance(xv, wv, 1.0, "fp32")).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1000000, 64), (40000, 300, 32), (6, 200, 60000), (5000, 5000, 40)])
+def test_long_axes(s2d2, M, N, K):
+    """Each axis long; a sample of rows and columns is checked."""
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x, w = torch.randn(M, K, generator=g, device="cuda"), torch.randn(N, K, generator=g, device="cuda") * 0.1
+    (xc, xs), (wc, ws) = quantize(s2d2, x, 0), quantize(s2d2, w, 0)
+    y = torch.full((M, N), float("nan"), device="cuda")
+    s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "fp32", M, N, K, stream=stream())
+    s2d2.ops_status(stream())
+    assert torch.isfinite(y).all()
+    r = np.unique(np.r_[0:min(M, 40), M // 2:min(M, M // 2 + 40), max(0, M - 40):M])
+    c = np.unique(np.r_[0:min(N, 150), N // 2:min(N, N // 2 + 150), max(0, N - 150):N])
+    xv = ou.mxfp4_values(*ou.mxfp4_encode(x[r].double().cpu().numpy()), K)
+    wv = ou.mxfp4_values(*ou.mxfp4_encode(w[c].double().cpu().numpy()), K)
+    err = np.abs(y[r][:, c].double().cpu().numpy() - xv @ wv.T)
+    assert (err <= product_tolerance(xv, wv, 1.0, "fp32")).all()
+
+
+def test_rows_further_apart_than_32_bits(s2d2):
+    """Inputs and outputs whose rows lie 2^31 + 8 elements apart: offsets of the last row pass 2^32."""
+    stride, K, N = 2 ** 31 + 8, 200, 130
+    buf = torch.empty(2 * stride + K, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (3, K), (stride, 1))
+    x.copy_(torch.randn(3, K, generator=torch.Generator().manual_seed(1)))
+    codes, scales = quantize(s2d2, x)
+    check_codes(x.double().cpu().numpy(), codes, scales)
+    want = ou.mxfp4_values(*ou.mxfp4_encode(x.double().cpu().numpy()), K)
+    buf.zero_()
+    s2d2.mxfp4_dequantize(codes.data_ptr(), scales.data_ptr(), 3, K, buf.data_ptr(), "bf16", stride, stream())
+    assert np.array_equal(x.double().cpu().numpy(), want)
+    (wc, ws), wv = operand(N, K, 2)
+    y = torch.as_strided(buf, (3, N), (stride, 1))
+    s2d2.mxfp4_gemm(codes.data_ptr(), scales.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "bf16", 3, N, K, stride, stream=stream())
+    s2d2.ops_status(stream())
+    assert (np.abs(y.double().cpu().numpy() - want @ wv.T) <= product_tolerance(want, wv, 1.0, "bf16")).all()
+
+
+FIRST_USE = """
+import sys, torch
+import paper_2603_25702_b200 as s
+torch.cuda.set_device(0)
+st = torch.cuda.Stream()
+M, N, K = 300, 20000, 256
+x, w = torch.randn(M, K, device="cuda"), torch.randn(N, K, device="cuda")
+bufs = [[torch.empty(n, dtype=torch.uint8, device="cuda") for n in s.mxfp4_sizes(*t.shape)] for t in (x, w)]
+y, lse = torch.empty(M, N, device="cuda"), torch.empty(2, M, device="cuda")
+tok = torch.zeros(M, dtype=torch.int32, device="cuda")
+ws = torch.empty(s.mxfp4_score_workspace(M, N, K), dtype=torch.uint8, device="cuda")
+torch.cuda.synchronize()
+with torch.cuda.stream(st):
+    s.ops_status(st.cuda_stream)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        p = [b.data_ptr() for pair in bufs for b in pair]
+        for t, (c, sc) in zip((x, w), bufs):
+            s.mxfp4_quantize(t.data_ptr(), "fp32", t.shape[0], K, K, c.data_ptr(), sc.data_ptr(), st.cuda_stream)
+        s.mxfp4_gemm(*p, y.data_ptr(), "fp32", M, N, K, stream=st.cuda_stream)
+        s.score_logits(y.data_ptr(), "fp32", M, N, N, d_lse=lse[0].data_ptr(), stream=st.cuda_stream)
+        s.mxfp4_score(*p, M, N, K, tok.data_ptr(), ws.data_ptr(), ws.numel(), d_lse=lse[1].data_ptr(), stream=st.cuda_stream)
+    g.replay()
+    s.ops_status(st.cuda_stream)
+want = torch.logsumexp(y.double(), 1)
+assert (lse[0] - want).abs().max() < 1e-3 and (lse[1] - want).abs().max() < 1e-3, (lse, want)
+print("captured first use ok")
+"""
+
+
+def test_first_use_may_be_captured_after_ops_status():
+    """In a fresh process: s2d2_ops_status loads every kernel, then the first launches happen inside a capture."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_USE], cwd=root, capture_output=True, text=True, timeout=240)
+    assert r.returncode == 0 and "captured first use ok" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]

@@ -189,6 +189,52 @@ def test_captured_call_follows_its_inputs(s2d2):
         assert np.abs(lse.cpu().numpy() - want["lse"]).max() <= ou.score_tolerance(20000, want["log_s"]).max() + 2.0 ** -23 * 20
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,V,k", [(2, 2000000, 32), (2, 1999999, 5), (6000, 60, 4), (700, 30000, 8)])
+def test_largest_vocabulary_and_many_rows(s2d2, dtype, rows, V, k):
+    x = logits(rows, V, dtype, V)
+    tokens = np.arange(rows) % V
+    check(run(s2d2, x, tokens, k), x.double().cpu().numpy(), tokens, k)
+
+
+def test_rows_further_apart_than_32_bits(s2d2):
+    """Three rows 2^31 + 5 elements apart: offsets of the last one pass 2^32."""
+    stride, V = 2 ** 31 + 5, 3000
+    buf = torch.empty(2 * stride + V, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (3, V), (stride, 1))
+    x.copy_(logits(3, V, "bf16", 5))
+    check(run(s2d2, x, [5, 6, 7], 4), x.double().cpu().numpy(), [5, 6, 7], 4)
+
+
+def test_concurrent_and_repeated_calls_agree_bit_for_bit(s2d2):
+    jobs = [(logits(r, V, d, r), np.arange(r) % V, k) for r, V, d, k in ((1, 151936, "fp32", 20), (300, 20000, "bf16", 8), (7, 999, "fp32", 3))]
+    alone = [run(s2d2, *j) for j in jobs]
+    outs = []
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for (x, tokens, k), st in zip(jobs, streams):
+        with torch.cuda.stream(st):
+            rows, V = x.shape
+            tok = torch.as_tensor(tokens, dtype=torch.int32).cuda(non_blocking=False)
+            reps = []
+            for _ in range(4):
+                f, i = torch.empty(3, rows, device="cuda"), torch.empty(rows, k + 1, dtype=torch.int32, device="cuda")
+                lp = torch.empty(rows, k, device="cuda")
+                ids = torch.empty(rows, k, dtype=torch.int32, device="cuda")
+                s2d2.score_logits(x.data_ptr(), "fp32" if x.dtype == torch.float32 else "bf16", rows, V, x.stride(0), tok.data_ptr(), k,
+                                  d_logprob=f[0].data_ptr(), d_lse=f[1].data_ptr(), d_entropy=f[2].data_ptr(), d_rank=i.data_ptr(),
+                                  d_top_ids=ids.data_ptr(), d_top_logprobs=lp.data_ptr(), stream=stream())
+                reps.append((f, i, ids, lp, tok))
+            outs.append(reps)
+    torch.cuda.synchronize()
+    for want, reps, (x, _, k) in zip(alone, outs, jobs):
+        rows = x.shape[0]
+        for f, i, ids, lp, _ in reps:
+            assert np.array_equal(f[0].cpu().numpy(), want["logprob"]) and np.array_equal(f[1].cpu().numpy(), want["lse"])
+            assert np.array_equal(f[2].cpu().numpy(), want["entropy"]) and np.array_equal(i.view(-1)[:rows].cpu().numpy(), want["rank"])
+            assert np.array_equal(ids.cpu().numpy(), want["top_ids"]) and np.array_equal(lp.cpu().numpy(), want["top_logprobs"])
+
+
 def test_score_pass_of_an_engine(s2d2):
     """Scores of the draft and the verifier logits of a decode step against the logits themselves."""
     from s2d2_inputs import generate_prompts, generate_weights, get_config
