@@ -217,6 +217,47 @@ __device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float c, fl
         }
 }
 
+// Rows split, split + S, ... of a tile's sum over the S CTAs of a cluster, each with a partial tile [T][128] at `part`.  A warp takes
+// a row at a time, a lane four of its elements, and has eight loads in flight: distant shared memory answers late.
+template <int S>
+__device__ __forceinline__ void sum_parts(const Params& p, uint32_t part, int split, int rows, int b0, int a) {
+    constexpr int AT_ONCE = 8 / S, WARPS = THREADS / 32;
+    const int warp = threadIdx.x >> 5;
+    for (int j0 = warp * AT_ONCE; j0 * S + split < rows; j0 += WARPS * AT_ONCE) {
+        float4 v[AT_ONCE][S];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+            for (int q = 0; q < S; ++q) {
+                const int b = (j0 + j) * S + split;
+                v[j][q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (b < rows)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(v[j][q].x), "=f"(v[j][q].y), "=f"(v[j][q].z), "=f"(v[j][q].w)
+                                 : "r"(cluster_map(part + b * ROWS * 4 + 16 * (threadIdx.x & 31), q))
+                                 : "memory");
+            }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int b = (j0 + j) * S + split;
+            if (b >= rows) break;
+            float4 sum = v[j][0];
+#pragma unroll
+            for (int q = 1; q < S; ++q) {
+                sum.x += v[j][q].x;
+                sum.y += v[j][q].y;
+                sum.z += v[j][q].z;
+                sum.w += v[j][q].w;
+            }
+            const float x[4] = {sum.x, sum.y, sum.z, sum.w};
+            const size_t at = (size_t)(b0 + b) * p.ldy + a;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (a + e < p.a_rows) store_y(p.y, p.y_bf16, at + e, p.scale * x[e]);
+        }
+    }
+}
+
 // One lane of a converged warp.  The warps that feed the tensor core and the copy engine run their loops with all lanes, so
 // that addresses and descriptors stay in uniform registers; only the instruction itself is left to one lane.
 __device__ __forceinline__ bool elect() {
@@ -512,21 +553,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         // sum of the partial tiles over the cluster
         cluster_arrive();
         cluster_wait();
-        if (warp >= 2 && warp < 10) {
-            Tiles u = first_tile<SCORE>(cluster);
-            next_tile<SCORE>(p, u, clusters);
-            const int rows = min(u.rows, p.b_rows - u.b0), row = (warp & 3) * 32 + lane, a = u.a0 * ROWS + row;
-            const uint32_t mine = smem_u32(ring) + 4 * row;
-            for (int b = split + p.splits * ((warp - 2) >> 2); b < rows; b += 2 * p.splits) {
-                float sum = 0.f;
-                for (int q = 0; q < p.splits; ++q) {
-                    float v;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_map(mine + b * ROWS * 4, q)) : "memory");
-                    sum += v;
-                }
-                if (a < p.a_rows) store_y(p.y, p.y_bf16, (size_t)(u.b0 + b) * p.ldy + a, p.scale * sum);
-            }
-        }
+        Tiles u = first_tile<SCORE>(cluster);
+        next_tile<SCORE>(p, u, clusters);
+        const int rows = min(u.rows, p.b_rows - u.b0), a = u.a0 * ROWS + 4 * lane;
+        if (p.splits == 2) sum_parts<2>(p, smem_u32(ring), split, rows, u.b0, a);
+        else if (p.splits == 4) sum_parts<4>(p, smem_u32(ring), split, rows, u.b0, a);
+        else sum_parts<8>(p, smem_u32(ring), split, rows, u.b0, a);
     }
     __syncthreads();
     if (*abort_flag) {
