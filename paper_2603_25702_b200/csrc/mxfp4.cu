@@ -284,7 +284,7 @@ void finish_plan(Plan& plan, long long tiles_per_cluster, int stages_wanted) {
     while ((int)p.tmem_cols < used) p.tmem_cols *= 2;
     const int sbytes = mx::stage_bytes(plan.cg, p.a_box, p.T, p.sf_tiles), fixed = 1024 + (int)sizeof(mx::Control),
               pad = mx::ring_bytes(plan.cg, 0, p.a_box, p.T, p.sf_tiles);
-    // CTAs that share k-blocks may be two to an SM
+    // clusters keep to half an SM's memory, so that the set-up of the next kernel may overlap
     const int room = (p.splits > 1 ? 113 * 1024 : MAX_SMEM) - fixed;
     p.stages = std::max(2, std::min(std::min(mx::MAX_STAGES, (room - pad) / sbytes), stages_wanted));
     p.control_at = std::max(mx::ring_bytes(plan.cg, p.stages, p.a_box, p.T, p.sf_tiles), p.splits > 1 ? p.T * mx::ROWS * 4 : 0);
@@ -335,8 +335,16 @@ void plan_product(Plan& plan, int n_sms, int M, int N, int K) {
     p.b_tiles = ceil_div(M, p.T);
     p.sf_tiles = 1;                            // T = 128, or one tile
     const long long tiles = (long long)p.a_tiles * p.b_tiles;
-    // Few tiles: split k while the CTAs fit side by side (two per SM with narrow tiles) and each keeps at least two k-blocks.
-    while (p.splits < 8 && tiles * p.splits * (p.T <= 64 ? 1 : 2) <= n_sms && p.kb_total >= 4 * p.splits) p.splits *= 2;
+    // Few tiles: the CTAs of a cluster share a tile's k-blocks.  Measured: 0.27 us per k-block in a CTA, and 0.6 us plus 7 ns per
+    // token row (12 ns with eight CTAs) for the sum over the cluster.  (M 1, N 4096, K 4096: 7.7 us unsplit, 5.6 us with four;
+    // M 64: 8.2 and 7.7; M 128, N 1024: 8.8 and 6.8; M 64, N 4096, K 2048 stays unsplit.)  Every cluster has to be at work at once;
+    // eight CTAs of a whole SM each do not fit everywhere.
+    double best = 1e30;
+    for (int s = 1; s <= 8 && s <= p.kb_total; s *= 2) {
+        if (s > 1 && tiles * s * (s == 8 && p.T > 64 ? 4 : 3) > 3 * n_sms) break;
+        const double cost = 0.27 * ceil_div(p.kb_total, s) + (s > 1 ? 0.6 + p.T * (s == 8 ? 0.012 : 0.007) : 0.0);
+        if (cost < best) best = cost, p.splits = s;
+    }
     const int clusters = (int)std::min<long long>(tiles, p.splits > 1 ? tiles : n_sms);
     plan.grid = clusters * p.splits;
     const long long per_cluster = (tiles + clusters - 1) / clusters;
