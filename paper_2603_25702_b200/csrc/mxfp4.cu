@@ -374,7 +374,9 @@ void plan_score(Plan& plan, int n_sms, int M, int N, int K) {
         const int unit = T % 128 ? 64 : 128, units = ceil_div(N, unit);
         if (plan.cg == 1 && T > 192) break;
         const double full = tile_cycles(plan.cg, p.a_box, T, p.kb_total);
-        for (int r = 1; r <= std::min(units, score_max_ranges(p.a_tiles, N)); ++r) {
+        // as many ranges as fill one to four waves of clusters
+        for (int w = ceil_div(p.a_tiles, slots), last = w + 3; w <= last; ++w) {
+            const int r = std::max(1, std::min({(int)((long long)slots * w / p.a_tiles), units, score_max_ranges(p.a_tiles, N)}));
             const int waves = ceil_div((long long)p.a_tiles * r, slots), len = ceil_div(units, r) * unit;
             // a single CTA loads no more of its last tile than the range holds
             const int rest = plan.cg == 1 && len % T ? len % T : T;

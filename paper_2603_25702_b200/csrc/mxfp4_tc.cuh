@@ -20,12 +20,12 @@ namespace mx {
 
 using namespace tc;
 
-constexpr int ROWS = 128;            // weight rows of a tile (MMA M of one CTA)
+constexpr int ROWS = 128;            // A rows of a CTA's tile (MMA M)
 constexpr int KBLOCK = 256;          // elements of a stage's k-block
 constexpr int KBYTES = KBLOCK / 2;
 constexpr int MMA_K = 64;
 constexpr int SF_TILE = 512;         // bytes of one scale tile: 128 rows x 4 blocks
-constexpr int THREADS = 352;        // warps: codes, MMA, eight of the epilogue, scales
+constexpr int THREADS = 352;         // warps: codes, MMA, eight of the epilogue, scales
 constexpr int MAX_STAGES = 12;
 constexpr int CUT = 64;              // B rows of a load of a tile that is cut short
 
@@ -265,6 +265,10 @@ __device__ __forceinline__ bool elect() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
     return e != 0;
 }
+// After a time-out: copies in flight land before anything else uses their shared memory.
+__device__ __forceinline__ void settle() {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+}
 // Position in the ring: stage and the parity of its current use.
 struct Ring {
     int s = 0;
@@ -486,6 +490,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bool ok = !*abort_flag && mbar_wait(&ctl.acc_full[acc], parity, abort_flag);
             if (!ok) *abort_flag = 1;
             ok = __all_sync(0xffffffffu, ok);
+            if (!ok && p.splits > 1) settle();               // the partial tile goes where they land
             tc_fence_after();
             const uint32_t taddr = tmem + d_col + acc * acc_columns(p.T) + col0 + ((uint32_t)(quarter * 32) << 16);
             const int a = t.a0 * CG * ROWS + row0;
@@ -563,7 +568,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __syncthreads();
     if (*abort_flag) {
         if (threadIdx.x == 0) atomicExch(p.status, 1);
-        for (int i = 0; i < 2000; ++i) __nanosleep(1000);       // copies in flight land before shared memory is given back
+        settle();
     }
     tc_fence_before();
     if (cluster_size > 1) {

@@ -409,22 +409,27 @@ __global__ void __launch_bounds__(NT) score_kernel(const ScoreParams p) {
             m = tm;
         }
         const Pair minus_m = pair(-m, -m), log2e = pair(LOG2E, LOG2E);
+        Pair sa[2] = {s2, pair(0.f, 0.f)}, ta[2] = {t2, pair(0.f, 0.f)};
 #pragma unroll
         for (int e = 0; e < TILE; e += 2) {
             const Pair u = (pair(x[e], x[e + 1]) + minus_m) * log2e;
             const float u0 = lo(u), u1 = hi(u);
             // NaN for a NaN, and for +inf (m is +inf then): such a row is reported as NaN
             const Pair ex = pair(exp2_fast(u0), exp2_fast(u1));
-            s2 = s2 + ex;
-            t2 = fma(pair(fmaxf(u0, -300.f), fmaxf(u1, -300.f)), ex, t2);
+            sa[(e >> 1) & 1] = sa[(e >> 1) & 1] + ex;
+            ta[(e >> 1) & 1] = fma(pair(fmaxf(u0, -300.f), fmaxf(u1, -300.f)), ex, ta[(e >> 1) & 1]);
         }
+        s2 = sa[0] + sa[1];
+        t2 = ta[0] + ta[1];
         // tokens that come before the given one: of most tiles not even the largest does
         if (has_token && tm >= x_t) {
             const int vt = v0 + i * VPT * NT + (int)threadIdx.x, i0 = row.first_id(vt), i1 = row.first_id(vt + (VPT - 1) * NT) + E;
             if (i0 >= 0 && (i1 <= token || (i0 > token && vt + (VPT - 1) * NT < v1))) {
                 const float bar = i1 <= token ? x_t : x_next;      // (behind the row's end lie elements read as -inf: never >= x_next)
+                int c[4] = {0, 0, 0, 0};
 #pragma unroll
-                for (int e = 0; e < TILE; ++e) before += x[e] >= bar;
+                for (int e = 0; e < TILE; ++e) c[e & 3] += x[e] >= bar;
+                before += (c[0] + c[1]) + (c[2] + c[3]);
             } else {
 #pragma unroll
                 for (int j = 0; j < VPT; ++j) {
