@@ -237,8 +237,8 @@ int elementwise(const char* op, bool inverse, const void* x, int dtype, long lon
     p.scales = (uint8_t*)const_cast<void*>(scales);
     p.vec = ((uintptr_t)x & 15) == 0 && (ld * size) % 16 == 0;
     const long long row_blocks = ((inverse ? rows : (rows + 127) / 128 * 128) + QROWS - 1) / QROWS;      // at most 2^19
-    // four steps per warp once that many blocks fill the GPU (12288 x 4096 bf16: 27.5 us each way, 42 us with one step);
-    // one step for small matrices (333 x 2049 fp32, both ways: 6 us, 11 us with four)
+    // four steps per warp once that many blocks fill the GPU (12288 x 4096 bf16: 20 us each way);
+    // one step for small matrices (333 x 2049 fp32, both ways: 8 us, 11 us with four)
     const int steps = row_blocks * ((p.quads + 7) / 8) >= 8LL * dev->n_sms ? 4 : 1;
     const dim3 grid((unsigned)row_blocks, (unsigned)((p.quads + 2 * steps - 1) / (2 * steps)));           // at most 2^12 along y
     void (*kernel)(QuantParams);

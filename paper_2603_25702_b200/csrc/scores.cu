@@ -13,6 +13,9 @@
 // largest element.  So only tiles whose maximum reaches the least of the warps' ceil(k / 8)-th largest thread maxima are read
 // again (two to three tiles of 16 elements per alternative), and only elements that reach it are ordered.
 //
+// Bound by HBM for the sums (1024 x 157184 fp32: 100 us, 6.4 TB/s; 117 us with five alternatives and ranks); for 16-bit logits
+// instructions weigh as much (256 x 151936: 20 us of which 12 are the bytes'). One row of 151936 takes 4 us, 9 with 20 alternatives.
+//
 // A row is shared by a cluster of 1, 2, 4 or 8 CTAs, so that a few rows fill the GPU; partial results meet in the shared memory
 // of the cluster's first CTA.  Nothing is kept in global memory, no atomics on it, no workspace.
 #include <float.h>
@@ -542,8 +545,9 @@ int run(const ops::Device* dev, ScoreParams p, long long rows, cudaStream_t st) 
     // vectors of a row, whatever its alignment
     const int n_vec = (p.V + E - 2) / E + 1;
     const int tiles = (n_vec + VPT * NT - 1) / (VPT * NT);
-    // CTAs per row: rows are cut, while a CTA keeps a tile of its own, until the CTAs are three per SM; and once where that
-    // fills the GPU more evenly than whole rows do.
+    // CTAs per row: rows are cut, while a CTA keeps a tile of its own, until the CTAs are three per SM (256 rows of 151936 bf16: 29 us with
+    // two, 35 with four, 44 with eight; one row: 8.7 us with eight, 21 with one).  Long rows that would fill only a few rounds of
+    // the four CTAs an SM holds are cut once all the same (1024 rows of 157184 fp32: 117 us, 134 uncut).
     int c = 1;
     while (c < MAX_CLUSTER && c < tiles && (rows * c < 3LL * dev->n_sms || (p.top && (tiles + c - 1) / c > MAX_TILES))) c *= 2;
     const long long slots = 4LL * dev->n_sms;
