@@ -31,6 +31,21 @@ def test_sizes(s2d2):
     refused(s2d2, -1, "columns", s2d2.mxfp4_sizes, 1, 0)
 
 
+def test_sizes_agree_with_the_library(s2d2):
+    """The binding computes sizes inside the limits itself; the library's entry point gives the same, and the refusals."""
+    import ctypes as C
+    from paper_2603_25702_b200.binding import load_library
+    lib = load_library()
+    rng = np.random.default_rng(0)
+    shapes = [(0, 1), (4194304, 1048576)] + [(int(r), int(c)) for r, c in np.exp(rng.uniform(0, 13, (200, 2)))]
+    for rows, cols in shapes:
+        a, b = C.c_int64(), C.c_int64()
+        assert lib.s2d2_mxfp4_sizes(rows, cols, C.byref(a), C.byref(b)) == 0
+        assert s2d2.mxfp4_sizes(rows, cols) == (a.value, b.value), (rows, cols)
+    refused(s2d2, -1, "rows", s2d2.mxfp4_sizes, 4194305, 1)
+    refused(s2d2, -1, "columns", s2d2.mxfp4_sizes, 1, 1048577)
+
+
 def test_quantize_refusals(s2d2):
     q, d = s2d2.mxfp4_quantize, s2d2.mxfp4_dequantize
     refused(s2d2, -1, "dtype", q, P, "fp16", 1, 32, 32, P, P)
