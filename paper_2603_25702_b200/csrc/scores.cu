@@ -263,9 +263,10 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
     constexpr int E = Row<T>::E, VPT = TILE / E;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned long long* best = sh.best;
-    // the warp's ceil(k / 8)-th largest thread maximum
+    // Of the warps whose threads all have elements (in a short row not all eight), the ceil(k / warps)-th largest thread maximum
+    const int active = min(NW, max(1, (v1 - v0) / 32));
     float rest = mine, bound = -INFINITY;
-    for (int i = 0; i < (k + NW - 1) / NW; ++i) {
+    for (int i = 0; i < (k + active - 1) / active; ++i) {
         bound = warp_max(rest);
         const unsigned who = __ballot_sync(0xffffffffu, rest == bound);
         if (lane == __ffs(who) - 1) rest = -INFINITY;
@@ -276,7 +277,8 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
     __syncthreads();
     float thr = sh.bound[0];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) thr = fminf(thr, sh.bound[w]);
+    for (int w = 1; w < NW; ++w)
+        if (w < active) thr = fminf(thr, sh.bound[w]);
     // Candidates are the elements from `bar` on: equal ones too, unless there are many of them, or they are -inf (which are never
     // drawn).
     const bool many_equal = __syncthreads_count(mine == thr) > MANY_EQUAL && thr > -INFINITY;
@@ -316,7 +318,7 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
         }
     }
     __syncthreads();
-    const int n = sh.n_cand;
+    int n = sh.n_cand;
     if (n_again > TILES || n > CAP) {
         // More candidates than are held here (a few threads own most of the large elements): value by value.
         int got = 0;
@@ -329,6 +331,36 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
         }
         __syncthreads();
         return;
+    }
+    if (n > NT) {
+        // A weak bound (a mask that leaves some warps nothing): the same again on the values of the candidates.
+        unsigned long long mine_too[CAP / NT];
+        unsigned top = 0;
+#pragma unroll
+        for (int j = 0; j < CAP / NT; ++j) {
+            const int i = (int)threadIdx.x + j * NT;
+            mine_too[j] = i < n ? sh.cand[i] : 0;
+            top = max(top, (unsigned)(mine_too[j] >> 32));
+        }
+        unsigned left = top, least = 0;
+        for (int i = 0; i < (k + NW - 1) / NW; ++i) {
+            least = __reduce_max_sync(0xffffffffu, left);
+            if (lane == __ffs(__ballot_sync(0xffffffffu, left == least)) - 1) left = 0;
+        }
+        if (lane == 0) sh.warp_count[warp] = (int)least;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) least = min(least, (unsigned)sh.warp_count[w]);
+        if (threadIdx.x == 0) sh.n_cand = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < CAP / NT; ++j) {
+            const bool in = mine_too[j] != 0 && (unsigned)(mine_too[j] >> 32) >= least;
+            const int at = warp_places(in, &sh.n_cand);
+            if (in) sh.cand[at] = mine_too[j];
+        }
+        __syncthreads();
+        n = sh.n_cand;
     }
     // position of each candidate = how many others come before it
     if (threadIdx.x < 8) sh.cand[n + threadIdx.x] = 0;

@@ -137,6 +137,22 @@ def test_orders_that_defeat_the_threshold(s2d2, kind, rows):
     check(run(s2d2, x.contiguous(), tokens, 20), x.double().cpu().numpy(), tokens, 20)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,left,k", [(151936, 700, 20), (151936, 300, 32), (60000, 1100, 8), (60000, 5000, 5), (670, 670, 8), (1081, 1081, 20),
+                                      (257, 257, 32), (40, 40, 32), (5000, 513, 1)])
+def test_masks_that_leave_a_stretch_and_short_rows(s2d2, dtype, V, left, k):
+    """Only some warps see logits: rows shorter than a tile, masks that leave a stretch of ids (also of equal values)."""
+    x = logits(4, V, dtype, V + k).clone()
+    x[1] = torch.round(x[1])
+    x[2] = torch.round(x[2] / 4)
+    for r, at in enumerate((0, V // 3, V - left, (V - left) // 2)):
+        keep = x[r, at:at + left].clone()
+        x[r] = float("-inf")
+        x[r, at:at + left][:keep.numel()] = keep[:x[r, at:at + left].numel()]
+    tokens = [0, V // 3, V - 1, 7]
+    check(run(s2d2, x, tokens, k), x.double().cpu().numpy(), tokens, k)
+
+
 def test_extreme_logits(s2d2):
     """Differences that underflow, a certain token, values near the type's ends."""
     x = torch.zeros(5, 5000, device="cuda")
