@@ -169,8 +169,10 @@ __device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, uint32_t (&r)[32
         : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Release at CTA scope: what it orders are the reads of tensor memory in front of the fence.  At cluster scope it would wait for all
+// stores of the warp (the output of the tile before), too.
 __device__ __forceinline__ void arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void store_y(void* y, int y_bf16, size_t at, float v) {
     if (y_bf16) reinterpret_cast<bf16*>(y)[at] = __float2bfloat16_rn(v);
@@ -197,23 +199,58 @@ __device__ __forceinline__ float exp2_fast(float x) {      // relative error 2^-
     return y;
 }
 
-// Folds up to 32 logits (accumulators times c, base 2) into a running maximum, sum and moment.
+// Folds up to 32 logits (accumulators times c, base 2) into a running maximum, sums and moments; even and odd columns apart.
+struct Sums {
+    float m;
+    float2 s, mo;
+};
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {      // two operations in one instruction
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
 template <bool FULL>
-__device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float c, float& m, float& s, float& mo) {
-    float top = m;
+__device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float c, Sums& a) {
+    float top = a.m;
+    if (FULL) {
+        // the largest product comes from the largest accumulator, or with a negative factor from the smallest
+        float high = __uint_as_float(v[0]), low = high;
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-        if (FULL || j < n) top = fmaxf(top, __uint_as_float(v[j]) * c);
-    const float dm = fmaxf(m - top, -300.f), f = exp2_fast(dm);
-    mo = f * (mo + dm * s);
-    s *= f;
-    m = top;
+        for (int j = 1; j < 31; j += 2) {
+            asm("max.f32 %0, %0, %1, %2;" : "+f"(high) : "f"(__uint_as_float(v[j])), "f"(__uint_as_float(v[j + 1])));
+            asm("min.f32 %0, %0, %1, %2;" : "+f"(low) : "f"(__uint_as_float(v[j])), "f"(__uint_as_float(v[j + 1])));
+        }
+        high = fmaxf(high, __uint_as_float(v[31]));
+        low = fminf(low, __uint_as_float(v[31]));
+        top = fmaxf(top, fmaxf(high * c, low * c));
+    } else {
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < 32; ++j)
+            if (j < n) top = fmaxf(top, __uint_as_float(v[j]) * c);
+    }
+    const float dm = fmaxf(a.m - top, -300.f), f = exp2_fast(dm);
+    const float2 zero = make_float2(0.f, 0.f), ff = make_float2(f, f);
+    a.mo = fma2(ff, fma2(make_float2(dm, dm), a.s, a.mo), zero);
+    a.s = fma2(ff, a.s, zero);
+    a.m = top;
+    const float2 cc = make_float2(c, c), minus_m = make_float2(-top, -top);
+#pragma unroll
+    for (int j = 0; j < 32; j += 2)
         if (FULL || j < n) {
-            const float u = fmaf(__uint_as_float(v[j]), c, -m), e = exp2_fast(u);
-            s += e;
-            mo += u * e;
+            float2 u = fma2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, minus_m);
+            float2 e = make_float2(exp2_fast(u.x), exp2_fast(u.y));
+            if (!FULL && j + 1 >= n) u.y = e.y = 0.f;
+            a.s = add2(a.s, e);
+            a.mo = fma2(u, e, a.mo);
         }
 }
 
@@ -485,7 +522,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         int acc = 0;
         uint32_t parity = 0;
         // scores
-        float m = 0.f, s = 0.f, mo = 0.f, x_t = 0.f;
+        Sums sums = {0.f, {0.f, 0.f}, {0.f, 0.f}};
+        float x_t = 0.f;
         int token = -1;
         const float c2 = p.scale * 1.4426950408889634f;
         if (SCORE) pdl_wait();
@@ -532,15 +570,15 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 }
             } else {
                 if (t.first) {
-                    m = -3.402823466e38f;
-                    s = mo = x_t = 0.f;
+                    sums = Sums{-3.402823466e38f, {0.f, 0.f}, {0.f, 0.f}};
+                    x_t = 0.f;
                     token = p.tokens && a < p.a_rows ? p.tokens[a] : -1;
                 }
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
                     if (!any || q * 32 >= cols) break;
-                    if (cols - q * 32 >= 32) fold<true>(v[q], 32, c2, m, s, mo);
-                    else fold<false>(v[q], cols - q * 32, c2, m, s, mo);
+                    if (cols - q * 32 >= 32) fold<true>(v[q], 32, c2, sums);
+                    else fold<false>(v[q], cols - q * 32, c2, sums);
                     const int at = token - (t.b0 + col0 + q * 32);
                     if (at >= 0 && at < 32) {
 #pragma unroll
@@ -548,10 +586,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             if (j == at) x_t = __uint_as_float(v[q][j]) * c2;
                     }
                 }
-                if (!ok) s = nan;
+                if (!ok) sums.s.x = nan;
                 if (t.last && a < p.a_rows) {
                     const int range = (t.item - clusters) / p.a_tiles;
-                    p.parts[(((size_t)t.a0 * p.ranges + range) * 2 + half) * (ROWS * CG) + row0] = make_float4(m, s, mo, x_t);
+                    p.parts[(((size_t)t.a0 * p.ranges + range) * 2 + half) * (ROWS * CG) + row0] = make_float4(sums.m, sums.s.x + sums.s.y, sums.mo.x + sums.mo.y, x_t);
                 }
             }
         }
