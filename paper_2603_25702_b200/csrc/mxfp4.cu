@@ -31,25 +31,21 @@ __host__ __device__ __forceinline__ size_t scale_word(long long row, int quad, i
     return ((size_t)(row / 128) * quads + quad) * 512 + (size_t)(row % 32) * 16 + (size_t)(row % 128) / 32 * 4;
 }
 
-// Eight elements from p on, `left` of which exist, as they stand in memory (zeros behind them).
+// Eight elements as they stand in memory, 16-byte aligned.
 template <typename T>
 struct Eight {
     uint4 w[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* p, bool vec, int left) {
-        if (vec && left >= 8) {
+    __device__ __forceinline__ void load_stream(const T* p) {
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldcs((const uint4*)p + i);
-        } else {
-            uint32_t u[2 * sizeof(T)];
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldcs((const uint4*)p + i);
+    }
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t f = e < left ? __float_as_uint(to_f32(p[e])) : 0u;
-                if (sizeof(T) == 4) u[e % (2 * sizeof(T))] = f;
-                else u[e / 2] = e & 1 ? u[e / 2] | (f & 0xffff0000u) : f >> 16;
-            }
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void load_shared(const T* p) {
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
-        }
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = *((const uint4*)p + i);
     }
     __device__ __forceinline__ void values(float* v) const {
 #pragma unroll
@@ -113,10 +109,13 @@ __device__ __forceinline__ void e2m1x8_values(uint32_t codes, float* v) {
 
 // A warp takes STEPS x 256 elements of a row, all of its loads in flight at once, 16 threads per 128 elements: four threads share
 // a block.  Scale and quotient are exact: the scale is a power of two.  Should be memory bound; what it has to watch is the
-// number of instructions (15 per element took 31 us for 12288 x 4096 bf16, about 7 take the time of the copy).  Rows that pad
-// the last scale tile get zeros.
-template <typename T, int STEPS>
+// number of instructions (15 per element took 31 us for 12288 x 4096 bf16, about 7 take the time of the copy).  Rows that are not
+// aligned to 16 bytes, and a row's end, go through shared memory: 32 consecutive elements per load (loads of each thread's own eight
+// took three times as long).  Rows that pad the last scale tile get zeros.
+// WHOLE: every warp's elements are whole and aligned (the other path costs registers: 42 us instead of 39).
+template <typename T, int STEPS, bool WHOLE>
 __global__ void __launch_bounds__(QT) quantize_kernel(const QuantParams p) {
+    __shared__ alignas(16) T staged[WHOLE ? 1 : QROWS][2 * QUAD];
     pdl_wait();
     pdl_launch();
     const int lane = threadIdx.x & 31, sub = lane & 15;
@@ -124,14 +123,40 @@ __global__ void __launch_bounds__(QT) quantize_kernel(const QuantParams p) {
     const int quad0 = (int)blockIdx.y * (2 * STEPS) + (lane >> 4), c0 = quad0 * QUAD + sub * 8;
     const bool inside = row < p.rows;
     const int left = inside ? p.cols - c0 : -(1 << 24);                 // elements from c0 on; none in a row that pads the tile
-    const T* x = (const T*)p.x + (inside ? row * p.ld : 0) + c0;
+    const int w0 = (int)blockIdx.y * (2 * STEPS) * QUAD;            // first element of the warp
+    const T* x = (const T*)p.x + (inside ? row * p.ld : 0) + w0;
+    const int n = inside ? p.cols - w0 : 0;                         // elements of the row from there on
+    // whole and aligned, or element by element: lane, lane + 32, ...
+    const bool direct = WHOLE || (p.vec && n >= STEPS * 2 * QUAD);
     Eight<T> in[STEPS];
+    T one[STEPS][8];
+    if (direct) {
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) in[i].load(x + i * (2 * QUAD), p.vec, left - i * (2 * QUAD));
+        for (int i = 0; i < STEPS; ++i) {
+            if (inside) in[i].load_stream(x + i * (2 * QUAD) + lane * 8);
+            else in[i].clear();
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int e = i * (2 * QUAD) + j * 32 + lane;
+                one[i][j] = e < n ? __ldcs(x + e) : from_f32<T>(0.f);
+            }
+    }
     uint32_t* codes = (uint32_t*)(p.codes + (inside ? row * p.code_ld : 0) + c0 / 2);
     uint32_t* scales = (uint32_t*)(p.scales + scale_word(row, quad0, p.quads));
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
+        if (!direct) {
+            T* stage = (T*)staged[threadIdx.x >> 5];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) stage[j * 32 + lane] = one[i][j];
+            __syncwarp();
+            in[i].load_shared(stage + lane * 8);
+            __syncwarp();
+        }
         float v[8];
         in[i].values(v);
         float m = max_magnitude(v[0], v[1], v[2]);
@@ -158,6 +183,7 @@ __global__ void __launch_bounds__(QT) quantize_kernel(const QuantParams p) {
 
 template <typename T, int STEPS>
 __global__ void __launch_bounds__(QT) dequantize_kernel(const QuantParams p) {
+    __shared__ alignas(16) T staged[QROWS][2 * QUAD];
     pdl_wait();
     pdl_launch();
     const int lane = threadIdx.x & 31, sub = lane & 15;
@@ -173,33 +199,41 @@ __global__ void __launch_bounds__(QT) dequantize_kernel(const QuantParams p) {
         codes[i] = some ? __ldcs(in + i * QUAD / 4) : 0u;
         byte[i] = some ? __ldg(scales + i * 2 * 512) : 0u;
     }
-    T* y = (T*)const_cast<void*>(p.x) + row * p.ld + c0;
+    const int w0 = (int)blockIdx.y * (2 * STEPS) * QUAD, n = p.cols - w0;
+    const bool direct = p.vec && n >= STEPS * 2 * QUAD;             // whole and aligned; else through shared memory, 32 elements per store
+    T* y = (T*)const_cast<void*>(p.x) + row * p.ld + w0;
 #pragma unroll
     for (int i = 0; i < STEPS; ++i, y += 2 * QUAD) {
-        const int n = left - i * (2 * QUAD);
-        if (n <= 0) break;
         const float scale = __uint_as_float(byte[i] == 255 ? 0x7fffffffu : byte[i] ? byte[i] << 23 : 0x00400000u);
         float v[8];
         e2m1x8_values(codes[i], v);
 #pragma unroll
         for (int e = 0; e < 8; e += 2) mul2(v[e], v[e + 1], scale);
-        if (p.vec && n >= 8) {
-            if (sizeof(T) == 4) {
-                __stcs((float4*)y, make_float4(v[0], v[1], v[2], v[3]));
-                __stcs((float4*)y + 1, make_float4(v[4], v[5], v[6], v[7]));
-            } else {
-                uint32_t w[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-                    w[e] = *reinterpret_cast<const uint32_t*>(&h);
-                }
-                __stcs((uint4*)y, make_uint4(w[0], w[1], w[2], w[3]));
-            }
+        uint4 w[sizeof(T) / 2];
+        if (sizeof(T) == 4) {
+            w[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            w[sizeof(T) / 2 - 1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
         } else {
+            uint32_t h[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < n) y[e] = from_f32<T>(v[e]);
+            for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+                h[e] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+            w[0] = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+        if (direct) {
+#pragma unroll
+            for (int j = 0; j < (int)sizeof(T) / 2; ++j) __stcs((uint4*)(y + lane * 8) + j, w[j]);
+        } else {
+            T* stage = (T*)staged[threadIdx.x >> 5];
+#pragma unroll
+            for (int j = 0; j < (int)sizeof(T) / 2; ++j) *((uint4*)(stage + lane * 8) + j) = w[j];
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i * (2 * QUAD) + j * 32 + lane < n) __stcs(y + j * 32 + lane, stage[j * 32 + lane]);
+            __syncwarp();
         }
     }
 }
@@ -241,13 +275,16 @@ int elementwise(const char* op, bool inverse, const void* x, int dtype, long lon
     // one step for small matrices (333 x 2049 fp32, both ways: 8 us, 11 us with four)
     const int steps = row_blocks * ((p.quads + 7) / 8) >= 8LL * dev->n_sms ? 4 : 1;
     const dim3 grid((unsigned)row_blocks, (unsigned)((p.quads + 2 * steps - 1) / (2 * steps)));           // at most 2^12 along y
+    const bool whole = p.vec && cols % (steps * 2 * QUAD) == 0;
     void (*kernel)(QuantParams);
     if (dtype == S2D2_DTYPE_F32)
-        kernel = inverse ? (steps == 4 ? dequantize_kernel<float, 4> : dequantize_kernel<float, 1>)
-                         : (steps == 4 ? quantize_kernel<float, 4> : quantize_kernel<float, 1>);
+        kernel = inverse      ? (steps == 4 ? dequantize_kernel<float, 4> : dequantize_kernel<float, 1>)
+                 : steps == 4 ? (whole ? quantize_kernel<float, 4, true> : quantize_kernel<float, 4, false>)
+                              : (whole ? quantize_kernel<float, 1, true> : quantize_kernel<float, 1, false>);
     else
-        kernel = inverse ? (steps == 4 ? dequantize_kernel<bf16, 4> : dequantize_kernel<bf16, 1>)
-                         : (steps == 4 ? quantize_kernel<bf16, 4> : quantize_kernel<bf16, 1>);
+        kernel = inverse      ? (steps == 4 ? dequantize_kernel<bf16, 4> : dequantize_kernel<bf16, 1>)
+                 : steps == 4 ? (whole ? quantize_kernel<bf16, 4, true> : quantize_kernel<bf16, 4, false>)
+                              : (whole ? quantize_kernel<bf16, 1, true> : quantize_kernel<bf16, 1, false>);
     const cudaError_t e = ops::launch(kernel, grid, QT, 0, 1, st, p);
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -447,8 +484,9 @@ int run_product(const ops::Device* dev, Plan& plan, const void* ac, const void* 
 }  // namespace
 
 cudaError_t ops::load_mxfp4_kernels() {
-    const cudaError_t all[] = {load(quantize_kernel<float, 1>), load(quantize_kernel<float, 4>), load(quantize_kernel<bf16, 1>),
-                               load(quantize_kernel<bf16, 4>), load(dequantize_kernel<float, 1>), load(dequantize_kernel<float, 4>),
+    const cudaError_t all[] = {load(quantize_kernel<float, 1, false>), load(quantize_kernel<float, 4, false>), load(quantize_kernel<bf16, 1, false>),
+                               load(quantize_kernel<bf16, 4, false>), load(quantize_kernel<float, 1, true>), load(quantize_kernel<float, 4, true>),
+                               load(quantize_kernel<bf16, 1, true>), load(quantize_kernel<bf16, 4, true>), load(dequantize_kernel<float, 1>), load(dequantize_kernel<float, 4>),
                                load(dequantize_kernel<bf16, 1>), load(dequantize_kernel<bf16, 4>),
                                load(mx::product_kernel<1, false, 1>, MAX_SMEM), load(mx::product_kernel<1, false, 3>, MAX_SMEM),
                                load(mx::product_kernel<2, false, 3>, MAX_SMEM), load(mx::product_kernel<2, false, 4>, MAX_SMEM),
