@@ -281,7 +281,7 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
         if (w < active) thr = fminf(thr, sh.bound[w]);
     // Candidates are the elements from `bar` on: equal ones too, unless there are many of them, or they are -inf (which are never
     // drawn).
-    const bool many_equal = __syncthreads_count(mine == thr) > MANY_EQUAL && thr > -INFINITY;
+    bool many_equal = __syncthreads_count(mine == thr) > MANY_EQUAL && thr > -INFINITY;
     const float bar = many_equal || thr == -INFINITY ? nextafterf(thr, INFINITY) : thr;
     // the tiles to read again: each thread marks its own (at most MAX_TILES), a warp takes places for all of its at once
     unsigned long long marks = 0;
@@ -352,10 +352,17 @@ __device__ void best_of_segment(const Row<T>& row, int v0, int v1, int n_tiles, 
 #pragma unroll
         for (int w = 0; w < NW; ++w) least = min(least, (unsigned)sh.warp_count[w]);
         if (threadIdx.x == 0) sh.n_cand = 0;
-        __syncthreads();
+        int reach = 0;
+#pragma unroll
+        for (int j = 0; j < CAP / NT; ++j) reach += __syncthreads_count(mine_too[j] != 0 && (unsigned)(mine_too[j] >> 32) >= least);
+        if (reach > NT) {                        // mostly equal ones: they are taken in id order
+            many_equal = true;
+            thr = key_value((unsigned long long)least << 32);
+        }
 #pragma unroll
         for (int j = 0; j < CAP / NT; ++j) {
-            const bool in = mine_too[j] != 0 && (unsigned)(mine_too[j] >> 32) >= least;
+            const unsigned value = (unsigned)(mine_too[j] >> 32);
+            const bool in = mine_too[j] != 0 && (reach > NT ? value > least : value >= least);
             const int at = warp_places(in, &sh.n_cand);
             if (in) sh.cand[at] = mine_too[j];
         }

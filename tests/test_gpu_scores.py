@@ -151,6 +151,8 @@ def test_masks_that_leave_a_stretch_and_short_rows(s2d2, dtype, V, left, k):
         x[r, at:at + left][:keep.numel()] = keep[:x[r, at:at + left].numel()]
     tokens = [0, V // 3, V - 1, 7]
     check(run(s2d2, x, tokens, k), x.double().cpu().numpy(), tokens, k)
+    x[torch.isneginf(x)] = LOWEST[dtype]                             # the same with the type's lowest value: hundreds of equal logits
+    check(run(s2d2, x, tokens, k), x.double().cpu().numpy(), tokens, k)
 
 
 def test_extreme_logits(s2d2):
