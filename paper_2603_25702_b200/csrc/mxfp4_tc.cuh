@@ -372,9 +372,9 @@ __device__ __forceinline__ bool next_tile(const Params& p, Tiles& t, int cluster
 // With few tiles the CTAs of a cluster (p.splits) share the k-blocks of one tile; the partial tiles meet in distributed
 // shared memory, where every CTA sums its share of the rows over the cluster in rank order: deterministic, no
 // workspace, no tickets, nothing that two launches could share.
-// Measured (B200): a head of 151936 x 4096 against 8 rows 57 us (330 MB at 5.8 TB/s); 1024 x 24576 x 4096 46 us (4.5 PFLOP/s; in a long
-// loop, with the quantisation of the rows, 57 us, 62 with T = 192, 72 with T = 128); scores of 1024 rows against the head 243 us
-// (5.2 PFLOP/s; 4.3 in a long loop, at the power limit).
+// Measured (B200): a head of 151936 x 4096 against 8 rows 57 us (330 MB at 5.8 TB/s); 1024 x 24576 x 4096, with the quantisation of the
+// rows, 46 us (52 with T = 192, 65 with T = 128; 55 in a long loop); scores of 1024 rows against the head 221 us (5.8 PFLOP/s; 4.9 in
+// a long loop, at the power limit; its MMAs alone 194 us).
 // Every wait on a barrier is bounded; after a time-out the outputs are NaN and the status word is raised.
 // NQ: groups of 32 columns that an epilogue warp holds; with one (T <= 64) two CTAs fit on an SM by their registers.
 template <int CG, bool SCORE, int NQ>
