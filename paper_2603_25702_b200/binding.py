@@ -188,6 +188,11 @@ def _dtype(name: str) -> int:
     return _DTYPES[name]
 
 
+def _c32(v: int) -> int:
+    """A size that does not fit the ABI's 32 bits is passed as -1, which every entry point refuses (ctypes would cut it off)."""
+    return v if -0x80000000 <= v <= 0x7FFFFFFF else -1
+
+
 def ops_status(stream: int = 0) -> None:
     """Waits for ``stream``; raises S2D2Error(-5) if a bounded wait in a kernel of the stand-alone operators ran out since
     the last call (that kernel's outputs are NaN then)."""
@@ -223,7 +228,7 @@ def mxfp4_gemm(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int,
                y_stride: Optional[int] = None, scale: float = 1.0, stream: int = 0) -> None:
     """y[M, N] = scale * x[M, K] w[N, K]^T of two MXFP4 matrices, y "fp32" or "bf16".  Asynchronous."""
     lib = load_library()
-    _ops_check(lib.s2d2_mxfp4_gemm(d_x_codes, d_x_scales, d_w_codes, d_w_scales, d_y, _dtype(y_dtype), M, N, K,
+    _ops_check(lib.s2d2_mxfp4_gemm(d_x_codes, d_x_scales, d_w_codes, d_w_scales, d_y, _dtype(y_dtype), _c32(M), _c32(N), _c32(K),
                                    N if y_stride is None else y_stride, scale, stream))
 
 
@@ -233,7 +238,7 @@ def score_logits(d_logits: int, dtype: str, n_rows: int, vocab: int, row_stride:
     """Log probability and rank of one given token per row (int32), log-sum-exp, entropy and the ``top_k`` most probable tokens of
     device logits ("fp32" or "bf16").  Outputs are fp32 (ids and ranks int32); 0 leaves one out.  Asynchronous."""
     lib = load_library()
-    _ops_check(lib.s2d2_score_logits(d_logits, _dtype(dtype), n_rows, vocab, row_stride, d_tokens, top_k, d_logprob, d_rank, d_lse,
+    _ops_check(lib.s2d2_score_logits(d_logits, _dtype(dtype), n_rows, _c32(vocab), row_stride, d_tokens, _c32(top_k), d_logprob, d_rank, d_lse,
                                      d_entropy, d_top_ids, d_top_logprobs, stream))
 
 
@@ -241,7 +246,7 @@ def mxfp4_score_workspace(M: int, N: int, K: int) -> int:
     """Bytes of workspace that mxfp4_score needs."""
     lib = load_library()
     n = C.c_int64()
-    _ops_check(lib.s2d2_mxfp4_score_workspace(M, N, K, C.byref(n)))
+    _ops_check(lib.s2d2_mxfp4_score_workspace(_c32(M), _c32(N), _c32(K), C.byref(n)))
     return n.value
 
 
@@ -250,7 +255,7 @@ def mxfp4_score(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int
     """Log probability of one token per row, log-sum-exp and entropy of the logits scale * x w^T (x [M, K] hidden rows, w [N, K]
     the head, both MXFP4) without the logits in memory.  ``d_ws``: mxfp4_score_workspace bytes.  Asynchronous."""
     lib = load_library()
-    _ops_check(lib.s2d2_mxfp4_score(d_x_codes, d_x_scales, d_w_codes, d_w_scales, M, N, K, scale, d_tokens, d_logprob, d_lse, d_entropy,
+    _ops_check(lib.s2d2_mxfp4_score(d_x_codes, d_x_scales, d_w_codes, d_w_scales, _c32(M), _c32(N), _c32(K), scale, d_tokens, d_logprob, d_lse, d_entropy,
                                     d_ws, ws_bytes, stream))
 
 
@@ -442,7 +447,7 @@ class Engine:
         if top_k > 0:
             out["top_ids"], out["top_logprobs"] = np.zeros((n_rows, top_k), np.int32), np.zeros((n_rows, top_k), np.float32)
         ptr = lambda name: out[name].ctypes.data if name in out else None
-        self._check(self.lib.s2d2_score_pass(self._h, which, n_rows, None if tok is None else tok.ctypes.data, top_k, ptr("logprob"),
+        self._check(self.lib.s2d2_score_pass(self._h, _c32(which), _c32(n_rows), None if tok is None else tok.ctypes.data, top_k, ptr("logprob"),
                                              ptr("rank"), ptr("lse"), ptr("entropy"), ptr("top_ids"), ptr("top_logprobs")))
         return out
 

@@ -227,6 +227,70 @@ def test_long_axes(s2d2, M, N, K):
     assert (err <= product_tolerance(xv, wv, 1.0, "fp32")).all()
 
 
+def test_the_largest_axes(s2d2):
+    """Columns and K, and rows, at their documented limits; a sample is checked."""
+    K, M, N = 1048576, 3, 140
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, w = torch.randn(M, K, generator=g, device="cuda"), torch.randn(N, K, generator=g, device="cuda") * 0.1
+    (xc, xs), (wc, ws) = quantize(s2d2, x, 0), quantize(s2d2, w, 0)
+    y = torch.empty(M, N, device="cuda")
+    s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "fp32", M, N, K, stream=stream())
+    s2d2.ops_status(stream())
+    xv = ou.mxfp4_values(*ou.mxfp4_encode(x.double().cpu().numpy()), K)
+    c = [0, 1, 127, 128, N - 1]
+    wv = ou.mxfp4_values(*ou.mxfp4_encode(w[c].double().cpu().numpy()), K)
+    err = np.abs(y[:, c].double().cpu().numpy() - xv @ wv.T)
+    assert (err <= product_tolerance(xv, wv, 1.0, "fp32")).all()
+    del x, w, xc, xs, wc, ws
+    rows = 4194304
+    x = torch.randn(rows, 3, generator=g, device="cuda")
+    codes, scales = quantize(s2d2, x, 0)
+    back = torch.empty_like(x)
+    s2d2.mxfp4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, 3, back.data_ptr(), "fp32", 3, stream())
+    at = np.r_[0:300, rows // 2:rows // 2 + 300, rows - 300:rows]
+    want = ou.mxfp4_values(*ou.mxfp4_encode(x[at].double().cpu().numpy()), 3)
+    assert np.array_equal(back[at].double().cpu().numpy(), want)
+
+
+def test_calls_from_several_host_threads(s2d2):
+    """Threads with streams of their own: results as alone, and each thread reads the text of its own failure."""
+    import threading
+    K = 1024
+    (wc, ws), wv = operand(600, K, 11)
+    jobs = [operand(M, K, M) for M in (1, 40, 130, 300)]
+    failures, outs = [], {}
+
+    def work(i):
+        try:
+            (xc, xs), xv = jobs[i]
+            M = xv.shape[0]
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                y = torch.empty(M, 600, device="cuda")
+                for _ in range(20):
+                    s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "fp32", M, 600, K,
+                                    stream=st.cuda_stream)
+                    try:
+                        s2d2.mxfp4_gemm(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), y.data_ptr(), "fp32", M, 600, K,
+                                        y_stride=i, stream=st.cuda_stream) if i % 2 else s2d2.score_logits(y.data_ptr(), "fp32", M, 0, 600)
+                    except s2d2.S2D2Error as e:
+                        assert ("y_stride" if i % 2 else "vocab") in str(e), str(e)
+                st.synchronize()
+                outs[i] = y
+        except BaseException as e:      # noqa: BLE001 - reported below
+            failures.append(repr(e))
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
+    for i, (_, xv) in enumerate(jobs):
+        assert (np.abs(outs[i].double().cpu().numpy() - xv @ wv.T) <= product_tolerance(xv, wv, 1.0, "fp32")).all()
+
+
 def test_rows_further_apart_than_32_bits(s2d2):
     """Inputs and outputs whose rows lie 2^31 + 8 elements apart: offsets of the last row pass 2^32."""
     stride, K, N = 2 ** 31 + 8, 200, 130

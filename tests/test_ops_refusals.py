@@ -83,6 +83,17 @@ def test_score_refusals(s2d2):
     refused(s2d2, -1, "no output", f, P, "fp32", 1, 8, 8, P)
 
 
+def test_sizes_beyond_32_bits_are_not_cut_off(s2d2):
+    big = 2 ** 32 + 4
+    refused(s2d2, -1, "M must", s2d2.mxfp4_gemm, P, P, P, P, P, "fp32", big, 1, 32, 1)
+    refused(s2d2, -1, "N must", s2d2.mxfp4_gemm, P, P, P, P, P, "fp32", 1, big, 32, big)
+    refused(s2d2, -1, "K must", s2d2.mxfp4_gemm, P, P, P, P, P, "fp32", 1, 1, big, 1)
+    refused(s2d2, -1, "vocab", s2d2.score_logits, P, "fp32", 1, big, big, d_lse=P)
+    refused(s2d2, -1, "top_k", s2d2.score_logits, P, "fp32", 1, 8, 8, P, big, d_top_ids=P)
+    refused(s2d2, -1, "M must", s2d2.mxfp4_score_workspace, big, 100, 32)
+    refused(s2d2, -1, "M must", s2d2.mxfp4_score, P, P, P, P, big, 100, 32, P, P, 1 << 30, d_lse=P)
+
+
 def test_hidden_score_refusals(s2d2):
     f, need = s2d2.mxfp4_score, s2d2.mxfp4_score_workspace(4, 1000, 64)
     assert need > 0 and need % 16 == 0 and s2d2.mxfp4_score_workspace(0, 1000, 64) == 0
