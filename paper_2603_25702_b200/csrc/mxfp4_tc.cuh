@@ -51,7 +51,7 @@ struct Params {
     int y_bf16;
     // scores
     const int* tokens;
-    float4* parts;                   // [a_tile][range][column half][A rows of a tile]: maximum, sum, moment (base 2), the token's logit or 0
+    float4* parts;                   // [a_tile][range][column half][A rows of a tile]: maximum, sum, moment (in units of log 2), the token's logit or 0
     int ranges;                      // ranges of B per A tile, in units of `unit` rows
     int unit;
 };
@@ -199,7 +199,10 @@ __device__ __forceinline__ float exp2_fast(float x) {      // relative error 2^-
     return y;
 }
 
-// Folds up to 32 logits (accumulators times c, base 2) into a running maximum, sums and moments; even and odd columns apart.
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float NEAR = 1048576.f;      // logits of up to this magnitude take the short form of fold()
+
+// Running maximum, sum and moment of a token's logits; even and odd columns apart, the moment in units of log 2.
 struct Sums {
     float m;
     float2 s, mo;
@@ -211,6 +214,13 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {      // two operati
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     float2 d;
     asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
@@ -218,12 +228,10 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
-template <bool FULL>
-__device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float c, Sums& a) {
-    float top = a.m;
-    if (FULL) {
-        // the largest product comes from the largest accumulator, or with a negative factor from the smallest
-        float high = __uint_as_float(v[0]), low = high;
+// The largest and the smallest of the first n of 32 accumulators (NaN is passed over).
+__device__ __forceinline__ void extremes(const uint32_t (&v)[32], int n, float& high, float& low) {
+    high = low = __uint_as_float(v[0]);
+    if (n >= 32) {
 #pragma unroll
         for (int j = 1; j < 31; j += 2) {
             asm("max.f32 %0, %0, %1, %2;" : "+f"(high) : "f"(__uint_as_float(v[j])), "f"(__uint_as_float(v[j + 1])));
@@ -231,27 +239,42 @@ __device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float c, Su
         }
         high = fmaxf(high, __uint_as_float(v[31]));
         low = fminf(low, __uint_as_float(v[31]));
-        top = fmaxf(top, fmaxf(high * c, low * c));
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < n) top = fmaxf(top, __uint_as_float(v[j]) * c);
+        for (int j = 1; j < 32; ++j)
+            if (j < n) high = fmaxf(high, __uint_as_float(v[j])), low = fminf(low, __uint_as_float(v[j]));
     }
-    const float dm = fmaxf(a.m - top, -300.f), f = exp2_fast(dm);
+}
+// Adds n logits (accumulators times scale) to the sums; m: the maximum from here on, these logits included.
+// NEAR_ALL: 32 logits and a maximum of at most NEAR in magnitude. x - m is one operation then: against a maximum that is rounded the
+// unrounded logit is up to 2^-24 NEAR larger, which is nothing. Otherwise the logit is rounded first, so that no
+// difference is positive, and differences are cut off where their exponential is zero: that of -3e38 and 3e38 is infinite.
+template <bool NEAR_ALL>
+__device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float scale, float m, Sums& a) {
+    const float dm = fmaxf((a.m - m) * LOG2E, -300.f), f = exp2_fast(dm);
     const float2 zero = make_float2(0.f, 0.f), ff = make_float2(f, f);
     a.mo = fma2(ff, fma2(make_float2(dm, dm), a.s, a.mo), zero);
     a.s = fma2(ff, a.s, zero);
-    a.m = top;
-    const float2 cc = make_float2(c, c), minus_m = make_float2(-top, -top);
+    a.m = m;
+    const float2 cc = make_float2(scale, scale), minus_m = make_float2(-m, -m), log2e = make_float2(LOG2E, LOG2E);
+    if (NEAR_ALL) {
 #pragma unroll
-    for (int j = 0; j < 32; j += 2)
-        if (FULL || j < n) {
-            float2 u = fma2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, minus_m);
-            float2 e = make_float2(exp2_fast(u.x), exp2_fast(u.y));
-            if (!FULL && j + 1 >= n) u.y = e.y = 0.f;
+        for (int j = 0; j < 32; j += 2) {
+            const float2 u = mul2(fma2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, minus_m), log2e);
+            const float2 e = make_float2(exp2_fast(u.x), exp2_fast(u.y));
             a.s = add2(a.s, e);
             a.mo = fma2(u, e, a.mo);
         }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < n) {
+                // NaN for a NaN, and for infinity (m is infinite then): such a row is undefined
+                const float u = (__fmul_rn(__uint_as_float(v[j]), scale) - m) * LOG2E, e = exp2_fast(u);
+                if (j & 1) a.s.y += e, a.mo.y = fmaf(fmaxf(u, -300.f), e, a.mo.y);
+                else a.s.x += e, a.mo.x = fmaf(fmaxf(u, -300.f), e, a.mo.x);
+            }
+    }
 }
 
 // Rows split, split + S, ... of a tile's sum over the S CTAs of a cluster, each with a partial tile [T][128] at `part`.  A warp takes
@@ -525,7 +548,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         Sums sums = {0.f, {0.f, 0.f}, {0.f, 0.f}};
         float x_t = 0.f;
         int token = -1;
-        const float c2 = p.scale * 1.4426950408889634f;
         if (SCORE) pdl_wait();
         while (next_tile<SCORE>(p, t, clusters)) {
             bool ok = !*abort_flag && mbar_wait(&ctl.acc_full[acc], parity, abort_flag);
@@ -577,13 +599,19 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
                     if (!any || q * 32 >= cols) break;
-                    if (cols - q * 32 >= 32) fold<true>(v[q], 32, c2, sums);
-                    else fold<false>(v[q], cols - q * 32, c2, sums);
+                    const int n = cols - q * 32;
+                    float high, low;
+                    extremes(v[q], n, high, low);
+                    // the largest product comes from the largest accumulator, or with a negative factor from the smallest
+                    const float x0 = high * p.scale, x1 = low * p.scale, m = fmaxf(sums.m, fmaxf(x0, x1)), bottom = fminf(x0, x1);
+                    if (n >= 32 && fmaxf(fabsf(m), -bottom) <= NEAR) fold<true>(v[q], 32, p.scale, m, sums);
+                    else fold<false>(v[q], n, p.scale, m, sums);
+                    if (bottom == -INFINITY) sums.s.x = nan;          // its exponential is zero: nothing else shows it
                     const int at = token - (t.b0 + col0 + q * 32);
                     if (at >= 0 && at < 32) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
-                            if (j == at) x_t = __uint_as_float(v[q][j]) * c2;
+                            if (j == at) x_t = __fmul_rn(__uint_as_float(v[q][j]), p.scale);
                     }
                 }
                 if (!ok) sums.s.x = nan;
@@ -635,7 +663,7 @@ score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse
     const bool has_token = token >= 0 && token < p.b_rows;
     float4 a = make_float4(-3.402823466e38f, 0.f, 0.f, 0.f);      // maximum, sum, moment; logit of the token (zero in all parts but one)
     auto add = [&](const float4 b) {
-        const float M = fmaxf(a.x, b.x), d1 = fmaxf(a.x - M, -300.f), d2 = fmaxf(b.x - M, -300.f);
+        const float M = fmaxf(a.x, b.x), d1 = fmaxf((a.x - M) * LOG2E, -300.f), d2 = fmaxf((b.x - M) * LOG2E, -300.f);
         const float f1 = exp2_fast(d1), f2 = exp2_fast(d2);
         a = make_float4(M, f1 * a.y + f2 * b.y, f1 * (a.z + d1 * a.y) + f2 * (b.z + d2 * b.y), a.w + b.w);
     };
@@ -651,11 +679,11 @@ score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse
     __syncthreads();
     if (threadIdx.x) return;
     for (int w = 1; w < 4; ++w) add(sh[w]);
-    const float ln2 = 0.6931471805599453f, log_s = log2f(a.y), nan = __int_as_float(0x7fffffff);
+    const float log_s = logf(a.y), nan = __int_as_float(0x7fffffff);
     const bool undefined = !(a.y > 0.f) || isinf(a.x);
-    if (lse) lse[r] = undefined ? nan : (a.x + log_s) * ln2;
-    if (entropy) entropy[r] = undefined ? nan : (log_s - a.z / a.y) * ln2;
-    if (logprob) logprob[r] = undefined || !has_token ? nan : ((a.w - a.x) - log_s) * ln2;
+    if (lse) lse[r] = undefined ? nan : a.x + log_s;
+    if (entropy) entropy[r] = undefined ? nan : log_s - a.z * 0.6931471805599453f / a.y;
+    if (logprob) logprob[r] = undefined || !has_token ? nan : (a.w - a.x) - log_s;
 }
 
 }  // namespace mx
