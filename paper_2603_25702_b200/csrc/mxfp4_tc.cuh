@@ -51,7 +51,7 @@ struct Params {
     int y_bf16;
     // scores
     const int* tokens;
-    float4* parts;                   // [a_tile][range][column half][A rows of a tile]: maximum, sum, moment (in units of log 2), the token's logit or 0
+    float4* parts;                   // [a_tile][range][column half][A rows of a tile]: reference, sum, moment (in units of log 2), the token's logit or 0
     int ranges;                      // ranges of B per A tile, in units of `unit` rows
     int unit;
 };
@@ -202,11 +202,28 @@ __device__ __forceinline__ float exp2_fast(float x) {      // relative error 2^-
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float NEAR = 1048576.f;      // logits of up to this magnitude take the short form of fold()
 
-// Running maximum, sum and moment of a token's logits; even and odd columns apart, the moment in units of log 2.
+// Sum of e^(x - m) and moment sum of u 2^u, u = (x - m) / log 2, over a token's logits; each with what its additions rounded off, since
+// one thread may add up millions of terms. m is the largest logit or up to 1 less: it rises in steps of more than 1, so
+// that the errors of the factors of its rises do not add up (each is weighted by the e^-1 of those behind it).
 struct Sums {
-    float m;
-    float2 s, mo;
+    float m, s, s_low, mo, mo_low;
 };
+// a + low += b, low taking the rounding error of the addition exactly
+__device__ __forceinline__ void add_exact(float& a, float& low, float b) {
+    const float t = a + b, c = t - a;
+    low += (a - (t - c)) + (b - c);
+    a = t;
+}
+__device__ __forceinline__ void raise(Sums& a, float top) {
+    if (top > a.m + 1.f) {
+        const float d = fmaxf((a.m - top) * LOG2E, -300.f), f = exp2_fast(d);
+        a.mo = f * fmaf(d, a.s, a.mo);
+        a.mo_low = f * fmaf(d, a.s_low, a.mo_low);
+        a.s *= f;
+        a.s_low *= f;
+        a.m = top;
+    }
+}
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {      // two operations in one instruction
     float2 d;
     asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
@@ -245,25 +262,22 @@ __device__ __forceinline__ void extremes(const uint32_t (&v)[32], int n, float& 
             if (j < n) high = fmaxf(high, __uint_as_float(v[j])), low = fminf(low, __uint_as_float(v[j]));
     }
 }
-// Adds n logits (accumulators times scale) to the sums; m: the maximum from here on, these logits included.
-// NEAR_ALL: 32 logits and a maximum of at most NEAR in magnitude. x - m is one operation then: against a maximum that is rounded the
-// unrounded logit is up to 2^-24 NEAR larger, which is nothing. Otherwise the logit is rounded first, so that no
-// difference is positive, and differences are cut off where their exponential is zero: that of -3e38 and 3e38 is infinite.
+// Adds n logits (accumulators times scale) to the sums: at most 16 terms one after the other, even and odd columns apart, then exactly.
+// NEAR_ALL: 32 logits, all of at most NEAR in magnitude, as is the reference. x - m is one operation then: against a reference that is
+// rounded the unrounded logit is up to 2^-24 NEAR larger, which is nothing. Otherwise the logit is rounded first and differences are cut off
+// where their exponential is zero: that of -3e38 and 3e38 is infinite.
 template <bool NEAR_ALL>
-__device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float scale, float m, Sums& a) {
-    const float dm = fmaxf((a.m - m) * LOG2E, -300.f), f = exp2_fast(dm);
-    const float2 zero = make_float2(0.f, 0.f), ff = make_float2(f, f);
-    a.mo = fma2(ff, fma2(make_float2(dm, dm), a.s, a.mo), zero);
-    a.s = fma2(ff, a.s, zero);
-    a.m = m;
+__device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float scale, Sums& a) {
+    float2 s = make_float2(0.f, 0.f), mo = s;
+    const float m = a.m;
     const float2 cc = make_float2(scale, scale), minus_m = make_float2(-m, -m), log2e = make_float2(LOG2E, LOG2E);
     if (NEAR_ALL) {
 #pragma unroll
         for (int j = 0; j < 32; j += 2) {
             const float2 u = mul2(fma2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), cc, minus_m), log2e);
             const float2 e = make_float2(exp2_fast(u.x), exp2_fast(u.y));
-            a.s = add2(a.s, e);
-            a.mo = fma2(u, e, a.mo);
+            s = add2(s, e);
+            mo = fma2(u, e, mo);
         }
     } else {
 #pragma unroll
@@ -271,10 +285,12 @@ __device__ __forceinline__ void fold(const uint32_t (&v)[32], int n, float scale
             if (j < n) {
                 // NaN for a NaN, and for infinity (m is infinite then): such a row is undefined
                 const float u = (__fmul_rn(__uint_as_float(v[j]), scale) - m) * LOG2E, e = exp2_fast(u);
-                if (j & 1) a.s.y += e, a.mo.y = fmaf(fmaxf(u, -300.f), e, a.mo.y);
-                else a.s.x += e, a.mo.x = fmaf(fmaxf(u, -300.f), e, a.mo.x);
+                if (j & 1) s.y += e, mo.y = fmaf(fmaxf(u, -300.f), e, mo.y);
+                else s.x += e, mo.x = fmaf(fmaxf(u, -300.f), e, mo.x);
             }
     }
+    add_exact(a.s, a.s_low, s.x + s.y);
+    add_exact(a.mo, a.mo_low, mo.x + mo.y);
 }
 
 // Rows split, split + S, ... of a tile's sum over the S CTAs of a cluster, each with a partial tile [T][128] at `part`.  A warp takes
@@ -385,7 +401,7 @@ __device__ __forceinline__ bool next_tile(const Params& p, Tiles& t, int cluster
 //   product (SCORE = false): A = weights, B = tokens.  The accumulator's lanes are output features, so an epilogue warp stores 32
 //     consecutive elements of an output row, whatever that row's alignment.
 //   scores (SCORE = true): A = tokens, B = head.  A lane is one token's row of logits: each thread folds the logits of
-//     its token into a running maximum, sum and moment; nothing is exchanged between threads and no logit leaves the SM.
+//     its token into a running reference, sum and moment; nothing is exchanged between threads and no logit leaves the SM.
 //   warp 0     producer of the codes: TMA into a ring of stages that runs on from tile to tile
 //   warp 10    producer of the scale tiles of the same stages
 //   warp 1     scales to tensor memory (two buffers), four MMAs of 64 elements per stage; tensor memory
@@ -545,7 +561,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         int acc = 0;
         uint32_t parity = 0;
         // scores
-        Sums sums = {0.f, {0.f, 0.f}, {0.f, 0.f}};
+        Sums sums = {};
         float x_t = 0.f;
         int token = -1;
         if (SCORE) pdl_wait();
@@ -592,7 +608,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 }
             } else {
                 if (t.first) {
-                    sums = Sums{-3.402823466e38f, {0.f, 0.f}, {0.f, 0.f}};
+                    sums = Sums{-3.402823466e38f, 0.f, 0.f, 0.f, 0.f};
                     x_t = 0.f;
                     token = p.tokens && a < p.a_rows ? p.tokens[a] : -1;
                 }
@@ -603,10 +619,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     float high, low;
                     extremes(v[q], n, high, low);
                     // the largest product comes from the largest accumulator, or with a negative factor from the smallest
-                    const float x0 = high * p.scale, x1 = low * p.scale, m = fmaxf(sums.m, fmaxf(x0, x1)), bottom = fminf(x0, x1);
-                    if (n >= 32 && fmaxf(fabsf(m), -bottom) <= NEAR) fold<true>(v[q], 32, p.scale, m, sums);
-                    else fold<false>(v[q], n, p.scale, m, sums);
-                    if (bottom == -INFINITY) sums.s.x = nan;          // its exponential is zero: nothing else shows it
+                    const float x0 = high * p.scale, x1 = low * p.scale, bottom = fminf(x0, x1);
+                    raise(sums, fmaxf(x0, x1));
+                    if (n >= 32 && fmaxf(fabsf(sums.m), -bottom) <= NEAR) fold<true>(v[q], 32, p.scale, sums);
+                    else fold<false>(v[q], n, p.scale, sums);
+                    if (bottom == -INFINITY) sums.s = nan;            // its exponential is zero: nothing else shows it
                     const int at = token - (t.b0 + col0 + q * 32);
                     if (at >= 0 && at < 32) {
 #pragma unroll
@@ -614,10 +631,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             if (j == at) x_t = __fmul_rn(__uint_as_float(v[q][j]), p.scale);
                     }
                 }
-                if (!ok) sums.s.x = nan;
+                if (!ok) sums.s = nan;
                 if (t.last && a < p.a_rows) {
                     const int range = (t.item - clusters) / p.a_tiles;
-                    p.parts[(((size_t)t.a0 * p.ranges + range) * 2 + half) * (ROWS * CG) + row0] = make_float4(sums.m, sums.s.x + sums.s.y, sums.mo.x + sums.mo.y, x_t);
+                    p.parts[(((size_t)t.a0 * p.ranges + range) * 2 + half) * (ROWS * CG) + row0] = make_float4(sums.m, sums.s + sums.s_low, sums.mo + sums.mo_low, x_t);
                 }
             }
         }
@@ -661,7 +678,7 @@ score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse
     const float4* parts = p.parts + (size_t)(r / rows_per_tile) * p.ranges * 2 * rows_per_tile + r % rows_per_tile;
     const int token = p.tokens ? p.tokens[r] : -1;
     const bool has_token = token >= 0 && token < p.b_rows;
-    float4 a = make_float4(-3.402823466e38f, 0.f, 0.f, 0.f);      // maximum, sum, moment; logit of the token (zero in all parts but one)
+    float4 a = make_float4(-3.402823466e38f, 0.f, 0.f, 0.f);      // reference, sum, moment; logit of the token (zero in all parts but one)
     auto add = [&](const float4 b) {
         const float M = fmaxf(a.x, b.x), d1 = fmaxf((a.x - M) * LOG2E, -300.f), d2 = fmaxf((b.x - M) * LOG2E, -300.f);
         const float f1 = exp2_fast(d1), f2 = exp2_fast(d2);
@@ -682,7 +699,8 @@ score_parts_kernel(const Params p, int rows_per_tile, float* logprob, float* lse
     const float log_s = logf(a.y), nan = __int_as_float(0x7fffffff);
     const bool undefined = !(a.y > 0.f) || isinf(a.x);
     if (lse) lse[r] = undefined ? nan : a.x + log_s;
-    if (entropy) entropy[r] = undefined ? nan : log_s - a.z * 0.6931471805599453f / a.y;
+    // (of a certain token: a difference of equal numbers, rounded)
+    if (entropy) entropy[r] = undefined ? nan : fmaxf(log_s - a.z * 0.6931471805599453f / a.y, 0.f);
     if (logprob) logprob[r] = undefined || !has_token ? nan : (a.w - a.x) - log_s;
 }
 
