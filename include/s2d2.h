@@ -447,6 +447,11 @@ int s2d2_mxfp4_score(const void* d_x_codes, const void* d_x_scales, const void* 
                      int32_t N, int32_t K, float scale, const int32_t* d_tokens, float* d_logprob, float* d_lse,
                      float* d_entropy, void* d_ws, int64_t ws_bytes, void* cuda_stream);
 
+/* Test tap: the waits of this host thread's next s2d2_mxfp4_gemm or s2d2_mxfp4_score run out after limit_polls polls (1..2^20; counted
+ * in steps of 32, a poll takes about 4 us). With withhold != 0 that call does not load its codes, so that they do run out: it writes NaN and
+ * raises the status. */
+int s2d2_debug_mxfp4_wait(uint32_t limit_polls, int32_t withhold);
+
 /* s2d2_score_logits on the logits that the last draft pass (which = 0) or verifier pass (which = 1) of a context left
  * behind: rows as s2d2_debug_copy_logits lists them, n_rows of them from the first one on.  Host pointers; outputs
  * [n_rows] and [n_rows, top_k], each may be NULL as above.  Synchronous. */

@@ -83,6 +83,7 @@ EXPORTS = [
     "s2d2_gemm_bf16_noalloc", "s2d2_noalloc_last_error",
     "s2d2_ops_last_error", "s2d2_ops_status", "s2d2_mxfp4_sizes", "s2d2_mxfp4_quantize", "s2d2_mxfp4_dequantize",
     "s2d2_mxfp4_gemm", "s2d2_mxfp4_score_workspace", "s2d2_mxfp4_score", "s2d2_score_logits", "s2d2_score_pass",
+    "s2d2_debug_mxfp4_wait",
 ]
 _TEXTS = ("s2d2_last_error", "s2d2_noalloc_last_error", "s2d2_ops_last_error")     # these return a string
 
@@ -153,6 +154,7 @@ def load_library() -> C.CDLL:
     lib.s2d2_mxfp4_score_workspace.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
     lib.s2d2_mxfp4_score.argtypes = [C.c_void_p] * 4 + [C.c_int32] * 3 + [C.c_float] + [C.c_void_p] * 5 + [C.c_int64, C.c_void_p]
     lib.s2d2_score_logits.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_int32] + [C.c_void_p] * 7
+    lib.s2d2_debug_mxfp4_wait.argtypes = [C.c_uint32, C.c_int32]
     lib.s2d2_score_pass.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32] + [C.c_void_p] * 6
     _LIB = lib
     return lib
@@ -257,6 +259,13 @@ def mxfp4_score(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int
     lib = load_library()
     _ops_check(lib.s2d2_mxfp4_score(d_x_codes, d_x_scales, d_w_codes, d_w_scales, _c32(M), _c32(N), _c32(K), scale, d_tokens, d_logprob, d_lse, d_entropy,
                                     d_ws, ws_bytes, stream))
+
+
+def debug_mxfp4_wait(limit_polls: int, withhold: bool = False) -> None:
+    """Test tap: the waits of this thread's next mxfp4_gemm or mxfp4_score run out after ``limit_polls`` polls; with ``withhold`` they
+    do, because its codes are not loaded."""
+    lib = load_library()
+    _ops_check(lib.s2d2_debug_mxfp4_wait(limit_polls, int(withhold)))
 
 
 class Engine:

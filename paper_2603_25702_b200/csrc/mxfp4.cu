@@ -464,9 +464,17 @@ int launch_product(const Plan& plan, const CUtensorMap* maps, cudaStream_t st) {
     return ops::fail(S2D2_ERR_CUDA, "mxfp4 product: %s", cudaGetErrorString(e));
 }
 
+// Test tap: waits of this host thread's next product (0: as they are), and whether its codes are held back.
+thread_local uint32_t g_wait_limit;
+thread_local int g_withhold;
+
 template <bool SCORE>
 int run_product(const ops::Device* dev, Plan& plan, const void* ac, const void* as, const void* bc, const void* bs, cudaStream_t st) {
-    const mx::Params& p = plan.p;
+    mx::Params& p = plan.p;
+    p.wait_limit = g_wait_limit ? g_wait_limit : tc::WAIT_LIMIT;
+    p.withhold = g_withhold;
+    g_wait_limit = 0;
+    g_withhold = 0;
     CUtensorMap maps[5];
     if (int rc = encode_codes(dev, &maps[0], ac, p.a_rows, p.K, p.a_box)) return rc;
     if (int rc = encode_codes(dev, &maps[1], bc, p.b_rows, p.K, p.T / plan.cg)) return rc;
@@ -585,5 +593,13 @@ extern "C" int s2d2_mxfp4_score(const void* d_x_codes, const void* d_x_scales, c
         cudaGetLastError();
         return ops::fail(S2D2_ERR_CUDA, "mxfp4_score: %s", cudaGetErrorString(e));
     }
+    return S2D2_OK;
+}
+
+extern "C" int s2d2_debug_mxfp4_wait(uint32_t limit_polls, int32_t withhold) {
+    ops::clear_error();
+    if (limit_polls < 1 || limit_polls > (1u << 20)) return ops::fail(S2D2_ERR_INVALID, "debug_mxfp4_wait: limit_polls must be in 1..2^20");
+    g_wait_limit = limit_polls;
+    g_withhold = withhold != 0;
     return S2D2_OK;
 }

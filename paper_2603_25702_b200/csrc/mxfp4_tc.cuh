@@ -45,6 +45,8 @@ struct Params {
     int control_at;                  // byte offset of Control behind the ring
     float scale;
     int* status;
+    uint32_t wait_limit;             // polls of a barrier before a wait is given up
+    int withhold;                    // test tap: the codes are not loaded, so that nothing ever completes a stage
     // product
     void* y;                         // [b_rows, a_rows], rows ldy elements apart
     long long ldy;
@@ -345,6 +347,27 @@ __device__ __forceinline__ bool elect() {
 __device__ __forceinline__ void settle() {
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
 }
+__device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
+// Bounded wait for the phase with the given parity; false when it has run out or another role of the CTA has given up. The limit is
+// looked at every 32 polls of about 4 us, beside a constant bound: as the loop's own bound it made every stage 4 % longer.
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, uint32_t limit, volatile int* abort_flag) {
+    const uint32_t addr = smem_u32(bar);
+    for (uint32_t it = 0; it < WAIT_LIMIT; ++it) {
+        if ((it & 31u) == 31u && (it >= limit || *abort_flag)) return false;
+        if (poll(addr, parity)) return true;
+    }
+    return false;
+}
 // Position in the ring: stage and the parity of its current use.
 struct Ring {
     int s = 0;
@@ -462,16 +485,18 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem = ctl.tmem_slot;
     pdl_launch();
+    // All warps: none reads or writes memory that the kernels in front still use, and the bounded waits begin behind them.
+    pdl_wait();
 
     Tiles t = first_tile<SCORE>(cluster);
     const int b_half = p.T / CG, a_bytes = p.a_box * KBYTES, b_bytes = b_half * KBYTES;
     if (warp == 0 || warp == 10) {
         // Producers: codes (warp 0) and scales (warp 10) of the same stage, reported to one barrier.
-        pdl_wait();
         const uint32_t fixed_bytes = (uint32_t)CG * (a_bytes + (1 + p.sf_tiles) * 2 * SF_TILE);
         Ring r;
         r.parity = 1;                                        // a fresh barrier passes a wait for the phase before its first
         bool ok = true;
+        if (p.withhold && warp == 0) t.item = 0x7fffffff;
         while (ok && next_tile<SCORE>(p, t, clusters)) {
             const int a_row = (t.a0 * CG + (CG == 2 ? (int)rank : 0)) * ROWS;
             const int b_row = t.b0 + (CG == 2 ? (int)rank * b_half : 0);
@@ -479,7 +504,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const bool cut = SCORE && CG == 1 && t.rows < p.T;          // a single CTA loads no more of it than the range holds
             const uint32_t bytes = fixed_bytes + (uint32_t)CG * (cut ? (t.rows + CUT - 1) / CUT * CUT : b_half) * KBYTES;
             for (int kb = kb0; kb < kb1; ++kb, r.next(S)) {
-                ok = __all_sync(0xffffffffu, mbar_wait(&ctl.empty[r.s], r.parity, abort_flag));
+                ok = __all_sync(0xffffffffu, wait(&ctl.empty[r.s], r.parity, p.wait_limit, abort_flag));
                 if (!ok) break;
                 const uint32_t a = smem_u32(ring) + r.s * sbytes;
                 uint32_t bar = smem_u32(&ctl.full[r.s]);
@@ -511,13 +536,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             uint32_t acc_parity = 1;
             bool ok = true;
             while (ok && next_tile<SCORE>(p, t, clusters)) {
-                ok = __all_sync(0xffffffffu, mbar_wait(&ctl.acc_empty[acc], acc_parity, abort_flag));
+                ok = __all_sync(0xffffffffu, wait(&ctl.acc_empty[acc], acc_parity, p.wait_limit, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t d = tmem + d_col + acc * acc_columns(p.T);
                 const uint32_t b_col = (uint32_t)(t.b0 % ROWS) / 32;
                 for (int kb = kb0; kb < kb1; ++kb, r.next(S), odd ^= 1) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(&ctl.full[r.s], r.parity, abort_flag));
+                    ok = __all_sync(0xffffffffu, wait(&ctl.full[r.s], r.parity, p.wait_limit, abort_flag));
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t a_addr = smem_u32(ring) + r.s * sbytes, sf_addr = a_addr + a_bytes + b_bytes;
@@ -564,9 +589,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         Sums sums = {};
         float x_t = 0.f;
         int token = -1;
-        if (SCORE) pdl_wait();
         while (next_tile<SCORE>(p, t, clusters)) {
-            bool ok = !*abort_flag && mbar_wait(&ctl.acc_full[acc], parity, abort_flag);
+            bool ok = !*abort_flag && wait(&ctl.acc_full[acc], parity, p.wait_limit, abort_flag);
             if (!ok) *abort_flag = 1;
             ok = __all_sync(0xffffffffu, ok);
             if (!ok && p.splits > 1) settle();               // the partial tile goes where they land
