@@ -404,7 +404,7 @@ const char* s2d2_noalloc_last_error(void);
 
 const char* s2d2_ops_last_error(void);
 /* Waits for the stream; S2D2_ERR_TIMEOUT if a bounded wait inside a kernel of these operators ran out since the last
- * call (the outputs of that kernel are NaN then, never stale), else S2D2_OK. */
+ * call (all outputs of the tiles that it concerns are NaN then, never stale), else S2D2_OK. */
 int s2d2_ops_status(void* cuda_stream);
 
 /* Bytes of the codes and of the scales of a [rows, cols] matrix. */

@@ -176,6 +176,9 @@ __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.
 __device__ __forceinline__ void arrive_remote(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void set_remote(uint32_t addr, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ void store_y(void* y, int y_bf16, size_t at, float v) {
     if (y_bf16) reinterpret_cast<bf16*>(y)[at] = __float2bfloat16_rn(v);
     else reinterpret_cast<float*>(y)[at] = v;
@@ -420,6 +423,26 @@ __device__ __forceinline__ bool next_tile(const Params& p, Tiles& t, int cluster
     return true;
 }
 
+// After a time-out: NaN in all outputs of the cluster's tiles, those that were finished included.
+template <int CG, bool SCORE>
+__device__ __forceinline__ void all_nan(const Params& p, int cluster, int clusters, int pair_rank) {
+    const float nan = __int_as_float(0x7fffffff);
+    Tiles t = first_tile<SCORE>(cluster);
+    while (next_tile<SCORE>(p, t, clusters)) {
+        const int row0 = pair_rank * ROWS, a0 = t.a0 * CG * ROWS + row0;
+        if (SCORE) {
+            const int range = (t.item - clusters) / p.a_tiles;
+            for (int i = threadIdx.x; t.last && i < 2 * ROWS; i += THREADS)
+                if (a0 + i % ROWS < p.a_rows)
+                    p.parts[(((size_t)t.a0 * p.ranges + range) * 2 + i / ROWS) * (ROWS * CG) + row0 + i % ROWS] = make_float4(0.f, nan, nan, nan);
+        } else {
+            const int rows = min(t.rows, p.b_rows - t.b0);
+            for (int i = threadIdx.x; i < rows * ROWS; i += THREADS)
+                if (a0 + i % ROWS < p.a_rows) store_y(p.y, p.y_bf16, (size_t)(t.b0 + i / ROWS) * p.ldy + a0 + i % ROWS, nan);
+        }
+    }
+}
+
 // One kernel for both operators and for one CTA or a pair of CTAs per tile.
 //   product (SCORE = false): A = weights, B = tokens.  The accumulator's lanes are output features, so an epilogue warp stores 32
 //     consecutive elements of an output row, whatever that row's alignment.
@@ -437,7 +460,7 @@ __device__ __forceinline__ bool next_tile(const Params& p, Tiles& t, int cluster
 // Measured (B200): a head of 151936 x 4096 against 8 rows 57 us (330 MB at 5.8 TB/s); 1024 x 24576 x 4096, with the quantisation of the
 // rows, 46 us (52 with T = 192, 65 with T = 128; 55 in a long loop); scores of 1024 rows against the head 221 us (5.8 PFLOP/s; 4.9 in
 // a long loop, at the power limit; its MMAs alone 194 us).
-// Every wait on a barrier is bounded; after a time-out the outputs are NaN and the status word is raised.
+// Every wait on a barrier is bounded; after a time-out all outputs of the cluster are NaN and the status word is raised.
 // NQ: groups of 32 columns that an epilogue warp holds; with one (T <= 64) two CTAs fit on an SM by their registers.
 template <int CG, bool SCORE, int NQ>
 __global__ void __launch_bounds__(THREADS, NQ == 1 ? 2 : 1)
@@ -590,10 +613,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         float x_t = 0.f;
         int token = -1;
         while (next_tile<SCORE>(p, t, clusters)) {
-            bool ok = !*abort_flag && wait(&ctl.acc_full[acc], parity, p.wait_limit, abort_flag);
-            if (!ok) *abort_flag = 1;
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok && p.splits > 1) settle();               // the partial tile goes where they land
+            if (!__all_sync(0xffffffffu, !*abort_flag && wait(&ctl.acc_full[acc], parity, p.wait_limit, abort_flag))) {
+                *abort_flag = 1;
+                break;
+            }
             tc_fence_after();
             const uint32_t taddr = tmem + d_col + acc * acc_columns(p.T) + col0 + ((uint32_t)(quarter * 32) << 16);
             const int a = t.a0 * CG * ROWS + row0;
@@ -625,10 +648,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
-                            if (q * 32 + j < cols) part[(q * 32 + j) * ROWS] = ok ? __uint_as_float(v[q][j]) : nan;
+                            if (q * 32 + j < cols) part[(q * 32 + j) * ROWS] = __uint_as_float(v[q][j]);
                 } else if (a < p.a_rows) {
-                    if (p.y_bf16) store_columns(reinterpret_cast<bf16*>(p.y) + (size_t)b * p.ldy + a, p.ldy, v, cols, ok ? p.scale : nan);
-                    else store_columns(reinterpret_cast<float*>(p.y) + (size_t)b * p.ldy + a, p.ldy, v, cols, ok ? p.scale : nan);
+                    if (p.y_bf16) store_columns(reinterpret_cast<bf16*>(p.y) + (size_t)b * p.ldy + a, p.ldy, v, cols, p.scale);
+                    else store_columns(reinterpret_cast<float*>(p.y) + (size_t)b * p.ldy + a, p.ldy, v, cols, p.scale);
                 }
             } else {
                 if (t.first) {
@@ -655,7 +678,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             if (j == at) x_t = __fmul_rn(__uint_as_float(v[q][j]), p.scale);
                     }
                 }
-                if (!ok) sums.s = nan;
                 if (t.last && a < p.a_rows) {
                     const int range = (t.item - clusters) / p.a_tiles;
                     p.parts[(((size_t)t.a0 * p.ranges + range) * 2 + half) * (ROWS * CG) + row0] = make_float4(sums.m, sums.s + sums.s_low, sums.mo + sums.mo_low, x_t);
@@ -677,8 +699,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     __syncthreads();
     if (*abort_flag) {
-        if (threadIdx.x == 0) atomicExch(p.status, 1);
         settle();
+        // the CTAs of a cluster fail together: what one of them missed is in the others' outputs, too
+        if (threadIdx.x < cluster_size) set_remote(cluster_size > 1 ? cluster_map(smem_u32(&ctl.abort_flag), threadIdx.x) : smem_u32(&ctl.abort_flag), 1);
     }
     tc_fence_before();
     if (cluster_size > 1) {
@@ -689,6 +712,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         __syncthreads();
     }
     if (warp == 1) dealloc<CG>(tmem, p.tmem_cols);
+    if (*abort_flag) {
+        // behind the barrier, so that these are the last values of the cluster's outputs
+        if (threadIdx.x == 0) atomicExch(p.status, 1);
+        all_nan<CG, SCORE>(p, cluster, clusters, CG == 2 ? (int)rank : 0);
+    }
 }
 
 // Scores from the partial results of a row: one block per row, a thread per part (or several), merged in a fixed order.

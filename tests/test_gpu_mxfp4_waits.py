@@ -38,3 +38,72 @@ def test_waits_begin_behind_the_kernels_in_front(s2d2):
         s2d2.ops_status(stream())
         err = np.abs(z.double().cpu().numpy() - xv @ wv.T)
         assert (err <= product_tolerance(xv, wv, 1.0, "fp32")).all()
+
+
+# a CTA per tile with one and with several tiles, clusters of two, four and eight that share k, pairs of CTAs with one and several tiles
+@pytest.mark.parametrize("y_type", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(5, 37000, 256), (64, 8192, 2048), (1, 4096, 4096), (3, 130, 8192), (300, 6001, 320), (450, 30001, 300)])
+def test_product_that_runs_out_is_nan_and_reported(s2d2, M, N, K, y_type):
+    from paper_2603_25702_b200 import binding
+    dt = {"fp32": torch.float32, "bf16": torch.bfloat16}[y_type]
+    (x, xv), (w, _) = operand(M, K, 1), operand(N, K, 2, 0.02)
+    pad = 3
+
+    def call(y):
+        s2d2.mxfp4_gemm(x[0].data_ptr(), x[1].data_ptr(), w[0].data_ptr(), w[1].data_ptr(), y.data_ptr(), y_type, M, N, K, N + pad,
+                        stream=stream())
+
+    want, y = (torch.full((M + 1, N + pad), 7.0, dtype=dt, device="cuda") for _ in range(2))
+    call(want)
+    s2d2.ops_status(stream())
+    binding.debug_mxfp4_wait(64, True)
+    call(y)
+    with pytest.raises(s2d2.S2D2Error) as e:
+        s2d2.ops_status(stream())
+    assert e.value.code == -5
+    assert y[:M, :N].isnan().all() and (y[:M, N:] == 7).all() and (y[M:] == 7).all()
+    s2d2.ops_status(stream())                                        # reported once
+    call(y)
+    s2d2.ops_status(stream())
+    assert torch.equal(y, want)                                      # and nothing of it is left
+
+
+@pytest.mark.parametrize("M,N,K", [(8, 20000, 512), (100, 300, 64), (300, 20000, 128), (20000, 200, 32)])
+def test_scores_that_run_out_are_nan_and_reported(s2d2, M, N, K):
+    from paper_2603_25702_b200 import binding
+    (x, _), (w, _) = operand(M, K, 1), operand(N, K, 2, 0.02)
+    tok = torch.arange(M, dtype=torch.int32, device="cuda") % N
+    ws = torch.zeros(s2d2.mxfp4_score_workspace(M, N, K), dtype=torch.uint8, device="cuda")
+
+    def call():
+        o = torch.full((3, M + 1), 7.0, device="cuda")
+        s2d2.mxfp4_score(x[0].data_ptr(), x[1].data_ptr(), w[0].data_ptr(), w[1].data_ptr(), M, N, K, tok.data_ptr(), ws.data_ptr(),
+                         ws.numel(), d_logprob=o[0].data_ptr(), d_lse=o[1].data_ptr(), d_entropy=o[2].data_ptr(), stream=stream())
+        return o
+
+    want = call()
+    s2d2.ops_status(stream())
+    binding.debug_mxfp4_wait(64, True)
+    got = call()
+    with pytest.raises(s2d2.S2D2Error) as e:
+        s2d2.ops_status(stream())
+    assert e.value.code == -5
+    assert got[:, :M].isnan().all() and (got[:, M:] == 7).all()
+    s2d2.ops_status(stream())
+    assert torch.equal(call(), want)
+
+
+def test_a_limit_that_is_not_reached_changes_nothing(s2d2):
+    from paper_2603_25702_b200 import binding
+    M, N, K = 64, 384, 4096
+    (x, xv), (w, wv) = operand(M, K, 1), operand(N, K, 2, 0.02)
+    a, b = torch.empty(M, N, device="cuda"), torch.empty(M, N, device="cuda")
+    gemm(s2d2, x, w, a, M, N, K)
+    binding.debug_mxfp4_wait(4096)
+    gemm(s2d2, x, w, b, M, N, K)
+    s2d2.ops_status(stream())
+    assert torch.equal(a, b)
+    for bad in (0, (1 << 20) + 1):
+        with pytest.raises(s2d2.S2D2Error) as e:
+            binding.debug_mxfp4_wait(bad)
+        assert e.value.code == -1
