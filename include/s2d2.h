@@ -403,8 +403,9 @@ const char* s2d2_noalloc_last_error(void);
 #define S2D2_MXFP4_MAX_DIM 4194304       /* rows, N and M of an MXFP4 matrix; columns and K: 1048576 */
 
 const char* s2d2_ops_last_error(void);
-/* Waits for the stream; S2D2_ERR_TIMEOUT if a bounded wait inside a kernel of these operators ran out since the last
- * call (all outputs of the tiles that it concerns are NaN then, never stale), else S2D2_OK. */
+/* Waits for the stream; S2D2_ERR_TIMEOUT if a bounded wait inside a kernel of these operators ran out (all outputs of the tiles that it
+ * concerns are NaN then, never stale), else S2D2_OK. The status is the device's, not the stream's: every host thread is told once of
+ * what ran out on any stream since its last call, in its first call of all that ever did. */
 int s2d2_ops_status(void* cuda_stream);
 
 /* Bytes of the codes and of the scales of a [rows, cols] matrix. */

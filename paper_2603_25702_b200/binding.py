@@ -196,8 +196,8 @@ def _c32(v: int) -> int:
 
 
 def ops_status(stream: int = 0) -> None:
-    """Waits for ``stream``; raises S2D2Error(-5) if a bounded wait in a kernel of the stand-alone operators ran out since
-    the last call (that kernel's outputs are NaN then)."""
+    """Waits for ``stream``; raises S2D2Error(-5) if a bounded wait in a kernel of the stand-alone operators ran out, on any stream of
+    the device, since this thread's last call (outputs are NaN then)."""
     lib = load_library()
     _ops_check(lib.s2d2_ops_status(stream))
 

@@ -546,7 +546,7 @@ extern "C" int s2d2_mxfp4_gemm(const void* d_x_codes, const void* d_x_scales, co
     plan.p.y_bf16 = y_dtype == S2D2_DTYPE_BF16;
     plan.p.ldy = y_stride;
     plan.p.scale = scale;
-    plan.p.status = dev->status;
+    plan.p.timeouts = dev->timeouts;
     return run_product<false>(dev, plan, d_w_codes, d_w_scales, d_x_codes, d_x_scales, (cudaStream_t)cuda_stream);
 }
 
@@ -582,7 +582,7 @@ extern "C" int s2d2_mxfp4_score(const void* d_x_codes, const void* d_x_scales, c
     Plan plan;
     plan_score(plan, dev->n_sms, M, N, K);
     plan.p.scale = scale;
-    plan.p.status = dev->status;
+    plan.p.timeouts = dev->timeouts;
     plan.p.tokens = d_tokens;
     plan.p.parts = (float4*)d_ws;
     const cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -44,7 +44,7 @@ struct Params {
     uint32_t tmem_cols;
     int control_at;                  // byte offset of Control behind the ring
     float scale;
-    int* status;
+    int* timeouts;
     uint32_t wait_limit;             // polls of a barrier before a wait is given up
     int withhold;                    // test tap: the codes are not loaded, so that nothing ever completes a stage
     // product
@@ -460,7 +460,7 @@ __device__ __forceinline__ void all_nan(const Params& p, int cluster, int cluste
 // Measured (B200): a head of 151936 x 4096 against 8 rows 57 us (330 MB at 5.8 TB/s); 1024 x 24576 x 4096, with the quantisation of the
 // rows, 46 us (52 with T = 192, 65 with T = 128; 55 in a long loop); scores of 1024 rows against the head 221 us (5.8 PFLOP/s; 4.9 in
 // a long loop, at the power limit; its MMAs alone 194 us).
-// Every wait on a barrier is bounded; after a time-out all outputs of the cluster are NaN and the status word is raised.
+// Every wait on a barrier is bounded; after a time-out all outputs of the cluster are NaN and it is counted.
 // NQ: groups of 32 columns that an epilogue warp holds; with one (T <= 64) two CTAs fit on an SM by their registers.
 template <int CG, bool SCORE, int NQ>
 __global__ void __launch_bounds__(THREADS, NQ == 1 ? 2 : 1)
@@ -714,7 +714,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (warp == 1) dealloc<CG>(tmem, p.tmem_cols);
     if (*abort_flag) {
         // behind the barrier, so that these are the last values of the cluster's outputs
-        if (threadIdx.x == 0) atomicExch(p.status, 1);
+        if (threadIdx.x == 0) atomicAdd(p.timeouts, 1);
         all_nan<CG, SCORE>(p, cluster, clusters, CG == 2 ? (int)rank : 0);
     }
 }

@@ -16,7 +16,8 @@ thread_local char g_err[256];
 std::mutex g_setup;
 std::atomic<bool> g_ready[MAX_DEVICES];
 Device g_dev[MAX_DEVICES];
-__device__ int g_status;
+__device__ int g_timeouts;
+thread_local int g_seen[MAX_DEVICES];
 }  // namespace
 
 void clear_error() { g_err[0] = 0; }
@@ -44,7 +45,7 @@ int device(const Device** out) {
                 (e = cudaDeviceGetAttribute(&d.n_sms, cudaDevAttrMultiProcessorCount, id)) != cudaSuccess)
                 return fail(S2D2_ERR_CUDA, "cudaDeviceGetAttribute: %s", cudaGetErrorString(e));
             if (major != 10) return fail(S2D2_ERR_UNSUPPORTED, "built for sm_100a only");
-            if ((e = cudaGetSymbolAddress((void**)&d.status, g_status)) != cudaSuccess)
+            if ((e = cudaGetSymbolAddress((void**)&d.timeouts, g_timeouts)) != cudaSuccess)
                 return fail(S2D2_ERR_CUDA, "cudaGetSymbolAddress: %s", cudaGetErrorString(e));
             void* fn = nullptr;
             cudaDriverEntryPointQueryResult q;
@@ -90,11 +91,11 @@ extern "C" int s2d2_ops_status(void* cuda_stream) {
     const ops::Device* d;
     if (int rc = ops::device(&d)) return rc;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    int status = 0;
-    cudaError_t e = cudaMemcpyAsync(&status, d->status, sizeof(int), cudaMemcpyDeviceToHost, st);
+    int n = 0;
+    cudaError_t e = cudaMemcpyAsync(&n, d->timeouts, sizeof(int), cudaMemcpyDeviceToHost, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-    if (e == cudaSuccess && status) e = cudaMemsetAsync(d->status, 0, sizeof(int), st);
     if (e != cudaSuccess) return ops::fail(S2D2_ERR_CUDA, "%s", cudaGetErrorString(e));
-    if (status) return ops::fail(S2D2_ERR_TIMEOUT, "a bounded wait inside a kernel ran out; its outputs are NaN");
-    return S2D2_OK;
+    if (n == ops::g_seen[d->id]) return S2D2_OK;
+    ops::g_seen[d->id] = n;
+    return ops::fail(S2D2_ERR_TIMEOUT, "a bounded wait inside a kernel ran out; its outputs are NaN");
 }

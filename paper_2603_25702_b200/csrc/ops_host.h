@@ -25,7 +25,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 struct Device {
     int id = -1;
     int n_sms = 0;
-    int* status = nullptr;            // device word a kernel raises when a bounded wait runs out
+    int* timeouts = nullptr;          // device word: CTAs whose bounded waits ran out so far; never cleared, so that no reader takes it from another
     EncodeTiledFn encode = nullptr;
 };
 // The current device, set up on first use; S2D2_OK or a failure with its text.  The set-up loads every kernel of these operators

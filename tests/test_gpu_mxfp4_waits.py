@@ -107,3 +107,45 @@ def test_a_limit_that_is_not_reached_changes_nothing(s2d2):
         with pytest.raises(s2d2.S2D2Error) as e:
             binding.debug_mxfp4_wait(bad)
         assert e.value.code == -1
+
+
+def test_every_host_thread_learns_of_a_wait_that_ran_out(s2d2):
+    """One thread's question does not take the answer from another, and nothing is left to be cleared on a stream."""
+    import threading
+    from paper_2603_25702_b200 import binding
+    M, N, K = 5, 300, 256
+    (x, xv), (w, wv) = operand(M, K, 1), operand(N, K, 2, 0.02)
+    y = torch.zeros(M, N, device="cuda")
+    torch.cuda.synchronize()
+    launched, asked, codes = threading.Event(), threading.Event(), []
+
+    def ask(raw):
+        try:
+            s2d2.ops_status(raw)
+            return 0
+        except s2d2.S2D2Error as e:
+            return e.code
+
+    def work():
+        st = torch.cuda.Stream()
+        with torch.cuda.stream(st):
+            ask(st.cuda_stream)                                      # a new thread is told of all earlier ones
+            binding.debug_mxfp4_wait(64, True)
+            gemm(s2d2, x, w, y, M, N, K)
+            launched.set()
+            asked.wait(60)
+            codes.append(ask(st.cuda_stream))
+            codes.append(ask(st.cuda_stream))
+            gemm(s2d2, x, w, y, M, N, K)
+            codes.append(ask(st.cuda_stream))
+
+    t = threading.Thread(target=work)
+    t.start()
+    launched.wait(60)
+    torch.cuda.synchronize()
+    codes.append(ask(stream()))
+    codes.append(ask(stream()))
+    asked.set()
+    t.join(60)
+    assert codes == [-5, 0, -5, 0, 0], codes
+    assert (np.abs(y.double().cpu().numpy() - xv @ wv.T) <= product_tolerance(xv, wv, 1.0, "fp32")).all()
