@@ -64,6 +64,10 @@ struct Eight {
     }
 };
 
+__device__ __forceinline__ float load_stream_one(const float* p) { return __ldcs(p); }
+// (as a whole number: the load of a bf16 itself is no volatile one, and may be moved in front of pdl_wait)
+__device__ __forceinline__ bf16 load_stream_one(const bf16* p) { return __ushort_as_bfloat16(__ldcs((const unsigned short*)p)); }
+
 // The larger magnitude; a NaN if there is one.
 __device__ __forceinline__ float max_magnitude(float a, float b, float c) {
     float d;
@@ -142,7 +146,7 @@ __global__ void __launch_bounds__(QT) quantize_kernel(const QuantParams p) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int e = i * (2 * QUAD) + j * 32 + lane;
-                one[i][j] = e < n ? __ldcs(x + e) : from_f32<T>(0.f);
+                one[i][j] = e < n ? load_stream_one(x + e) : from_f32<T>(0.f);
             }
     }
     uint32_t* codes = (uint32_t*)(p.codes + (inside ? row * p.code_ld : 0) + c0 / 2);
@@ -197,7 +201,7 @@ __global__ void __launch_bounds__(QT) dequantize_kernel(const QuantParams p) {
     for (int i = 0; i < STEPS; ++i) {
         const bool some = left > i * (2 * QUAD);
         codes[i] = some ? __ldcs(in + i * QUAD / 4) : 0u;
-        byte[i] = some ? __ldg(scales + i * 2 * 512) : 0u;
+        byte[i] = some ? scales[i * 2 * 512] : 0u;      // (not through the read-only path: the kernel in front may write them while this one begins)
     }
     const int w0 = (int)blockIdx.y * (2 * STEPS) * QUAD, n = p.cols - w0;
     const bool direct = p.vec && n >= STEPS * 2 * QUAD;             // whole and aligned; else through shared memory, 32 elements per store

@@ -130,10 +130,11 @@ struct Row {
             }
         }
     }
-    // a vector as it stands in memory; `inside`: all of it lies in the row
+    // a vector as it stands in memory; `inside`: all of it lies in the row. Not through the read-only path: the logits may be written
+    // by the kernel in front after this one has begun.
     __device__ __forceinline__ uint4 raw(int vec, bool inside) const {
         const int i0 = first_id(vec);
-        if (inside || (i0 >= 0 && i0 + E <= V)) return __ldg(reinterpret_cast<const uint4*>(p + i0));
+        if (inside || (i0 >= 0 && i0 + E <= V)) return *reinterpret_cast<const uint4*>(p + i0);
         uint32_t u[4];
 #pragma unroll
         for (int e = 0; e < E; e += 4 / (int)sizeof(T)) {
