@@ -177,6 +177,7 @@ def gemm_bf16_noalloc(d_x: int, d_w: int, d_y: int, M: int, N: int, K: int, stre
 
 
 _DTYPES = {"fp32": 0, "bf16": 1}
+SCORE_MAX_TOP = 32
 
 
 def _ops_check(rc: int) -> None:
@@ -195,6 +196,11 @@ def _c32(v: int) -> int:
     return v if -0x80000000 <= v <= 0x7FFFFFFF else -1
 
 
+def _c64(v: int) -> int:
+    """The same for 64 bits."""
+    return v if -(1 << 63) <= v < 1 << 63 else -1
+
+
 def ops_status(stream: int = 0) -> None:
     """Waits for ``stream``; raises S2D2Error(-5) if a bounded wait in a kernel of the stand-alone operators ran out, on any stream of
     the device, since this thread's last call (outputs are NaN then)."""
@@ -209,7 +215,7 @@ def mxfp4_sizes(rows: int, cols: int):
         return rows * blocks * 16, (rows + 127) // 128 * ((blocks + 3) // 4) * 512
     lib = load_library()
     a, b = C.c_int64(), C.c_int64()
-    _ops_check(lib.s2d2_mxfp4_sizes(rows, cols, C.byref(a), C.byref(b)))
+    _ops_check(lib.s2d2_mxfp4_sizes(_c64(rows), _c64(cols), C.byref(a), C.byref(b)))
     return a.value, b.value
 
 
@@ -217,13 +223,13 @@ def mxfp4_quantize(d_x: int, dtype: str, rows: int, cols: int, row_stride: int, 
     """codes, scales <- x [rows, cols] ("fp32" or "bf16", rows ``row_stride`` elements apart).  Raw device pointers;
     asynchronous on ``stream``."""
     lib = load_library()
-    _ops_check(lib.s2d2_mxfp4_quantize(d_x, _dtype(dtype), rows, cols, row_stride, d_codes, d_scales, stream))
+    _ops_check(lib.s2d2_mxfp4_quantize(d_x, _dtype(dtype), _c64(rows), _c64(cols), _c64(row_stride), d_codes, d_scales, stream))
 
 
 def mxfp4_dequantize(d_codes: int, d_scales: int, rows: int, cols: int, d_y: int, dtype: str, row_stride: int, stream: int = 0) -> None:
     """y [rows, cols] <- the values that codes and scales stand for.  Asynchronous."""
     lib = load_library()
-    _ops_check(lib.s2d2_mxfp4_dequantize(d_codes, d_scales, rows, cols, d_y, _dtype(dtype), row_stride, stream))
+    _ops_check(lib.s2d2_mxfp4_dequantize(d_codes, d_scales, _c64(rows), _c64(cols), d_y, _dtype(dtype), _c64(row_stride), stream))
 
 
 def mxfp4_gemm(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int, d_y: int, y_dtype: str, M: int, N: int, K: int,
@@ -231,7 +237,7 @@ def mxfp4_gemm(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int,
     """y[M, N] = scale * x[M, K] w[N, K]^T of two MXFP4 matrices, y "fp32" or "bf16".  Asynchronous."""
     lib = load_library()
     _ops_check(lib.s2d2_mxfp4_gemm(d_x_codes, d_x_scales, d_w_codes, d_w_scales, d_y, _dtype(y_dtype), _c32(M), _c32(N), _c32(K),
-                                   N if y_stride is None else y_stride, scale, stream))
+                                   _c64(N if y_stride is None else y_stride), scale, stream))
 
 
 def score_logits(d_logits: int, dtype: str, n_rows: int, vocab: int, row_stride: int, d_tokens: int = 0, top_k: int = 0, *,
@@ -240,8 +246,8 @@ def score_logits(d_logits: int, dtype: str, n_rows: int, vocab: int, row_stride:
     """Log probability and rank of one given token per row (int32), log-sum-exp, entropy and the ``top_k`` most probable tokens of
     device logits ("fp32" or "bf16").  Outputs are fp32 (ids and ranks int32); 0 leaves one out.  Asynchronous."""
     lib = load_library()
-    _ops_check(lib.s2d2_score_logits(d_logits, _dtype(dtype), n_rows, _c32(vocab), row_stride, d_tokens, _c32(top_k), d_logprob, d_rank, d_lse,
-                                     d_entropy, d_top_ids, d_top_logprobs, stream))
+    _ops_check(lib.s2d2_score_logits(d_logits, _dtype(dtype), _c64(n_rows), _c32(vocab), _c64(row_stride), d_tokens, _c32(top_k), d_logprob,
+                                     d_rank, d_lse, d_entropy, d_top_ids, d_top_logprobs, stream))
 
 
 def mxfp4_score_workspace(M: int, N: int, K: int) -> int:
@@ -257,8 +263,8 @@ def mxfp4_score(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int
     """Log probability of one token per row, log-sum-exp and entropy of the logits scale * x w^T (x [M, K] hidden rows, w [N, K]
     the head, both MXFP4) without the logits in memory.  ``d_ws``: mxfp4_score_workspace bytes.  Asynchronous."""
     lib = load_library()
-    _ops_check(lib.s2d2_mxfp4_score(d_x_codes, d_x_scales, d_w_codes, d_w_scales, _c32(M), _c32(N), _c32(K), scale, d_tokens, d_logprob, d_lse, d_entropy,
-                                    d_ws, ws_bytes, stream))
+    _ops_check(lib.s2d2_mxfp4_score(d_x_codes, d_x_scales, d_w_codes, d_w_scales, _c32(M), _c32(N), _c32(K), scale, d_tokens, d_logprob, d_lse,
+                                    d_entropy, d_ws, _c64(ws_bytes), stream))
 
 
 def debug_mxfp4_wait(limit_polls: int, withhold: bool = False) -> None:
@@ -446,18 +452,20 @@ class Engine:
     def score_pass(self, which: int, n_rows: int, tokens=None, top_k: int = 0):
         """Scores of the first ``n_rows`` logit rows of the last draft (which = 0) or verifier pass (1): a dict with "lse",
         "entropy", with ``tokens`` also "logprob" and "rank", with ``top_k`` also "top_ids" and "top_logprobs"."""
-        out = {"lse": np.zeros(n_rows, np.float32), "entropy": np.zeros(n_rows, np.float32)}
+        rows, k = max(0, _c32(n_rows)), top_k if 0 < top_k <= SCORE_MAX_TOP else 0       # others are refused by the call
+        out = {"lse": np.zeros(rows, np.float32), "entropy": np.zeros(rows, np.float32)}
         tok = None
         if tokens is not None:
-            tok = np.ascontiguousarray(tokens, dtype=np.int32).reshape(-1)
+            tok = np.asarray(tokens).reshape(-1)
             if tok.size != n_rows:
                 raise ValueError("one token per row")
-            out["logprob"], out["rank"] = np.zeros(n_rows, np.float32), np.zeros(n_rows, np.int32)
-        if top_k > 0:
-            out["top_ids"], out["top_logprobs"] = np.zeros((n_rows, top_k), np.int32), np.zeros((n_rows, top_k), np.float32)
+            tok = np.where((tok < 0) | (tok > 0x7FFFFFFF), -1, tok).astype(np.int32)     # outside of every vocabulary
+            out["logprob"], out["rank"] = np.zeros(rows, np.float32), np.zeros(rows, np.int32)
+        if k:
+            out["top_ids"], out["top_logprobs"] = np.zeros((rows, k), np.int32), np.zeros((rows, k), np.float32)
         ptr = lambda name: out[name].ctypes.data if name in out else None
-        self._check(self.lib.s2d2_score_pass(self._h, _c32(which), _c32(n_rows), None if tok is None else tok.ctypes.data, top_k, ptr("logprob"),
-                                             ptr("rank"), ptr("lse"), ptr("entropy"), ptr("top_ids"), ptr("top_logprobs")))
+        self._check(self.lib.s2d2_score_pass(self._h, _c32(which), _c32(n_rows), None if tok is None else tok.ctypes.data, _c32(top_k),
+                                             ptr("logprob"), ptr("rank"), ptr("lse"), ptr("entropy"), ptr("top_ids"), ptr("top_logprobs")))
         return out
 
     def debug_copy_logits(self, which: int, max_rows: int) -> np.ndarray:
