@@ -350,6 +350,8 @@ int s2d2_debug_pass_trace(s2d2_ctx* ctx, uint64_t* out, int64_t cap, int32_t* n_
  * the status word and returns normally, and the call returns S2D2_ERR_TIMEOUT; the context stays
  * usable.  With target == 0 the wait is satisfied at once and the call returns S2D2_OK. */
 int s2d2_debug_wait_timeout(s2d2_ctx* ctx, uint32_t target, uint32_t limit_polls);
+/* Leaves the device status word as a pass whose kernel gave up on a bounded wait does (0: as none). */
+int s2d2_debug_set_status(s2d2_ctx* ctx, int32_t word);
 
 /* y[M, N] = x[M, K] w[N, K]^T on device buffers, without any allocation.
  * (The paper has no counterpart: this is a service entry for hosts that must not
@@ -455,7 +457,9 @@ int s2d2_debug_mxfp4_wait(uint32_t limit_polls, int32_t withhold);
 
 /* s2d2_score_logits on the logits that the last draft pass (which = 0) or verifier pass (which = 1) of a context left
  * behind: rows as s2d2_debug_copy_logits lists them, n_rows of them from the first one on.  Host pointers; outputs
- * [n_rows] and [n_rows, top_k], each may be NULL as above.  Synchronous. */
+ * [n_rows] and [n_rows, top_k], each may be NULL as above.  Synchronous.  S2D2_ERR_STATE where there is no such pass or it
+ * failed; S2D2_ERR_TIMEOUT where the verifier pass gave up on a bounded wait (accept_and_commit reports it, too): the outputs mean
+ * nothing then. */
 int s2d2_score_pass(s2d2_ctx* ctx, int32_t which, int32_t n_rows, const int32_t* tokens, int32_t top_k, float* logprob,
                     int32_t* rank, float* lse, float* entropy, int32_t* top_ids, float* top_logprobs);
 

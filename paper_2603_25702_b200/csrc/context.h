@@ -122,6 +122,7 @@ struct s2d2_ctx {
     int *dsamp_h = nullptr, *dsamp_d = nullptr;    // draft sampling: per logit row position, Philox stream, step (pinned / device)
     float* score_d = nullptr;                      // s2d2_score_pass: tokens and outputs of up to max_logit_rows rows
     int n_draft_logit_rows = 0, n_verify_logit_rows = 0;
+    bool draft_logits_ok = false, verify_logits_ok = false;      // s2d2_score_pass: the last pass of the kind was launched and did not fail
     // The logits of a pass live in per-context buffers that the next pass of the same kind overwrites; the passes
     // are numbered so that a sequence whose rows have been overwritten is recognised (S2D2_ERR_STATE).
     unsigned long long draft_gen = 0, verify_gen = 0;

@@ -387,6 +387,7 @@ static int check_status(s2d2_ctx* c) {
     if (*c->h_status == 0) return S2D2_OK;
     const int code = *c->h_status;
     *c->h_status = 0;
+    c->verify_logits_ok = false;      // a verifier pass is not checked before the next synchronous call: it may have been that one
     cudaMemsetAsync(c->d_status, 0, 4, c->stream);
     gemm_reset_tickets(c);      // a split-K CTA that gave up took no ticket: start the next GEMM from clean counters
     FAIL(c, S2D2_ERR_TIMEOUT, "a kernel gave up on a bounded wait (results of this call are invalid; device status word " +
@@ -794,6 +795,7 @@ extern "C" int s2d2_draft_block(s2d2_ctx* c, int32_t n, const int32_t* ids, s2d2
     }
     if (pb.n_logit > c->max_logit_rows || pb.n_rows > c->max_rows) FAIL(c, S2D2_ERR_UNSUPPORTED, "pass too large");
     CUDA_TRY(c, cudaEventRecord(c->ev[0], c->stream));
+    c->draft_logits_ok = false;
     if ((rc = run_pass(c, pb, c->logits_draft))) return rc;
     if (c->dc.draft_mode == S2D2_DRAFT_SAMPLE) {      // Philox words of the logit rows, in row order
         int r = 0;
@@ -827,6 +829,7 @@ extern "C" int s2d2_draft_block(s2d2_ctx* c, int32_t n, const int32_t* ids, s2d2
     c->cnt.n_draft_passes++;
     c->cnt.n_rows_draft += pb.n_rows;
     c->n_draft_logit_rows = pb.n_logit;
+    c->draft_logits_ok = true;
     for (int i = 0; i < n; ++i) {
         SeqState& s = c->seqs[ids[i]];
         s2d2_draft_stats& o = out[i];
@@ -1024,7 +1027,9 @@ extern "C" int s2d2_verify_block(s2d2_ctx* c, int32_t n, const int32_t* ids, con
     c->n_verify_logit_rows = pb.n_logit;
     if (pb.n_rows == 0) return S2D2_OK;
     CUDA_TRY(c, cudaEventRecord(c->ev[2], c->stream));
+    c->verify_logits_ok = false;
     if ((rc = run_pass(c, pb, c->logits_verify))) return rc;
+    c->verify_logits_ok = true;
     CUDA_TRY(c, cudaEventRecord(c->ev[3], c->stream));
     c->verify_timing_pending = true;
     c->cnt.n_verify_passes++;
@@ -1341,6 +1346,7 @@ extern "C" int s2d2_score_pass(s2d2_ctx* c, int32_t which, int32_t n_rows, const
     if (top_k < 0 || top_k > S2D2_SCORE_MAX_TOP) FAIL(c, S2D2_ERR_INVALID, "score_pass: top_k must be in 0..32");
     if ((logprob || rank) && !tokens) FAIL(c, S2D2_ERR_INVALID, "score_pass: log probability and rank need tokens");
     if (n_rows == 0) return S2D2_OK;
+    if (!(which == 0 ? c->draft_logits_ok : c->verify_logits_ok)) FAIL(c, S2D2_ERR_STATE, "score_pass: the last pass of this kind failed");
     const size_t R = n_rows, cap = c->max_logit_rows;
     int32_t* d_tok = (int32_t*)c->score_d;
     float* d_out = c->score_d + cap;      // logprob, rank, lse, entropy, ids, log probabilities of the alternatives
@@ -1366,7 +1372,13 @@ extern "C" int s2d2_score_pass(s2d2_ctx* c, int32_t which, int32_t n_rows, const
             CUDA_TRY(c, cudaMemcpyAsync(b.to, b.from, b.n * 4, cudaMemcpyDeviceToHost, c->stream));
             c->cnt.d2h_bytes += b.n * 4;
         }
+    // A verifier pass is asynchronous: whether it gave up on a wait is known here for the first time. The word stays raised, so that
+    // accept_and_commit sees it, too.
+    int rc2;
+    if (which == 1 && (rc2 = enqueue_status_read(c))) return rc2;
     CUDA_TRY(c, cudaStreamSynchronize(c->stream));
+    if (which == 1 && *c->h_status)
+        FAIL(c, S2D2_ERR_TIMEOUT, "score_pass: a kernel of the verifier pass gave up on a bounded wait (its logits are invalid)");
     return S2D2_OK;
 }
 
@@ -1638,4 +1650,11 @@ extern "C" int s2d2_debug_wait_timeout(s2d2_ctx* c, uint32_t target, uint32_t li
     }
     cudaFree(word);
     return rc;
+}
+
+extern "C" int s2d2_debug_set_status(s2d2_ctx* c, int32_t word) {
+    if (!c) return S2D2_ERR_INVALID;
+    CUDA_TRY(c, cudaStreamSynchronize(c->stream));
+    CUDA_TRY(c, cudaMemcpy(c->d_status, &word, 4, cudaMemcpyHostToDevice));
+    return S2D2_OK;
 }
