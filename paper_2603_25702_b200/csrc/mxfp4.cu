@@ -116,7 +116,7 @@ __device__ __forceinline__ void e2m1x8_values(uint32_t codes, float* v) {
 // number of instructions (15 per element took 31 us for 12288 x 4096 bf16, about 7 take the time of the copy).  Rows that are not
 // aligned to 16 bytes, and a row's end, go through shared memory: 32 consecutive elements per load (loads of each thread's own eight
 // took three times as long).  Rows that pad the last scale tile get zeros.
-// WHOLE: every warp's elements are whole and aligned (the other path costs registers: 42 us instead of 39).
+// WHOLE: every warp's elements are whole and aligned (the other path costs registers: 42 us both ways instead of 38).
 template <typename T, int STEPS, bool WHOLE>
 __global__ void __launch_bounds__(QT) quantize_kernel(const QuantParams p) {
     __shared__ alignas(16) T staged[WHOLE ? 1 : QROWS][2 * QUAD];
@@ -275,8 +275,8 @@ int elementwise(const char* op, bool inverse, const void* x, int dtype, long lon
     p.scales = (uint8_t*)const_cast<void*>(scales);
     p.vec = ((uintptr_t)x & 15) == 0 && (ld * size) % 16 == 0;
     const long long row_blocks = ((inverse ? rows : (rows + 127) / 128 * 128) + QROWS - 1) / QROWS;      // at most 2^19
-    // four steps per warp once that many blocks fill the GPU (12288 x 4096 bf16: 20 us each way);
-    // one step for small matrices (333 x 2049 fp32, both ways: 8 us, 11 us with four)
+    // four steps per warp once that many blocks fill the GPU (12288 x 4096 bf16, both ways: 38 us, 57 with one);
+    // one step for small matrices (333 x 2049 fp32, both ways: 3.4 us, 4.8 with four)
     const int steps = row_blocks * ((p.quads + 7) / 8) >= 8LL * dev->n_sms ? 4 : 1;
     const dim3 grid((unsigned)row_blocks, (unsigned)((p.quads + 2 * steps - 1) / (2 * steps)));           // at most 2^12 along y
     const bool whole = p.vec && cols % (steps * 2 * QUAD) == 0;

@@ -458,7 +458,7 @@ __device__ __forceinline__ void all_nan(const Params& p, int cluster, int cluste
 // shared memory, where every CTA sums its share of the rows over the cluster in rank order: deterministic, no
 // workspace, no tickets, nothing that two launches could share.
 // Measured (B200): a head of 151936 x 4096 against 8 rows 57 us (330 MB at 5.8 TB/s); 1024 x 24576 x 4096, with the quantisation of the
-// rows, 46 us (52 with T = 192, 65 with T = 128; 55 in a long loop); scores of 1024 rows against the head 221 us (5.8 PFLOP/s; 4.9 in
+// rows, 46 us (52 with T = 192, 65 with T = 128; 55 in a long loop); scores of 1024 rows against the head 225 us (5.7 PFLOP/s; 4.8 in
 // a long loop, at the power limit; its MMAs alone 194 us).
 // Every wait on a barrier is bounded; after a time-out all outputs of the cluster are NaN and it is counted.
 // NQ: groups of 32 columns that an epilogue warp holds; with one (T <= 64) two CTAs fit on an SM by their registers.
