@@ -455,6 +455,100 @@ int s2d2_mxfp4_score(const void* d_x_codes, const void* d_x_scales, const void* 
  * raises the status. */
 int s2d2_debug_mxfp4_wait(uint32_t limit_polls, int32_t withhold);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Stand-alone operators: the attention block of a layer, for hosts that run a model of their own.  The conventions of the
+ * operators above hold: device pointers unless a struct or a name without d_ says otherwise, asynchronous, nothing kept
+ * between calls, nothing allocated, capturable.  The structs below are read during the call only.
+ *
+ * Positions.  A pair of elements of a head turns by the angle position * d_freqs[i], i < rot_dim / 2, (computed in 64 bits) and
+ * is multiplied by `scale`.  Pairs are (i, i + rot_dim / 2) (S2D2_ROPE_HALF) or (2 i, 2 i + 1) (S2D2_ROPE_INTERLEAVED); elements from
+ * rot_dim on are left as they are.  With a gain (fp32 [head_dim]) the head is first divided by sqrt(mean x^2 + eps) and
+ * multiplied by it.  Arithmetic in fp32, one rounding at the end. */
+enum { S2D2_ROPE_HALF = 0, S2D2_ROPE_INTERLEAVED = 1 };
+enum { S2D2_ROPE_SCALING_NONE = 0, S2D2_ROPE_SCALING_LINEAR = 1, S2D2_ROPE_SCALING_NTK = 2, S2D2_ROPE_SCALING_YARN = 3, S2D2_ROPE_SCALING_BANDS = 4 };
+#define S2D2_ROPE_MAX_DIM 512            /* head_dim and rot_dim                     */
+#define S2D2_MAX_HEADS 4096
+#define S2D2_MAX_PAGE_TOKENS 1048576
+typedef struct {
+    const double* d_freqs;      /* [rot_dim / 2] radians per position; may be NULL with rot_dim = 0 (norm only) */
+    const float* d_q_gain;      /* NULL: no norm of the queries                  */
+    const float* d_k_gain;      /* NULL: no norm of the keys                     */
+    int32_t rot_dim;            /* even, 0..head_dim                             */
+    int32_t layout;             /* S2D2_ROPE_HALF | S2D2_ROPE_INTERLEAVED        */
+    float scale;
+    float eps;                  /* >= 0                                          */
+} s2d2_rope;
+
+/* Frequencies and scale of rotary positions for s2d2_rope, on the HOST (copy the frequencies to the device once).
+ * With f_i = base^(-2 i / rot_dim), s = factor, L = original_len (tokens the model was trained on):
+ *   NONE f_i   LINEAR f_i / s   NTK the same formula with base * s^(rot_dim / (rot_dim - 2))
+ *   YARN f_i / s * r + f_i (1 - r), r the ramp from 0 to 1 over pair indices from d(turns_fast), rounded down and at least 0, to
+ *        d(turns_slow), rounded up and at most rot_dim - 1, d(t) = rot_dim ln(L / (2 pi t)) / (2 ln base); *scale = 0.1 ln s + 1
+ *   BANDS the same blend with r = 1 - (L f_i / (2 pi) - turns_slow) / (turns_fast - turns_slow), cut to 0..1
+ * *scale is 1 except for YARN.  rot_dim even, 2..S2D2_ROPE_MAX_DIM; base > 1; factor >= 1; L > 0 and
+ * turns_fast > turns_slow > 0 where they are used; NTK needs rot_dim > 2. */
+int s2d2_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len, double turns_fast,
+                          double turns_slow, double* freqs, float* scale);
+
+/* q_out, k_out <- q, k [n_rows, heads, head_dim] normed and rotated.  Elements of a head and heads of a row are contiguous, rows
+ * *_stride elements apart; dtype S2D2_DTYPE_* of inputs and outputs; any alignment of the type (16 bytes, and head_dim and rot_dim multiples
+ * of 16, are faster).  q_out = q and k_out = k (same stride) work in place.  d_pos [n_rows].  n_q_heads or n_k_heads may be 0 (its pointers
+ * are not looked at). */
+int s2d2_qk_rope(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride, int32_t n_q_heads, const void* d_k,
+                 int64_t k_stride, void* d_k_out, int64_t k_out_stride, int32_t n_k_heads, int32_t dtype, int64_t n_rows,
+                 int32_t head_dim, const int32_t* d_pos, const s2d2_rope* rope, void* cuda_stream);
+
+/* The rows (new tokens) of a batch.  Lengths and page lists are on the device: a captured graph may run with others.
+ * Sequence s has rows d_row0[s] .. d_row0[s + 1] - 1 (none is allowed); with them its cache holds d_kv_len[s] tokens: row i of its n rows stands at
+ * cache index d_kv_len[s] - n + i.  Index j is token j % page_tokens of page d_pages[s * max_pages + j / page_tokens]; entries behind the
+ * last used one are not looked at.  Rows behind d_row0[n_seqs] pad the batch: their outputs are left as they were.
+ * d_row0 must not decrease and must stay within 0..n_rows: a sequence for which it does not has no rows.  A d_kv_len outside
+ * 0..max_pages * page_tokens, or a page outside 0..n_pages - 1, is not followed (see the calls). */
+typedef struct {
+    const int32_t* d_row0;      /* [n_seqs + 1]                                  */
+    const int32_t* d_kv_len;    /* [n_seqs]                                      */
+    const int32_t* d_pages;     /* [n_seqs, max_pages]                           */
+    int32_t n_rows, n_seqs, max_pages;
+    int32_t max_rows;           /* most rows of a sequence, as far as the host knows (1..n_rows): decides speed, not results */
+} s2d2_rows;
+
+/* A paged cache of one layer in bf16.  Element e of token t of head h of page p is d_k[p * page_stride + h * head_stride +
+ * t * token_stride + e], and the same of d_v: tokens of a head or heads of a token may be the neighbours, and keys and values may share a
+ * buffer.  d_k, d_v 16-byte aligned, strides multiples of 8, head_dim a multiple of 8; page_tokens a power of two, 8..S2D2_MAX_PAGE_TOKENS. */
+typedef struct {
+    void* d_k;
+    void* d_v;
+    int64_t page_stride, head_stride, token_stride;
+    int32_t n_pages, page_tokens, n_kv_heads, head_dim;
+} s2d2_paged_kv;
+
+/* Cache <- k (normed, rotated) and v [n_rows, n_kv_heads, head_dim] of the batch's rows, and q_out <- q normed and rotated (bf16; d_q NULL or n_q_heads 0:
+ * none).  Inputs of dtype S2D2_DTYPE_*, layout as in s2d2_qk_rope.  Position of a row: d_pos[row], or its cache index (d_pos NULL).
+ * rope NULL: no norm, no rotation.  A row whose cache index is negative, or whose page is not one, is not written to the cache (its q_out
+ * is).  Two rows must not have the same place in the cache. */
+int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride, int32_t n_q_heads, const void* d_k,
+                   int64_t k_stride, const void* d_v, int64_t v_stride, int32_t dtype, const int32_t* d_pos, const s2d2_rope* rope,
+                   const s2d2_rows* rows, const s2d2_paged_kv* kv, void* cuda_stream);
+
+/* out[row, h] <- softmax over the visible keys of (scale q[row, h] . k) times the values, q and out [n_rows, n_q_heads, head_dim] bf16,
+ * rows *_stride elements apart (16-byte aligned, strides multiples of 8); head h reads kv head h / (n_q_heads / n_kv_heads);
+ * d_lse [n_rows, n_q_heads] (may be NULL) <- log sum exp of its scores.  head_dim up to 128.  scale > 0.
+ * Visible to row i of n (the cache holds kv tokens, the row's index is p = kv - n + i):
+ *   mask_block = 1     j <= p (causal)
+ *   mask_block = B > 1 j < min(kv, (p / B + 1) B): whole blocks of B
+ *   mask_block = 0     all kv tokens
+ *   d_row_mask given   (mask_block must be 0) all tokens in front of the sequence's rows, and row b < min(n, 64) of them if bit b of
+ *                      d_row_mask[row] is set
+ * A row that sees nothing (or only scores of -inf) gets 0 and lse -inf; keys and values that a row does not see have no influence on it, NaN
+ * and infinities included.  Scores, sums and maxima are fp32; probabilities are rounded to bf16 for the product with the
+ * values.  A kv length that is not followed makes the sequence's rows NaN, a page that is not one makes rows NaN that look at its tokens.
+ * d_ws: at least s2d2_paged_attention_workspace bytes (they depend on the fields of the structs, not on what is on the device),
+ * 16-byte aligned, used by this call alone while it runs, whatever it holds. */
+int s2d2_paged_attention_workspace(const s2d2_rows* rows, const s2d2_paged_kv* kv, int32_t n_q_heads, int64_t* bytes);
+int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_out, int64_t out_stride, float* d_lse, int32_t n_q_heads,
+                         const s2d2_rows* rows, const s2d2_paged_kv* kv, int32_t mask_block, const uint64_t* d_row_mask, float scale,
+                         void* d_ws, int64_t ws_bytes, void* cuda_stream);
+
 /* s2d2_score_logits on the logits that the last draft pass (which = 0) or verifier pass (which = 1) of a context left
  * behind: rows as s2d2_debug_copy_logits lists them, n_rows of them from the first one on.  Host pointers; outputs
  * [n_rows] and [n_rows, top_k], each may be NULL as above.  Synchronous.  S2D2_ERR_STATE where there is no such pass or it

@@ -4,10 +4,14 @@ an ``Engine`` does, and fails loudly if the library is missing."""
 from .binding import (  # noqa: F401
     DraftStats,
     Engine,
+    PagedKV,
+    Rope,
     RoutePolicy,
+    Rows,
     S2D2Error,
     StepResult,
     gemm_bf16_noalloc,
+    kv_append,
     library_path,
     load_library,
     mxfp4_dequantize,
@@ -17,5 +21,9 @@ from .binding import (  # noqa: F401
     mxfp4_score_workspace,
     mxfp4_sizes,
     ops_status,
+    paged_attention,
+    paged_attention_workspace,
+    qk_rope,
+    rope_frequencies,
     score_logits,
 )

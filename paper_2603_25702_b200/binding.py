@@ -72,6 +72,41 @@ class RoutePolicy(C.Structure):
                 ("dynamic_cost", C.c_int32), ("alpha_entropy", C.c_int32), ("alpha_param", C.c_float)]
 
 
+class Rope(C.Structure):
+    """Rotary positions (and norms) for qk_rope and kv_append: device pointers to the frequencies (fp64 [rot_dim / 2], see
+    rope_frequencies) and, where heads are normed, to the gains (fp32 [head_dim]); ``layout`` "half" or "interleaved"."""
+    _fields_ = [("d_freqs", C.c_void_p), ("d_q_gain", C.c_void_p), ("d_k_gain", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32),
+                ("scale", C.c_float), ("eps", C.c_float)]
+
+    def __init__(self, d_freqs: int, rot_dim: int, layout: str = "half", scale: float = 1.0, *, d_q_gain: int = 0, d_k_gain: int = 0,
+                 eps: float = 1e-6):
+        if layout not in _LAYOUTS:
+            raise S2D2Error(-1, f"layout must be 'half' or 'interleaved', not {layout!r}")
+        super().__init__(d_freqs, d_q_gain, d_k_gain, _c32(rot_dim), _LAYOUTS[layout], scale, eps)
+
+
+class Rows(C.Structure):
+    """The rows (new tokens) of a batch: device pointers to row0 [n_seqs + 1], kv_len [n_seqs] and page lists [n_seqs, max_pages],
+    all int32 (semantics: include/s2d2.h).  ``max_rows``: most rows of a sequence, as far as the host knows (default: n_rows)."""
+    _fields_ = [("d_row0", C.c_void_p), ("d_kv_len", C.c_void_p), ("d_pages", C.c_void_p), ("n_rows", C.c_int32), ("n_seqs", C.c_int32),
+                ("max_pages", C.c_int32), ("max_rows", C.c_int32)]
+
+    def __init__(self, n_rows: int, n_seqs: int, d_row0: int, d_kv_len: int, d_pages: int, max_pages: int, max_rows: Optional[int] = None):
+        super().__init__(d_row0, d_kv_len, d_pages, _c32(n_rows), _c32(n_seqs), _c32(max_pages), _c32(n_rows if max_rows is None else max_rows))
+
+
+class PagedKV(C.Structure):
+    """A paged bf16 cache of one layer: element e of token t of head h of page p at p * page_stride + h * head_stride + t *
+    token_stride + e behind each of the device pointers (strides in elements)."""
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+    def __init__(self, d_k: int, d_v: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, *, page_stride: int,
+                 head_stride: int, token_stride: int):
+        super().__init__(d_k, d_v, _c64(page_stride), _c64(head_stride), _c64(token_stride), _c32(n_pages), _c32(page_tokens),
+                         _c32(n_kv_heads), _c32(head_dim))
+
+
 ROUTE_FN = C.CFUNCTYPE(C.c_int, C.c_void_p, C.POINTER(DraftStats))
 
 EXPORTS = [
@@ -84,6 +119,7 @@ EXPORTS = [
     "s2d2_ops_last_error", "s2d2_ops_status", "s2d2_mxfp4_sizes", "s2d2_mxfp4_quantize", "s2d2_mxfp4_dequantize",
     "s2d2_mxfp4_gemm", "s2d2_mxfp4_score_workspace", "s2d2_mxfp4_score", "s2d2_score_logits", "s2d2_score_pass",
     "s2d2_debug_mxfp4_wait",
+    "s2d2_rope_frequencies", "s2d2_qk_rope", "s2d2_kv_append", "s2d2_paged_attention_workspace", "s2d2_paged_attention",
 ]
 _TEXTS = ("s2d2_last_error", "s2d2_noalloc_last_error", "s2d2_ops_last_error")     # these return a string
 
@@ -156,6 +192,14 @@ def load_library() -> C.CDLL:
     lib.s2d2_mxfp4_score.argtypes = [C.c_void_p] * 4 + [C.c_int32] * 3 + [C.c_float] + [C.c_void_p] * 5 + [C.c_int64, C.c_void_p]
     lib.s2d2_score_logits.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_int32] + [C.c_void_p] * 7
     lib.s2d2_debug_mxfp4_wait.argtypes = [C.c_uint32, C.c_int32]
+    ptr = C.c_void_p
+    lib.s2d2_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [ptr, C.POINTER(C.c_float)]
+    lib.s2d2_qk_rope.argtypes = [ptr, C.c_int64, ptr, C.c_int64, C.c_int32] * 2 + [C.c_int32, C.c_int64, C.c_int32, ptr, C.POINTER(Rope), ptr]
+    lib.s2d2_kv_append.argtypes = [ptr, C.c_int64, ptr, C.c_int64, C.c_int32, ptr, C.c_int64, ptr, C.c_int64, C.c_int32, ptr,
+                                   C.POINTER(Rope), C.POINTER(Rows), C.POINTER(PagedKV), ptr]
+    lib.s2d2_paged_attention_workspace.argtypes = [C.POINTER(Rows), C.POINTER(PagedKV), C.c_int32, C.POINTER(C.c_int64)]
+    lib.s2d2_paged_attention.argtypes = [ptr, C.c_int64, ptr, C.c_int64, ptr, C.c_int32, C.POINTER(Rows), C.POINTER(PagedKV), C.c_int32, ptr,
+                                         C.c_float, ptr, C.c_int64, ptr]
     lib.s2d2_score_pass.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32] + [C.c_void_p] * 6
     _LIB = lib
     return lib
@@ -178,6 +222,8 @@ def gemm_bf16_noalloc(d_x: int, d_w: int, d_y: int, M: int, N: int, K: int, stre
 
 
 _DTYPES = {"fp32": 0, "bf16": 1}
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
 SCORE_MAX_TOP = 32
 
 
@@ -266,6 +312,64 @@ def mxfp4_score(d_x_codes: int, d_x_scales: int, d_w_codes: int, d_w_scales: int
     lib = load_library()
     _ops_check(lib.s2d2_mxfp4_score(d_x_codes, d_x_scales, d_w_codes, d_w_scales, _c32(M), _c32(N), _c32(K), scale, d_tokens, d_logprob, d_lse,
                                     d_entropy, d_ws, _c64(ws_bytes), stream))
+
+
+def rope_frequencies(rot_dim: int, base: float, scaling: str = "none", *, factor: float = 1.0, original_len: float = 0.0,
+                     turns_fast: float = 32.0, turns_slow: float = 1.0):
+    """(radians per position of each pair as fp64 [rot_dim / 2] on the host, scale) for Rope; ``scaling`` "none", "linear", "ntk", "yarn" or
+    "bands" (formulas: include/s2d2.h)."""
+    lib = load_library()
+    if scaling not in _SCALINGS:
+        raise S2D2Error(-1, f"scaling must be one of {', '.join(_SCALINGS)}, not {scaling!r}")
+    freqs = np.zeros(rot_dim // 2 if 2 <= rot_dim <= 512 else 0, dtype=np.float64)      # other sizes are refused before anything is written
+    scale = C.c_float()
+    _ops_check(lib.s2d2_rope_frequencies(_c32(rot_dim), base, _SCALINGS[scaling], factor, original_len, turns_fast, turns_slow, freqs.ctypes.data,
+                                         C.byref(scale)))
+    return freqs, scale.value
+
+
+def qk_rope(d_q: int, d_q_out: int, n_q_heads: int, d_k: int, d_k_out: int, n_k_heads: int, dtype: str, n_rows: int, head_dim: int, d_pos: int,
+            rope: Rope, *, q_stride: Optional[int] = None, q_out_stride: Optional[int] = None, k_stride: Optional[int] = None,
+            k_out_stride: Optional[int] = None, stream: int = 0) -> None:
+    """q_out, k_out <- q, k [n_rows, heads, head_dim] ("fp32" or "bf16", rows *_stride elements apart, default contiguous), each head normed
+    (where ``rope`` has a gain) and rotated by the row's position (int32).  In place with equal pointers and strides.  Asynchronous."""
+    lib = load_library()
+    wide = lambda given, heads: _c64(heads * head_dim if given is None else given)
+    _ops_check(lib.s2d2_qk_rope(d_q, wide(q_stride, n_q_heads), d_q_out, wide(q_out_stride, n_q_heads), _c32(n_q_heads), d_k,
+                                wide(k_stride, n_k_heads), d_k_out, wide(k_out_stride, n_k_heads), _c32(n_k_heads), _dtype(dtype), _c64(n_rows),
+                                _c32(head_dim), d_pos, rope, stream))
+
+
+def kv_append(d_k: int, d_v: int, dtype: str, rows: Rows, kv: PagedKV, rope: Optional[Rope] = None, *, k_stride: Optional[int] = None,
+              v_stride: Optional[int] = None, d_pos: int = 0, d_q: int = 0, d_q_out: int = 0, n_q_heads: int = 0, q_stride: Optional[int] = None,
+              q_out_stride: Optional[int] = None, stream: int = 0) -> None:
+    """Cache <- keys (normed and rotated as ``rope`` says) and values of the batch's rows; with ``d_q`` also q_out (bf16) <- queries, normed and
+    rotated.  Positions: ``d_pos`` (int32), or the rows' cache indices.  Asynchronous."""
+    lib = load_library()
+    wide = lambda given, heads: _c64(heads * kv.head_dim if given is None else given)
+    _ops_check(lib.s2d2_kv_append(d_q, wide(q_stride, n_q_heads), d_q_out, wide(q_out_stride, n_q_heads), _c32(n_q_heads), d_k,
+                                  wide(k_stride, kv.n_kv_heads), d_v, wide(v_stride, kv.n_kv_heads), _dtype(dtype), d_pos, rope, rows, kv, stream))
+
+
+def paged_attention_workspace(rows: Rows, kv: PagedKV, n_q_heads: int) -> int:
+    """Bytes of workspace that paged_attention needs."""
+    lib = load_library()
+    n = C.c_int64()
+    _ops_check(lib.s2d2_paged_attention_workspace(rows, kv, _c32(n_q_heads), C.byref(n)))
+    return n.value
+
+
+def paged_attention(d_q: int, d_out: int, n_q_heads: int, rows: Rows, kv: PagedKV, d_ws: int, ws_bytes: int, *, mask_block: int = 1,
+                    d_row_mask: int = 0, scale: Optional[float] = None, d_lse: int = 0, q_stride: Optional[int] = None,
+                    out_stride: Optional[int] = None, stream: int = 0) -> None:
+    """out <- attention of the batch's rows over the cache, q and out bf16 [n_rows, n_q_heads, head_dim].  ``mask_block``: 1 causal, B whole
+    blocks of B, 0 all tokens, or 0 with ``d_row_mask`` (uint64 per row over the sequence's own rows).  ``scale`` defaults to
+    head_dim^-0.5; ``d_lse`` fp32 [n_rows, n_q_heads].  Asynchronous."""
+    lib = load_library()
+    width = n_q_heads * kv.head_dim
+    _ops_check(lib.s2d2_paged_attention(d_q, _c64(width if q_stride is None else q_stride), d_out, _c64(width if out_stride is None else out_stride),
+                                        d_lse, _c32(n_q_heads), rows, kv, _c32(mask_block), d_row_mask,
+                                        kv.head_dim ** -0.5 if scale is None else scale, d_ws, _c64(ws_bytes), stream))
 
 
 def debug_mxfp4_wait(limit_polls: int, withhold: bool = False) -> None:

@@ -8,7 +8,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libs2d2.so")
-SOURCES = ["s2d2_api.cu", "gemm.cu", "attention.cu", "pass.cu", "ops.cu", "scores.cu", "mxfp4.cu"]
+SOURCES = ["s2d2_api.cu", "gemm.cu", "attention.cu", "pass.cu", "ops.cu", "scores.cu", "mxfp4.cu", "rope.cu", "paged_attention.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 

@@ -52,7 +52,8 @@ int device(const Device** out) {
             if ((e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q)) != cudaSuccess || !fn)
                 return fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
             d.encode = (EncodeTiledFn)fn;
-            if ((e = load_score_kernels()) != cudaSuccess || (e = load_mxfp4_kernels()) != cudaSuccess) {
+            if ((e = load_score_kernels()) != cudaSuccess || (e = load_mxfp4_kernels()) != cudaSuccess ||
+                (e = load_rope_kernels()) != cudaSuccess || (e = load_attention_kernels()) != cudaSuccess) {
                 cudaGetLastError();
                 return fail(S2D2_ERR_CUDA, "loading the kernels: %s", cudaGetErrorString(e));
             }

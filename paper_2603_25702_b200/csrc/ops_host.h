@@ -1,4 +1,4 @@
-// Host side shared by the stand-alone operators (scores.cu, mxfp4.cu): error text, argument checks, launches.
+// Host side shared by the stand-alone operators (scores.cu, mxfp4.cu, rope.cu, paged_attention.cu): error text, argument checks, launches.
 //
 // These operators keep nothing between calls: no context, no scratch of their own.  Two calls may run at the same
 // time on different streams or in different captured graphs, and every call is asynchronous.
@@ -33,6 +33,8 @@ struct Device {
 int device(const Device** out);
 cudaError_t load_score_kernels();      // scores.cu
 cudaError_t load_mxfp4_kernels();      // mxfp4.cu
+cudaError_t load_rope_kernels();       // rope.cu
+cudaError_t load_attention_kernels();  // paged_attention.cu
 
 // Loads a kernel and allows it `smem` bytes of dynamic shared memory.
 template <typename... P>

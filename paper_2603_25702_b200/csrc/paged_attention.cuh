@@ -1,0 +1,114 @@
+// Attention of new rows over a paged cache, row by row.
+#pragma once
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace s2d2 {
+namespace patt {
+
+struct Params {
+    paged::Batch b;
+    paged::Cache c;
+    const bf16* q;
+    bf16* out;
+    float* lse;                      // may be null
+    long long q_ld, out_ld;
+    const unsigned long long* row_mask;
+    int mask_block, heads, kv_heads, group, head_dim;
+    float scale_log2;                // scale / ln 2: exponentials are powers of two
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {      // relative error 2^-22; below 2^-126 zero
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
+        s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+    }
+    return s;
+}
+
+// Maximum (times scale_log2), sum and weighted values of one (row, head) over the keys [k0, k1), by a warp: a lane takes a key's
+// score, then every lane takes the elements lane, lane + 32, .. of the values.  Keys that are not seen are not read.
+struct RowSum {
+    float m, l, o[4];
+};
+__device__ __forceinline__ RowSum row_sum(const Params& p, int seq, int kv, int kvh, const bf16* q, const paged::View& view, int k0, int k1) {
+    const int lane = threadIdx.x & 31;
+    RowSum a;
+    a.m = -INFINITY;
+    a.l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a.o[i] = 0.f;
+    const long long head = (long long)kvh * p.c.head_stride;
+    for (int j0 = k0; j0 < k1; j0 += 32) {
+        const int j = j0 + lane;
+        const bool seen = j < min(k1, kv) && view.sees(j);
+        long long at = -1;
+        float s = -INFINITY;
+        if (seen) {
+            const int page = paged::page_of(p.b, seq, j);
+            if (page >= 0) {
+                at = page * p.c.page_stride + head + (j & p.c.page_mask) * p.c.token_stride;
+                s = 0.f;
+                for (int e = 0; e < p.head_dim; e += 8)
+                    s = dot8(*reinterpret_cast<const uint4*>(q + e), *reinterpret_cast<const uint4*>(p.c.k + at + e), s);
+                s *= p.scale_log2;
+            } else {
+                s = __int_as_float(0x7fffffff);
+            }
+        }
+        const float m = fmaxf(a.m, warp_max(s));         // passes NaN over
+        const float ref = m == -INFINITY ? 0.f : m;
+        const float shrink = exp2_fast(a.m - ref), e = exp2_fast(s - ref);      // (infinity - infinity: NaN, as it should be)
+        a.l = a.l * shrink + warp_sum(e);
+        a.m = m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.o[i] *= shrink;
+        for (int t = 0; t < 32; ++t) {
+            const float w = __shfl_sync(0xffffffffu, e, t);
+            const long long from = __shfl_sync(0xffffffffu, at, t);
+            if (w == 0.f) continue;                      // not seen, or nothing
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (lane + 32 * i < p.head_dim) a.o[i] = from < 0 ? w : fmaf(w, to_f32(p.c.v[from + lane + 32 * i]), a.o[i]);
+        }
+    }
+    return a;
+}
+
+// A warp per (row, head).
+__global__ void __launch_bounds__(128) rows_kernel(const Params p) {
+    pdl_wait();
+    pdl_launch();
+    const int lane = threadIdx.x & 31;
+    const long long tasks = (long long)p.b.n_rows * p.heads;
+    for (long long t = blockIdx.x * 4LL + (threadIdx.x >> 5); t < tasks; t += gridDim.x * 4LL) {
+        const int row = (int)(t / p.heads), h = (int)(t % p.heads);
+        const int seq = paged::find_seq(p.b, row);
+        if (seq < 0) continue;
+        const paged::Seq s = paged::read_seq(p.b, seq);
+        RowSum a;
+        if (s.ok) {
+            const paged::View view = paged::row_view(p.mask_block, p.row_mask, s, row - s.row0);
+            a = row_sum(p, seq, s.kv, h / p.group, p.q + row * p.q_ld + (long long)h * p.head_dim, view, 0, s.kv);
+        } else {
+            a.m = a.l = __int_as_float(0x7fffffff);
+        }
+        const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (lane + 32 * i < p.head_dim)
+                p.out[row * p.out_ld + (long long)h * p.head_dim + lane + 32 * i] = __float2bfloat16_rn(s.ok ? a.o[i] * inv : a.l);
+        if (p.lse && lane == 0) p.lse[(long long)row * p.heads + h] = a.l == 0.f ? -INFINITY : (a.m + log2f(a.l)) * 0.6931471805599453f;
+    }
+}
+
+}  // namespace patt
+}  // namespace s2d2
