@@ -120,6 +120,7 @@ EXPORTS = [
     "s2d2_mxfp4_gemm", "s2d2_mxfp4_score_workspace", "s2d2_mxfp4_score", "s2d2_score_logits", "s2d2_score_pass",
     "s2d2_debug_mxfp4_wait",
     "s2d2_rope_frequencies", "s2d2_qk_rope", "s2d2_kv_append", "s2d2_paged_attention_workspace", "s2d2_paged_attention",
+    "s2d2_debug_attention_wait",
 ]
 _TEXTS = ("s2d2_last_error", "s2d2_noalloc_last_error", "s2d2_ops_last_error")     # these return a string
 
@@ -200,6 +201,7 @@ def load_library() -> C.CDLL:
     lib.s2d2_paged_attention_workspace.argtypes = [C.POINTER(Rows), C.POINTER(PagedKV), C.c_int32, C.POINTER(C.c_int64)]
     lib.s2d2_paged_attention.argtypes = [ptr, C.c_int64, ptr, C.c_int64, ptr, C.c_int32, C.POINTER(Rows), C.POINTER(PagedKV), C.c_int32, ptr,
                                          C.c_float, ptr, C.c_int64, ptr]
+    lib.s2d2_debug_attention_wait.argtypes = [C.c_uint32, C.c_int32]
     lib.s2d2_score_pass.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32] + [C.c_void_p] * 6
     _LIB = lib
     return lib
@@ -377,6 +379,12 @@ def debug_mxfp4_wait(limit_polls: int, withhold: bool = False) -> None:
     do, because its codes are not loaded."""
     lib = load_library()
     _ops_check(lib.s2d2_debug_mxfp4_wait(limit_polls, int(withhold)))
+
+
+def debug_attention_wait(limit_polls: int, withhold: bool = False) -> None:
+    """Test tap: the same for this thread's next paged_attention."""
+    lib = load_library()
+    _ops_check(lib.s2d2_debug_attention_wait(limit_polls, int(withhold)))
 
 
 class Engine:

@@ -1,10 +1,15 @@
 // Attention of a batch's new rows over a paged cache: s2d2_paged_attention.
 #include <math.h>
 
-#include "paged_attention.cuh"
+#include "paged_attention_tc.cuh"
 
 namespace s2d2 {
 namespace {
+
+constexpr long long MAX_LEN = 1 << 30;      // tokens of a sequence, and query vectors of a kv head
+
+thread_local uint32_t g_wait_limit = tc::WAIT_LIMIT;
+thread_local int g_withhold = 0;
 
 int check_shape(const char* op, const s2d2_rows* rows, const s2d2_paged_kv* kv, int n_q_heads) {
     if (int rc = ops::check_rows(op, rows)) return rc;
@@ -12,13 +17,63 @@ int check_shape(const char* op, const s2d2_rows* rows, const s2d2_paged_kv* kv, 
     if (kv->head_dim > 128) return ops::fail(S2D2_ERR_UNSUPPORTED, "%s: head_dim must be at most 128", op);
     if (n_q_heads < 1 || n_q_heads > S2D2_MAX_HEADS || n_q_heads % kv->n_kv_heads)
         return ops::fail(S2D2_ERR_INVALID, "%s: n_q_heads must be a multiple of n_kv_heads, at most %d", op, S2D2_MAX_HEADS);
+    if ((long long)rows->n_rows * (n_q_heads / kv->n_kv_heads) > MAX_LEN)
+        return ops::fail(S2D2_ERR_UNSUPPORTED, "%s: n_rows * n_q_heads / n_kv_heads must be at most 2^30", op);
+    if ((long long)rows->max_pages * kv->page_tokens > MAX_LEN) return ops::fail(S2D2_ERR_UNSUPPORTED, "%s: max_pages * page_tokens must be at most 2^30", op);
     return S2D2_OK;
+}
+
+// How the work is cut, from what the host knows.
+struct Plan {
+    int hdp, ctas, stages, smem, control_at;
+    bool joins;                      // an item may be cut
+    long long ml_at, o_at, bytes;    // of the workspace
+};
+Plan make_plan(const s2d2_rows* rows, const s2d2_paged_kv* kv, int n_q_heads) {
+    Plan n;
+    n.hdp = kv->head_dim > 64 ? 128 : 64;
+    const long long group = n_q_heads / kv->n_kv_heads, most = std::max(1LL, ((long long)rows->max_pages * kv->page_tokens + patt::KEYS - 1) / patt::KEYS);
+    const long long items = (rows->n_rows * group + patt::QROWS - 1) / patt::QROWS + std::min(rows->n_seqs, rows->n_rows);
+    n.ctas = (int)std::min<long long>(patt::MAX_CTAS, items * most >= patt::MAX_CTAS ? patt::MAX_CTAS : items * most * kv->n_kv_heads);
+    n.joins = most > 1;
+    const int stage = patt::KEYS * n.hdp * 2, q = 2 * patt::QTILE * n.hdp * 2;
+    n.stages = std::min(patt::MAX_STAGES, (224 * 1024 - q) / stage);
+    n.control_at = q + n.stages * stage;
+    n.smem = 1024 + n.control_at + (int)sizeof(patt::Control);
+    n.ml_at = n.ctas * 32LL;
+    n.o_at = n.ml_at + (n.joins ? 2LL * n.ctas * patt::QROWS * 8 : 0);
+    n.bytes = n.o_at + (n.joins ? 2LL * n.ctas * patt::QROWS * n.hdp * 4 : 0);
+    return n;
+}
+
+// Keys or values of a layer as [page][head][token][element] in boxes of up to 128 tokens x 64 elements; elements behind the head's read as zero.
+int encode(const ops::Device* dev, CUtensorMap* map, const void* base, const s2d2_paged_kv* kv) {
+    cuuint64_t dims[4] = {(cuuint64_t)kv->head_dim, (cuuint64_t)kv->page_tokens, (cuuint64_t)kv->n_kv_heads, (cuuint64_t)kv->n_pages};
+    cuuint64_t strides[3] = {(cuuint64_t)kv->token_stride * 2, (cuuint64_t)kv->head_stride * 2, (cuuint64_t)kv->page_stride * 2};
+    cuuint32_t box[4] = {64, (cuuint32_t)std::min(kv->page_tokens, patt::KEYS), 1, 1}, step[4] = {1, 1, 1, 1};
+    const CUresult r = dev->encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step,
+                                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? S2D2_OK : ops::fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
+template <int HDP>
+cudaError_t launch_tiles(const CUtensorMap& map_k, const CUtensorMap& map_v, const patt::TileParams& t, const Plan& n, cudaStream_t st) {
+    cudaError_t e = ops::launch(patt::tile_kernel<HDP>, dim3(n.ctas), patt::THREADS, n.smem, 1, st, map_k, map_v, t);
+    if (!e && n.joins) e = ops::launch(patt::join_kernel<HDP>, dim3(n.ctas, patt::QROWS / 32), 256, 0, 1, st, t);
+    return e;
 }
 
 }  // namespace
 
 namespace ops {
-cudaError_t load_attention_kernels() { return load(patt::rows_kernel); }
+cudaError_t load_attention_kernels() {
+    constexpr int most = 227 * 1024;
+    cudaError_t e = load(patt::tile_kernel<64>, most);
+    if (!e) e = load(patt::tile_kernel<128>, most);
+    if (!e) e = load(patt::join_kernel<64>);
+    return e ? e : load(patt::join_kernel<128>);
+}
 }  // namespace ops
 }  // namespace s2d2
 
@@ -29,7 +84,7 @@ extern "C" int s2d2_paged_attention_workspace(const s2d2_rows* rows, const s2d2_
     const char* op = "paged_attention_workspace";
     if (!bytes) return ops::fail(S2D2_ERR_INVALID, "%s: bytes: null pointer", op);
     if (int rc = check_shape(op, rows, kv, n_q_heads)) return rc;
-    *bytes = 0;
+    *bytes = make_plan(rows, kv, n_q_heads).bytes;
     return S2D2_OK;
 }
 
@@ -45,14 +100,19 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     if (mask_block < 0) return ops::fail(S2D2_ERR_INVALID, "%s: mask_block must not be negative", op);
     if (d_row_mask && mask_block) return ops::fail(S2D2_ERR_INVALID, "%s: mask_block must be 0 with row masks", op);
     if (!(scale > 0.f) || !isfinite(scale)) return ops::fail(S2D2_ERR_INVALID, "%s: scale must be positive", op);
+    const Plan n = make_plan(rows, kv, n_q_heads);
+    const bool work = rows->n_rows && rows->n_seqs;
+    if (work && ws_bytes < n.bytes) return ops::fail(S2D2_ERR_INVALID, "%s: workspace of %lld bytes, needs %lld", op, (long long)ws_bytes, n.bytes);
     const ops::Device* dev;
     if (int rc = ops::device(&dev)) return rc;
-    if (rows->n_rows == 0 || rows->n_seqs == 0) return S2D2_OK;
-    patt::Params p = {};
+    if (!work) return S2D2_OK;
+    patt::TileParams t = {};
+    patt::Params& p = t.a;
     if (int rc = ops::device_rows(dev, op, rows, kv, &p.b)) return rc;
     if (int rc = ops::device_kv(dev, op, kv, &p.c)) return rc;
     if (int rc = ops::check_ptr(dev, d_q, 16, "q")) return rc;
     if (int rc = ops::check_ptr(dev, d_out, 16, "out")) return rc;
+    if (int rc = ops::check_ptr(dev, d_ws, 16, "workspace")) return rc;
     if (d_lse)
         if (int rc = ops::check_ptr(dev, d_lse, 4, "lse")) return rc;
     if (d_row_mask)
@@ -69,11 +129,37 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     p.group = n_q_heads / kv->n_kv_heads;
     p.head_dim = kv->head_dim;
     p.scale_log2 = scale * 1.4426950408889634f;
-    const long long tasks = (long long)p.b.n_rows * n_q_heads;
-    const cudaError_t e = ops::launch(patt::rows_kernel, dim3((unsigned)std::min<long long>((tasks + 3) / 4, 1 << 20)), 128, 0, 1, (cudaStream_t)cuda_stream, p);
+    CUtensorMap map_k, map_v;
+    if (int rc = encode(dev, &map_k, kv->d_k, kv)) return rc;
+    if (int rc = encode(dev, &map_v, kv->d_v, kv)) return rc;
+    t.ctas = n.ctas;
+    t.stages = n.stages;
+    t.control_at = n.control_at;
+    // threads per sequence when units are counted: as many as it may have items, as long as one round takes all sequences
+    t.seq_lanes = 1;
+    while (t.seq_lanes < 32 && t.seq_lanes * patt::QROWS < (long long)rows->max_rows * p.group && (long long)rows->n_seqs * t.seq_lanes * 2 <= patt::THREADS)
+        t.seq_lanes *= 2;
+    t.split = (int4*)d_ws;
+    t.part_ml = (float2*)((char*)d_ws + n.ml_at);
+    t.part_o = (float*)((char*)d_ws + n.o_at);
+    t.timeouts = dev->timeouts;
+    t.wait_limit = g_wait_limit;
+    t.withhold = g_withhold;
+    g_wait_limit = tc::WAIT_LIMIT;
+    g_withhold = 0;
+    const cudaError_t e = n.hdp == 128 ? launch_tiles<128>(map_k, map_v, t, n, (cudaStream_t)cuda_stream)
+                                       : launch_tiles<64>(map_k, map_v, t, n, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return ops::fail(S2D2_ERR_CUDA, "%s: %s", op, cudaGetErrorString(e));
     }
+    return S2D2_OK;
+}
+
+extern "C" int s2d2_debug_attention_wait(uint32_t limit_polls, int32_t withhold) {
+    ops::clear_error();
+    if (limit_polls < 1 || limit_polls > 1u << 20) return ops::fail(S2D2_ERR_INVALID, "debug_attention_wait: limit_polls must be in 1..2^20");
+    g_wait_limit = limit_polls;
+    g_withhold = withhold != 0;
     return S2D2_OK;
 }

@@ -1,4 +1,4 @@
-// Attention of new rows over a paged cache, row by row.
+// Attention of new rows over a paged cache: parameters, and one row by a warp.
 #pragma once
 #include <algorithm>
 
@@ -81,33 +81,6 @@ __device__ __forceinline__ RowSum row_sum(const Params& p, int seq, int kv, int 
         }
     }
     return a;
-}
-
-// A warp per (row, head).
-__global__ void __launch_bounds__(128) rows_kernel(const Params p) {
-    pdl_wait();
-    pdl_launch();
-    const int lane = threadIdx.x & 31;
-    const long long tasks = (long long)p.b.n_rows * p.heads;
-    for (long long t = blockIdx.x * 4LL + (threadIdx.x >> 5); t < tasks; t += gridDim.x * 4LL) {
-        const int row = (int)(t / p.heads), h = (int)(t % p.heads);
-        const int seq = paged::find_seq(p.b, row);
-        if (seq < 0) continue;
-        const paged::Seq s = paged::read_seq(p.b, seq);
-        RowSum a;
-        if (s.ok) {
-            const paged::View view = paged::row_view(p.mask_block, p.row_mask, s, row - s.row0);
-            a = row_sum(p, seq, s.kv, h / p.group, p.q + row * p.q_ld + (long long)h * p.head_dim, view, 0, s.kv);
-        } else {
-            a.m = a.l = __int_as_float(0x7fffffff);
-        }
-        const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (lane + 32 * i < p.head_dim)
-                p.out[row * p.out_ld + (long long)h * p.head_dim + lane + 32 * i] = __float2bfloat16_rn(s.ok ? a.o[i] * inv : a.l);
-        if (p.lse && lane == 0) p.lse[(long long)row * p.heads + h] = a.l == 0.f ? -INFINITY : (a.m + log2f(a.l)) * 0.6931471805599453f;
-    }
 }
 
 }  // namespace patt
