@@ -542,9 +542,9 @@ int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_o
  * A row that sees nothing (or only scores of -inf) gets 0 and lse -inf; keys and values that a row does not see have no influence on it, NaN
  * and infinities included.  Scores, sums and maxima are fp32; probabilities are rounded to bf16 for the product with the
  * values.  A kv length that is not followed makes the sequence's rows NaN, a page that is not one the rows that see its tokens (and rows next to
- * them may become NaN, too).  max_pages * page_tokens and n_rows * n_q_heads / n_kv_heads are at most 2^30.
+ * them may become NaN, too).  n_rows is at most 2^22, max_pages * page_tokens and n_rows * n_q_heads / n_kv_heads at most 2^30.
  * d_ws: at least s2d2_paged_attention_workspace bytes (they depend on the fields of the structs, not on what is on the device),
- * 16-byte aligned, used by this call alone while it runs, whatever it holds. */
+ * 32-byte aligned, used by this call alone while it runs, whatever it holds. */
 int s2d2_paged_attention_workspace(const s2d2_rows* rows, const s2d2_paged_kv* kv, int32_t n_q_heads, int64_t* bytes);
 int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_out, int64_t out_stride, float* d_lse, int32_t n_q_heads,
                          const s2d2_rows* rows, const s2d2_paged_kv* kv, int32_t mask_block, const uint64_t* d_row_mask, float scale,

@@ -6,6 +6,7 @@
 namespace s2d2 {
 namespace {
 
+constexpr int MAX_ROWS = 1 << 22;
 constexpr long long MAX_LEN = 1 << 30;      // tokens of a sequence, and query vectors of a kv head
 
 thread_local uint32_t g_wait_limit = tc::WAIT_LIMIT;
@@ -19,13 +20,14 @@ int check_shape(const char* op, const s2d2_rows* rows, const s2d2_paged_kv* kv, 
         return ops::fail(S2D2_ERR_INVALID, "%s: n_q_heads must be a multiple of n_kv_heads, at most %d", op, S2D2_MAX_HEADS);
     if ((long long)rows->n_rows * (n_q_heads / kv->n_kv_heads) > MAX_LEN)
         return ops::fail(S2D2_ERR_UNSUPPORTED, "%s: n_rows * n_q_heads / n_kv_heads must be at most 2^30", op);
+    if (rows->n_rows > MAX_ROWS) return ops::fail(S2D2_ERR_UNSUPPORTED, "%s: n_rows must be at most 2^22", op);
     if ((long long)rows->max_pages * kv->page_tokens > MAX_LEN) return ops::fail(S2D2_ERR_UNSUPPORTED, "%s: max_pages * page_tokens must be at most 2^30", op);
     return S2D2_OK;
 }
 
 // How the work is cut, from what the host knows.
 struct Plan {
-    int hdp, ctas, stages, smem, control_at;
+    int hdp, nh, ctas, stages, smem, control_at;
     bool joins;                      // an item may be cut
     long long ml_at, o_at, bytes;    // of the workspace
 };
@@ -33,16 +35,20 @@ Plan make_plan(const s2d2_rows* rows, const s2d2_paged_kv* kv, int n_q_heads) {
     Plan n;
     n.hdp = kv->head_dim > 64 ? 128 : 64;
     const long long group = n_q_heads / kv->n_kv_heads, most = std::max(1LL, ((long long)rows->max_pages * kv->page_tokens + patt::KEYS - 1) / patt::KEYS);
-    const long long items = (rows->n_rows * group + patt::QROWS - 1) / patt::QROWS + std::min(rows->n_seqs, rows->n_rows);
+    // items of 128 query vectors where no sequence has more, as far as the host knows
+    n.nh = rows->max_rows * group <= patt::QTILE ? 1 : 2;
+    const int per = patt::QTILE * n.nh;
+    const long long items = (rows->n_rows * group + per - 1) / per + std::min(rows->n_seqs, rows->n_rows);
     n.ctas = (int)std::min<long long>(patt::MAX_CTAS, items * most >= patt::MAX_CTAS ? patt::MAX_CTAS : items * most * kv->n_kv_heads);
     n.joins = most > 1;
-    const int stage = patt::KEYS * n.hdp * 2, q = 2 * patt::QTILE * n.hdp * 2;
-    n.stages = std::min(patt::MAX_STAGES, (224 * 1024 - q) / stage);
+    const int stage = patt::KEYS * n.hdp * 2, q = n.nh * patt::QTILE * n.hdp * 2, most_smem = 227 * 1024 - 1024 - (int)sizeof(patt::Control);
+    n.stages = std::min(patt::MAX_STAGES, (most_smem - q) / stage);
     n.control_at = q + n.stages * stage;
-    n.smem = 1024 + n.control_at + (int)sizeof(patt::Control);
+    // (at least 200 KB: no other CTA that takes tensor memory is on the SM, so taking all of it does not wait)
+    n.smem = std::max(200 * 1024, 1024 + n.control_at + (int)sizeof(patt::Control));
     n.ml_at = n.ctas * 32LL;
-    n.o_at = n.ml_at + (n.joins ? 2LL * n.ctas * patt::QROWS * 8 : 0);
-    n.bytes = n.o_at + (n.joins ? 2LL * n.ctas * patt::QROWS * n.hdp * 4 : 0);
+    n.o_at = n.ml_at + (n.joins ? 2LL * n.ctas * per * 8 : 0);      // (a multiple of 32)
+    n.bytes = n.o_at + (n.joins ? 2LL * n.ctas * per * n.hdp * 4 : 0);
     return n;
 }
 
@@ -57,10 +63,10 @@ int encode(const ops::Device* dev, CUtensorMap* map, const void* base, const s2d
     return r == CUDA_SUCCESS ? S2D2_OK : ops::fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
-template <int HDP>
+template <int HDP, int NH>
 cudaError_t launch_tiles(const CUtensorMap& map_k, const CUtensorMap& map_v, const patt::TileParams& t, const Plan& n, cudaStream_t st) {
-    cudaError_t e = ops::launch(patt::tile_kernel<HDP>, dim3(n.ctas), patt::THREADS, n.smem, 1, st, map_k, map_v, t);
-    if (!e && n.joins) e = ops::launch(patt::join_kernel<HDP>, dim3(n.ctas, patt::QROWS / 32), 256, 0, 1, st, t);
+    cudaError_t e = ops::launch(patt::tile_kernel<HDP, NH>, dim3(n.ctas), patt::threads(NH), n.smem, 1, st, map_k, map_v, t);
+    if (!e && n.joins) e = ops::launch(patt::join_kernel<HDP>, dim3(n.ctas, 4 * NH), 256, 0, 1, st, t);
     return e;
 }
 
@@ -69,8 +75,10 @@ cudaError_t launch_tiles(const CUtensorMap& map_k, const CUtensorMap& map_v, con
 namespace ops {
 cudaError_t load_attention_kernels() {
     constexpr int most = 227 * 1024;
-    cudaError_t e = load(patt::tile_kernel<64>, most);
-    if (!e) e = load(patt::tile_kernel<128>, most);
+    cudaError_t e = load(patt::tile_kernel<64, 1>, most);
+    if (!e) e = load(patt::tile_kernel<64, 2>, most);
+    if (!e) e = load(patt::tile_kernel<128, 1>, most);
+    if (!e) e = load(patt::tile_kernel<128, 2>, most);
     if (!e) e = load(patt::join_kernel<64>);
     return e ? e : load(patt::join_kernel<128>);
 }
@@ -112,7 +120,7 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     if (int rc = ops::device_kv(dev, op, kv, &p.c)) return rc;
     if (int rc = ops::check_ptr(dev, d_q, 16, "q")) return rc;
     if (int rc = ops::check_ptr(dev, d_out, 16, "out")) return rc;
-    if (int rc = ops::check_ptr(dev, d_ws, 16, "workspace")) return rc;
+    if (int rc = ops::check_ptr(dev, d_ws, 32, "workspace")) return rc;
     if (d_lse)
         if (int rc = ops::check_ptr(dev, d_lse, 4, "lse")) return rc;
     if (d_row_mask)
@@ -136,19 +144,21 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     t.stages = n.stages;
     t.control_at = n.control_at;
     // threads per sequence when units are counted: as many as it may have items, as long as one round takes all sequences
+    t.rows = patt::QTILE * n.nh;
     t.seq_lanes = 1;
-    while (t.seq_lanes < 32 && t.seq_lanes * patt::QROWS < (long long)rows->max_rows * p.group && (long long)rows->n_seqs * t.seq_lanes * 2 <= patt::THREADS)
+    while (t.seq_lanes < 32 && t.seq_lanes * t.rows < (long long)rows->max_rows * p.group && (long long)rows->n_seqs * t.seq_lanes * 2 <= patt::threads(n.nh))
         t.seq_lanes *= 2;
     t.split = (int4*)d_ws;
     t.part_ml = (float2*)((char*)d_ws + n.ml_at);
     t.part_o = (float*)((char*)d_ws + n.o_at);
+    t.out_32 = ((uintptr_t)d_out & 31) == 0 && out_stride % 16 == 0 && kv->head_dim % 16 == 0;
     t.timeouts = dev->timeouts;
     t.wait_limit = g_wait_limit;
     t.withhold = g_withhold;
     g_wait_limit = tc::WAIT_LIMIT;
     g_withhold = 0;
-    const cudaError_t e = n.hdp == 128 ? launch_tiles<128>(map_k, map_v, t, n, (cudaStream_t)cuda_stream)
-                                       : launch_tiles<64>(map_k, map_v, t, n, (cudaStream_t)cuda_stream);
+    const auto launch = n.hdp == 128 ? (n.nh == 1 ? launch_tiles<128, 1> : launch_tiles<128, 2>) : (n.nh == 1 ? launch_tiles<64, 1> : launch_tiles<64, 2>);
+    const cudaError_t e = launch(map_k, map_v, t, n, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return ops::fail(S2D2_ERR_CUDA, "%s: %s", op, cudaGetErrorString(e));

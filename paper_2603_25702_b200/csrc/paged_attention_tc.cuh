@@ -3,11 +3,12 @@
 //   O[row] = sum_j p_j V[j] / sum_j p_j,   p_j = 2^(s_j - m),   s = scale log2(e) Q K^T,   in one pass over the keys with a running m and sum
 //
 // The query vectors of a kv head are its sequence's rows times the group of heads that read it (row-major: vector = row * group + head
-// of the group), so K and V are read once for a whole group.  An item is (sequence, kv head, 256 query vectors); its units are the
+// of the group), so K and V are read once for a whole group.  An item is (sequence, kv head, 256 or 128 query vectors); its units are the
 // tiles of 128 keys that any of its rows sees.  All units, in the order of the items, are cut into as many equal ranges as there
-// are CTAs: a long cache is shared by many CTAs, many short sequences by few, a ragged batch evenly, and no CTA gets more than
-// one unit above the average.  Items that a cut went through leave parts (maximum, sum, weighted values) in the workspace, which
-// join_kernel adds up in the order of the keys: deterministic, no tickets.  Lengths are read on the device.
+// are CTAs (an item counts one unit more than it has: its start and its end cost about as much), so that a long cache is shared by many
+// CTAs, many short sequences by few, and a ragged batch evenly.  Items that a cut went through leave parts (maximum, sum, weighted
+// values) in the workspace, which join_kernel adds up in the order of the keys: deterministic, no tickets.  Lengths are read on
+// the device.
 #pragma once
 #include "paged_attention.cuh"
 #include "tc_ptx.cuh"
@@ -19,9 +20,10 @@ using namespace tc;
 
 constexpr int KEYS = 128;            // keys of a tile
 constexpr int QTILE = 128;           // query vectors of an MMA
-constexpr int QROWS = 256;           // of an item
 constexpr int MAX_CTAS = 148;
-constexpr int THREADS = 384;         // warps 0-3 and 4-7: softmax of the two halves of an item; 8: MMA; 9: copies (10, 11: none)
+// NH: MMA tiles of query vectors in an item, its halves (2: many rows; 1: few).  Warps 0 .. 4 NH - 1: softmax; then items and copies, Q,
+// and NH for the MMAs.
+__host__ __device__ constexpr int threads(int nh) { return 128 * nh + 128; }
 
 // ---- instructions ----
 __device__ __forceinline__ bool elect() {                      // one lane of a converged warp
@@ -34,6 +36,18 @@ __device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return done;
+}
+// Whether the phase is over, without waiting (poll() may wait for some microseconds).
+__device__ __forceinline__ bool peek(uint64_t* bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
         : "r"(smem_u32(bar)), "r"(parity)
@@ -70,10 +84,6 @@ __device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
 __device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t chunk_bytes) {      // the next 64 columns are chunk_bytes further
     return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(chunk_bytes >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-// D fp32, A and B bf16, A K-major, M = 128; B K-major or MN-major
-__device__ __forceinline__ uint32_t idesc_bf16(int n, int b_mn) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-}
 // D (+)= A B with A in tensor memory: lane = row, a 32-bit column two neighbouring k
 __device__ __forceinline__ void umma_bf16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -99,9 +109,9 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {      // NaN if there is one
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {      // two operations in one instruction
@@ -118,6 +128,22 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
+// 2^x of two numbers below 2^7 on the multipliers, where the unit for exponentials (16 a cycle) is what a tile waits for: x = n + f with n the
+// nearest integer, 2^f = 1 + f (..) by a polynomial of degree 4 with equal ripples of 2.8e-6 on [-1/2, 1/2], n added to the exponent.
+// -127 and less, and NaN: exactly 0 (the bits of 1 less 127 in the exponent).
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+    const float2 big = make_float2(12582912.f, 12582912.f);      // 1.5 2^23: the sum's last bits are the integer
+    x = make_float2(fmaxf(x.x, -127.f), fmaxf(x.y, -127.f));
+    const float2 t = add2(x, big), n = add2(t, make_float2(-12582912.f, -12582912.f));
+    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+    float2 y = fma2(make_float2(0.009582576341927052f, 0.009582576341927052f), f, make_float2(0.05590682849287987f, 0.05590682849287987f));
+    y = fma2(y, f, make_float2(0.24024106562137604f, 0.24024106562137604f));
+    y = fma2(y, f, make_float2(0.6931241154670715f, 0.6931241154670715f));
+    y = fma2(y, f, make_float2(1.f, 1.f));
+    y.x = __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
+    y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
+    return y;
+}
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -128,13 +154,15 @@ struct TileParams {
     Params a;
     int ctas;                        // CTAs that share the units, at most
     int stages;
-    int seq_lanes;                   // threads that count a sequence's units: 1, or 32 where sequences have many items
+    int rows;                        // query vectors of an item: 128 NH
+    int seq_lanes;                   // threads that count a sequence's units: a power of two up to 32
     int control_at;                  // byte offset of Control
-    float* part_o;                   // [2 ctas][QROWS][HDP]
-    float2* part_ml;                 // [2 ctas][QROWS]: reference, sum
+    float* part_o;                   // [2 ctas][rows][HDP]
+    float2* part_ml;                 // [2 ctas][rows]: reference, sum
     int4* split;                     // [ctas][2]: the item that CTA c begins and does not end: sequence, kv head, item, last CTA; row0, n, kv, ok (sequence -1: none)
     int* timeouts;
     uint32_t wait_limit;
+    int out_32;                      // rows of heads of the output are multiples of 32 bytes and aligned to them
     int withhold;                    // test tap: nothing is loaded, so that nothing ever completes a stage
 };
 
@@ -143,74 +171,85 @@ __device__ __forceinline__ paged::Seq usable_seq(const Params& p, int s) {      
     if (!q.ok) q.kv = 0;
     return q;
 }
-__device__ __forceinline__ int items_of(const Params& p, int n) { return (n * p.group + QROWS - 1) / QROWS; }
+template <int NH>
+__device__ __forceinline__ int items_of(const Params& p, int n) { return (n * p.group + 128 * NH - 1) / (128 * NH); }
 // Units of item qt of a sequence: at least one, so that rows that see nothing are written.
+template <int NH>
 __device__ __forceinline__ int units_of(const Params& p, const paged::Seq& s, int qt) {
-    const int last = (min(s.n * p.group, (qt + 1) * QROWS) - 1) / p.group;
+    const int last = (min(s.n * p.group, (qt + 1) * 128 * NH) - 1) / p.group;
     const int end = paged::key_end(p.mask_block, p.row_mask != nullptr, s.n, s.kv, last);
     return max(1, (end + KEYS - 1) / KEYS);
 }
 
-// The items of a CTA's range, one after the other.
+// The items of a CTA's range, one after the other.  Ranges are in costs: an item has `extra` in front of its units.
 struct Items {
-    int seq, kvh, qt, j;             // the next unit
-    long long left;                  // units of the range that are left
+    int seq, kvh, qt, extra;
+    long long at, left;              // costs of item qt in front of the range, costs of the range that are left
     paged::Seq s;                    // of seq
 };
 struct Item {
     paged::Seq s;
-    int seq, kvh, qt, j0, j1, units;
+    int seq, kvh, qt, j0, j1, units;     // j1 = 0: there are no more
     __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == units; }
 };
+template <int NH>
 __device__ __forceinline__ bool next_item(const Params& p, Items& t, Item& w) {
-    if (t.left <= 0) return false;
-    while (t.qt >= items_of(p, t.s.n)) {       // behind the last item of a head
-        t.qt = 0;
-        if (t.s.n == 0 || ++t.kvh >= p.kv_heads) {
-            t.kvh = 0;
-            if (++t.seq >= p.b.n_seqs) {       // (cannot be: the range ends with the last unit)
-                t.left = 0;
-                return false;
+    while (t.left > 0) {
+        while (t.qt >= items_of<NH>(p, t.s.n)) {       // behind the last item of a head
+            t.qt = 0;
+            if (t.s.n == 0 || ++t.kvh >= p.kv_heads) {
+                t.kvh = 0;
+                if (++t.seq >= p.b.n_seqs) {           // (cannot be: the range ends with the last unit)
+                    t.left = 0;
+                    return false;
+                }
+                t.s = usable_seq(p, t.seq);
             }
-            t.s = usable_seq(p, t.seq);
         }
+        w.s = t.s;
+        w.seq = t.seq;
+        w.kvh = t.kvh;
+        w.qt = t.qt;
+        w.units = units_of<NH>(p, t.s, t.qt);
+        const long long end = min(t.at + t.left, (long long)w.units + t.extra);
+        w.j0 = (int)max(0LL, t.at - t.extra);
+        w.j1 = (int)max(0LL, end - t.extra);
+        t.left -= end - t.at;
+        t.at = 0;
+        ++t.qt;
+        if (w.j1 > w.j0) return true;                  // else the cut went through the extra
     }
-    w.s = t.s;
-    w.seq = t.seq;
-    w.kvh = t.kvh;
-    w.qt = t.qt;
-    w.j0 = t.j;
-    w.units = units_of(p, t.s, t.qt);
-    w.j1 = (int)min((long long)w.units, t.j + t.left);
-    t.left -= w.j1 - w.j0;
-    if (w.j1 == w.units) ++t.qt, t.j = 0;
-    else t.j = w.j1;
-    return true;
+    return false;
 }
 
 struct Setup {
-    long long warp_sum[THREADS / 32];
-    long long at;                    // units in front of the sequence of the first unit
-    long long total, ctas, u1;       // all units, the CTAs that share them, the end of this CTA's range
+    long long warp_sum[threads(2) / 32];
+    long long front;                 // costs in front of the sequence of the range's begin
+    long long total, ctas, u1;       // all costs, the CTAs that share them, the end of this CTA's range
     Items first;
 };
 
-// All threads: the first unit of this CTA's range and its length, from the lengths on the device.  Sequences are counted THREADS / seq_lanes at a time.
+// All threads: the begin of this CTA's range and its length, from the lengths on the device.  Sequences are counted threads / seq_lanes at
+// a time.
+template <int NH>
 __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out) {
+    constexpr int NT = threads(NH);
     const Params& p = tp.a;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = THREADS / tp.seq_lanes;
-    auto units = [&](int s) -> long long {      // of a sequence, by seq_lanes threads; the first of them has the sum
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = NT / tp.seq_lanes;
+    // items (from bit 40 on; below 2^23) and units of a sequence, by seq_lanes threads; the first of them has the sums
+    auto count = [&](int s) -> long long {
         long long n = 0;
         if (s < p.b.n_seqs) {
             const paged::Seq q = usable_seq(p, s);
-            const int items = items_of(p, q.n);
-            for (int t = tid & (tp.seq_lanes - 1); t < items; t += tp.seq_lanes) n += units_of(p, q, t);
+            const int items = items_of<NH>(p, q.n);
+            for (int t = tid & (tp.seq_lanes - 1); t < items; t += tp.seq_lanes) n += units_of<NH>(p, q, t) + (1LL << 40);
         }
         for (int o = tp.seq_lanes >> 1; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        return (tid & (tp.seq_lanes - 1)) ? 0 : n * p.kv_heads;
+        return (tid & (tp.seq_lanes - 1)) ? 0 : n;
     };
-    long long total = 0, mine = 0, before = 0;
-    // inclusive sums over the CTA's threads; `before` excludes the thread's own
+    auto cost = [&](long long n, int extra) { return ((n & ((1LL << 40) - 1)) + (n >> 40) * extra) * p.kv_heads; };
+    long long mine = 0, before = 0;
+    // sum over the CTA's threads; `before` is that of the threads in front of this one
     auto scan = [&](long long v) -> long long {
         long long x = v;
 #pragma unroll
@@ -223,31 +262,35 @@ __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out
         __syncthreads();
         long long all = 0, front = 0;
 #pragma unroll
-        for (int i = 0; i < THREADS / 32; ++i) {
+        for (int i = 0; i < NT / 32; ++i) {
             if (i == warp) front = all;
             all += sh.warp_sum[i];
         }
         before = front + x - v;
         return all;
     };
+    long long sum = 0;
     for (int s0 = 0; s0 < p.b.n_seqs; s0 += per) {
-        mine = units(s0 + tid / tp.seq_lanes);
-        total += scan(mine);
+        mine = count(s0 + tid / tp.seq_lanes);
+        sum += scan(mine);
     }
-    const long long ctas = min((long long)tp.ctas, total), c = blockIdx.x;
     out.left = 0;
-    if (tid == 0) tp.split[2 * c] = make_int4(-1, 0, 0, 0);
+    if (tid == 0) tp.split[2 * blockIdx.x] = make_int4(-1, 0, 0, 0);
+    // With few units per CTA every one of them counts more than an even spread of starts and ends
+    const int extra = cost(sum, 0) > 4LL * tp.ctas ? 1 : 0;
+    const long long total = cost(sum, extra), ctas = min((long long)tp.ctas, total), c = blockIdx.x;
     if (c >= ctas) return;
     const long long u0 = total * c / ctas, u1 = total * (c + 1) / ctas;
     long long base = 0;
     for (int s0 = 0; s0 < p.b.n_seqs; s0 += per) {
-        if (p.b.n_seqs > per) mine = units(s0 + tid / tp.seq_lanes);
-        const long long all = p.b.n_seqs > per ? scan(mine) : total;
-        if (mine > 0 && base + before <= u0 && u0 < base + before + mine) {
+        if (p.b.n_seqs > per) mine = count(s0 + tid / tp.seq_lanes);
+        const long long all = p.b.n_seqs > per ? scan(mine) : sum;
+        const long long lo = base + cost(before, extra);
+        if (mine > 0 && lo <= u0 && u0 < lo + cost(mine, extra)) {
             sh.first.seq = s0 + tid / tp.seq_lanes;
-            sh.at = base + before;
+            sh.front = lo;
         }
-        base += all;
+        base += cost(all, extra);
         if (u0 < base) break;                  // (the same for all threads)
     }
     __syncthreads();
@@ -255,16 +298,17 @@ __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out
         Items t;
         t.seq = sh.first.seq;
         t.s = usable_seq(p, t.seq);
-        const int items = items_of(p, t.s.n);
+        t.extra = extra;
+        const int items = items_of<NH>(p, t.s.n);
         long long per_head = 0;
-        for (int i = lane; i < items; i += 32) per_head += units_of(p, t.s, i);
+        for (int i = lane; i < items; i += 32) per_head += units_of<NH>(p, t.s, i) + extra;
 #pragma unroll
         for (int o = 16; o; o >>= 1) per_head += __shfl_xor_sync(0xffffffffu, per_head, o);
-        long long rest = u0 - sh.at;
+        long long rest = u0 - sh.front;
         t.kvh = (int)(rest / per_head);
         rest -= t.kvh * per_head;
         for (t.qt = 0;; t.qt += 32) {          // 32 items at a time
-            const int n = t.qt + lane < items ? units_of(p, t.s, t.qt + lane) : 0;
+            const int n = t.qt + lane < items ? units_of<NH>(p, t.s, t.qt + lane) + extra : 0;
             int x = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -273,9 +317,9 @@ __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out
             }
             const unsigned in = __ballot_sync(0xffffffffu, rest < x);      // inclusive sums grow: the first lane above
             if (in) {
-                const int at = __ffs(in) - 1;
-                rest -= __shfl_sync(0xffffffffu, x - n, at);
-                t.qt += at;
+                const int i = __ffs(in) - 1;
+                rest -= __shfl_sync(0xffffffffu, x - n, i);
+                t.qt += i;
                 break;
             }
             rest -= __shfl_sync(0xffffffffu, x, 31);
@@ -284,7 +328,7 @@ __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out
                 break;
             }
         }
-        t.j = (int)rest;
+        t.at = rest;
         t.left = u1 - u0;
         if (lane == 0) sh.first = t, sh.total = total, sh.ctas = ctas, sh.u1 = u1;
     }
@@ -300,9 +344,14 @@ __device__ __forceinline__ void note_split(const TileParams& tp, const Setup& sh
 }
 
 constexpr int MAX_STAGES = 12;
+constexpr int ITEMS = 8;             // that the copy warp may be ahead of the others
 struct Control {
-    uint64_t full[MAX_STAGES], empty[MAX_STAGES], q_full[2], s_full[2], p_full[2], o_full[2];
-    int bad[16];                     // bad[i % 16] == i + 1: item i of this CTA has a page that is not one
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], item_full[ITEMS], item_empty[ITEMS];
+    uint64_t q_full[2], q_empty[2];                                          // per half
+    // Per half and buffer (a unit's first and second 64 keys).  A barrier of a buffer cannot be two phases ahead of who waits for it.
+    uint64_t s_full[2][2], p_full[2][2], o_full[2][2];
+    Item items[ITEMS];
+    int bad[2 * ITEMS];                    // bad[i % 16] == i + 1: item i of this CTA has a page that is not one
     uint32_t tmem_slot;
     int abort_flag;
     Setup setup;
@@ -317,7 +366,7 @@ struct Ring {                        // position in the ring: stage, and the par
 
 // Rows whose accumulators are not finite: a NaN or an infinity in a value that a row does not see has come in through a probability of zero (or the
 // row sees it: then the result is the same).  The warp takes them again, one by one, without the keys that they do not see.
-__device__ __noinline__ void repair_rows(const Params& p, const Item& w, int qv, bool bad, float* part_o, float2* part_ml, int hdp) {
+__device__ __noinline__ void repair_rows(const Params& p, const Item& w, int qv, bool bad, float* part_o, float2* part_ml, int hdp, int rows) {
     unsigned todo = __ballot_sync(0xffffffffu, bad);
     const int lane = threadIdx.x & 31;
     while (todo) {
@@ -327,7 +376,7 @@ __device__ __noinline__ void repair_rows(const Params& p, const Item& w, int qv,
         const long long row = w.s.row0 + i;
         const paged::View view = paged::row_view(p.mask_block, p.row_mask, w.s, i);
         const RowSum a = row_sum(p, w.seq, w.s.kv, w.kvh, p.q + row * p.q_ld + (long long)h * p.head_dim, view, w.j0 * KEYS, w.j1 * KEYS);
-        const int r = v - w.qt * QROWS;
+        const int r = v - w.qt * rows;
         const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -346,126 +395,181 @@ __device__ __noinline__ void repair_rows(const Params& p, const Item& w, int qv,
 }
 
 // After a time-out: NaN in all outputs of the CTA's range, those that were finished included.
+template <int NH>
 __device__ __noinline__ void all_nan(const TileParams& tp, const Setup& sh, Items t, int hdp) {
     const Params& p = tp.a;
     const float nan = __int_as_float(0x7fffffff);
     Item w;
-    while (next_item(p, t, w)) {
+    while (next_item<NH>(p, t, w)) {
         if (threadIdx.x == 0) note_split(tp, sh, w);
-        const int n = min(QROWS, w.s.n * p.group - w.qt * QROWS);
-        for (int r = threadIdx.x; r < n; r += THREADS) {
-            const int qv = w.qt * QROWS + r, i = qv / p.group, h = w.kvh * p.group + (qv - i * p.group);
+        const int n = min(128 * NH, w.s.n * p.group - w.qt * 128 * NH);
+        for (int r = threadIdx.x; r < n; r += threads(NH)) {
+            const int qv = w.qt * 128 * NH + r, i = qv / p.group, h = w.kvh * p.group + (qv - i * p.group);
             const long long row = w.s.row0 + i;
             if (w.whole()) {
                 for (int d = 0; d < p.head_dim; ++d) p.out[row * p.out_ld + (long long)h * p.head_dim + d] = __float2bfloat16_rn(nan);
                 if (p.lse) p.lse[row * p.heads + h] = nan;
             } else {
-                const int slot = 2 * blockIdx.x + (w.j0 == 0);
-                tp.part_ml[(size_t)slot * QROWS + r] = make_float2(0.f, nan);
-                for (int d = 0; d < hdp; ++d) tp.part_o[((size_t)slot * QROWS + r) * hdp + d] = nan;
+                const size_t at = (size_t)(2 * blockIdx.x + (w.j0 == 0)) * (128 * NH) + r;
+                tp.part_ml[at] = make_float2(0.f, nan);
+                for (int d = 0; d < hdp; ++d) tp.part_o[at * hdp + d] = nan;
             }
         }
     }
 }
 
-// Softmax warps: a thread has a query vector's row of scores, S[128], in a lane of tensor memory.  Its probabilities take the place of the
-// scores as bf16 pairs (the left operand of the second product, straight from tensor memory).  The reference m follows the running maximum
-// lazily, when that has grown by more than 2^8: the probabilities stay below 256 (their bf16 rounding is relative) and
-// the accumulator is rarely rescaled.  That is safe without a wait: scores of tile j are complete after the product with the values of tile j - 1,
-// and the next one waits for these probabilities.
-template <int HDP>
-__device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl, uint8_t* q_tiles, Items t, int half) {
+// Tensor memory: columns 0-255 scores, two buffers of 64 keys for each half; probabilities (bf16 pairs, 32 columns) stand over the scores that
+// they come from; accumulators of the halves from column 256 on.
+constexpr int STEP = 64;
+
+// The items of this CTA as its copy warp lists them, in order; every warp gives them back.
+struct Listed {
+    int index = 0;
+    __device__ __forceinline__ bool get(Control& ctl, const TileParams& tp, Item& w) const {
+        if (!__all_sync(0xffffffffu, wait(&ctl.item_full[index % ITEMS], index / ITEMS & 1, tp.wait_limit, &ctl.abort_flag))) return false;
+        w = ctl.items[index % ITEMS];
+        return true;
+    }
+    __device__ __forceinline__ void done(Control& ctl) {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) arrive(&ctl.item_empty[index % ITEMS]);
+        ++index;
+    }
+};
+template <int NH>
+__device__ __forceinline__ bool active(const Params& p, const Item& w, int half) { return half == 0 || w.s.n * p.group > (w.qt * NH + half) * QTILE; }
+
+// 32 bytes of a lane's own row: with one store, a whole sector, where rows are aligned to that.
+__device__ __forceinline__ void store32(void* dst, const uint32_t* v, bool aligned, bool second) {
+    if (aligned) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+                     "r"(v[6]), "r"(v[7])
+                     : "memory");
+    } else {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
+        if (second) *(reinterpret_cast<uint4*>(dst) + 1) = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
+
+// 32 probabilities 2^(s factor - m) of scores s as bf16 pairs, and their sum in two chains.  `high`: the largest exponent that went to the
+// polynomial, which is wrong above 2^7, or NaN.
+__device__ __forceinline__ void probabilities(const uint32_t (&v)[32], float factor, float minus_m, uint32_t (&pk)[16], float2& sum, float2& sum1, float& high) {
+    const float2 cc = make_float2(factor, factor), rr = make_float2(minus_m, minus_m);
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+        const float2 x = fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), cc, rr);
+        // Of four pairs one by the polynomial: the exponentials' unit takes 8 cycles for a warp's instruction, the polynomial's two-fold
+        // instructions about 14 on other units (64 scores of two warps: 890 cycles; without 1190, three of eight 970).
+        float2 y;
+        if ((e / 2) % 4 < 3) {
+            y = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+        } else {
+            high = max3_nan(high, x.x, x.y);
+            y = exp2_poly(x);
+        }
+        if (e & 2) sum1 = add2(sum1, y);
+        else sum = add2(sum, y);
+        pk[e / 2] = pack2(y.x, y.y);
+    }
+}
+__device__ __forceinline__ float max64(const uint32_t (&v)[2][32]) {      // NaN if there is one
+    float mx[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint32_t* x = v[c >> 1] + (c & 1) * 16;
+        mx[c] = max3_nan(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]));
+#pragma unroll
+        for (int e = 3; e < 15; e += 2) mx[c] = max3_nan(mx[c], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+        mx[c] = max3_nan(mx[c], __uint_as_float(x[15]), __uint_as_float(x[15]));
+    }
+    return max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]);
+}
+__device__ __forceinline__ float first_reference(const uint32_t (&v)[32]) {
+    float m = __uint_as_float(v[0]);
+#pragma unroll
+    for (int e = 1; e < 31; e += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(__uint_as_float(v[e])), "f"(__uint_as_float(v[e + 1])));
+    return m;
+}
+// -inf for the keys from `key` on that are not seen
+__device__ __forceinline__ void mask64(uint32_t (&v)[2][32], const paged::View& view, int key) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const int n = view.lim - (key + 32 * c), d = key + 32 * c - view.base;
+        uint32_t seen = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
+        if (d >= 0 && d < 64) seen |= (uint32_t)(view.bits >> d);
+        else if (d < 0 && d > -32) seen |= (uint32_t)view.bits << -d;
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (!(seen >> e & 1)) v[c][e] = 0xff800000u;
+    }
+}
+
+// Softmax warps: a thread has a query vector's row of scores, a lane of tensor memory, and takes it in steps of 64 keys.  It leaves the probabilities
+// over the scores as bf16 pairs, the left operand of the second product.  The scores of the next step are computed meanwhile (two buffers
+// of 64 columns; with one of 128, the most that fits beside the accumulators, every unit waited 1500 cycles for its scores).  The
+// reference m is not the maximum but what the maximum was when a step's probabilities last added up to more than 512, so these stay below that
+// (their bf16 rounding is relative), the accumulator is rarely rescaled, and no maximum is taken but then: the step's exponentials are taken
+// again with the new reference.  An item's first reference is the maximum of its first 32 scores.
+// What bounds it: 7 cycles per score and warp for exponentials and sums, and code: what runs seldom is kept short and out of
+// the way, straight code of more than one pass over the scores was slowed down by instruction fetches.
+template <int HDP, int NH>
+__device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl) {
+    constexpr float FAR = 1048576.f;
     const Params& p = tp.a;
     volatile int* abort_flag = &ctl.abort_flag;
-    const int tid = threadIdx.x & 127, warp = tid >> 5;
-    const uint32_t tmem = ctl.tmem_slot, lanes = (uint32_t)(warp * 32) << 16;
-    const uint32_t ts = tmem + half * KEYS + lanes, to = tmem + 2 * KEYS + half * HDP + lanes;
-    const uint32_t q_addr = smem_u32(q_tiles) + half * (QTILE * HDP * 2);
-    const float inv_group = 1.f / (float)p.group;
-    uint32_t s_parity = 0, o_parity = 0;
-
-    // Q rows of an item's half: copies of 16 bytes into the swizzled tile; rows and elements that do not exist are zero.
-    auto load_q = [&](const Item& w) {
-        constexpr int CH = HDP / 8;
-        const int q0 = w.qt * QROWS + half * QTILE, nq = w.s.n * p.group;
-        const int i0 = q0 / p.group, g0 = q0 - i0 * p.group;
-#pragma unroll 4
-        for (int k = 0; k < QTILE * CH / 128; ++k) {
-            const int idx = tid + k * 128, r = idx / CH, c = idx % CH;
-            int i = (int)(((float)(g0 + r) + 0.5f) * inv_group);                  // (g0 + r) / group, of numbers below 2^13
-            const int g = g0 + r - i * p.group;
-            const bool some = q0 + r < nq && c * 8 < p.head_dim;
-            const bf16* src = p.q + (long long)(w.s.row0 + i0 + i) * p.q_ld + (long long)(w.kvh * p.group + g) * p.head_dim + c * 8;
-            copy16(q_addr + (c >> 3) * (QTILE * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), some ? src : p.q, some);
-        }
-    };
-    auto q_ready = [&]() {
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        fence_async_shared();
-        arrive(&ctl.q_full[half]);
-    };
-    auto active = [&](const Item& w) { return w.s.n * p.group > w.qt * QROWS + half * QTILE; };
-
-    Item w, next;
-    bool have = next_item(p, t, w);
-    if (have && active(w)) {
-        load_q(w);
-        q_ready();
-    }
-    for (int index = 0; have; ++index) {
-        const bool have_next = next_item(p, t, next);
-        if (half == 0 && tid == 0) note_split(tp, ctl.setup, w);
-        if (active(w)) {
-            const int qv = w.qt * QROWS + half * QTILE + tid;
-            const bool valid = qv < w.s.n * p.group;
-            const int i = (valid ? qv : 0) / p.group;
-            paged::View view;
-            view.lim = 0x7fffffff;
-            view.base = 0;
-            view.bits = 0;
-            if (valid) view = paged::row_view(p.mask_block, p.row_mask, w.s, i);
-            float m = -INFINITY, l = 0.f;
-            for (int j = w.j0; j < w.j1; ++j) {
-                if (!__all_sync(0xffffffffu, wait(&ctl.s_full[half], s_parity, tp.wait_limit, abort_flag))) return false;
-                s_parity ^= 1;
+    const int half = threadIdx.x >> 7, r = threadIdx.x & 127;
+    const uint32_t tmem = ctl.tmem_slot + ((uint32_t)(r & 96) << 16), to = tmem + 256 + half * HDP;
+    uint32_t steps = 0;                                      // of this half so far
+    Listed list;
+    Item w;
+    for (;; list.done(ctl)) {
+        if (!list.get(ctl, tp, w)) return false;
+        if (w.j1 == 0) return true;
+        if (!active<NH>(p, w, half)) continue;
+        const int qv = (w.qt * NH + half) * QTILE + r, i = qv / p.group;
+        const bool valid = qv < w.s.n * p.group, any = __any_sync(0xffffffffu, valid);
+        paged::View view;
+        view.lim = 0x7fffffff;
+        view.base = 0;
+        view.bits = 0;
+        if (valid) view = paged::row_view(p.mask_block, p.row_mask, w.s, i);
+        float m = -INFINITY, l = 0.f;
+        const int end = w.j1 * KEYS;
+        for (int key = w.j0 * KEYS; key < end; key += STEP, ++steps) {
+            const uint32_t buf = steps & 1;
+            if (!__all_sync(0xffffffffu, wait(&ctl.s_full[half][buf], steps >> 1 & 1, tp.wait_limit, abort_flag))) return false;
+            if (any) {
                 tc_fence_after();
-                const bool last = j + 1 == w.j1;
-                if (last && have_next && active(next)) load_q(next);              // the scores of this item are complete: its Q tile is free
-                uint32_t v[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32_issue(ts + c * 32, v[c]);
+                const uint32_t ts = tmem + half * 2 * STEP + buf * STEP;
+                uint32_t v[2][32], pk[2][16];
+                tmem_ld32_issue(ts, v[0]);
+                tmem_ld32_issue(ts + 32, v[1]);
                 tmem_ld_wait();
-                const int key0 = j * KEYS;
-                if (!__all_sync(0xffffffffu, key0 + KEYS <= view.lim)) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int n = view.lim - (key0 + 32 * c), d = key0 + 32 * c - view.base;
-                        uint32_t seen = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
-                        if (d >= 0 && d < 64) seen |= (uint32_t)(view.bits >> d);
-                        else if (d < 0 && d > -32) seen |= (uint32_t)view.bits << -d;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!(seen >> e & 1)) v[c][e] = 0xff800000u;          // -inf
-                    }
-                }
-                float mx[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    mx[c] = __uint_as_float(v[c][0]);
-#pragma unroll
-                    for (int e = 1; e < 31; e += 2) mx[c] = max3(mx[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
-                    mx[c] = fmaxf(mx[c], __uint_as_float(v[c][31]));
-                }
-                const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * p.scale_log2;
-                float alpha = 1.f;
-                if (top > m + 8.f || (m == -INFINITY && top > m)) {
-                    alpha = exp2_fast(m - top);
-                    m = top;
-                }
-                if (__any_sync(0xffffffffu, alpha != 1.f)) {
+                if (!__all_sync(0xffffffffu, key + STEP <= view.lim)) mask64(v, view, key);
+                const float before = m;
+                if (key == w.j0 * KEYS) m = first_reference(v[0]) * p.scale_log2;
+                float2 sum, sum1;
+                float factor = p.scale_log2, total;
+#pragma unroll 1
+                for (bool again = false;; again = true) {
+                    const float minus_m = m == -INFINITY ? 0.f : -m;
+                    float high = -INFINITY;
+                    sum = sum1 = make_float2(0.f, 0.f);
+                    probabilities(v[0], factor, minus_m, pk[0], sum, sum1, high);
+                    probabilities(v[1], factor, minus_m, pk[1], sum, sum1, high);
+                    sum = add2(sum, sum1);
+                    total = sum.x + sum.y;
+                    // in order: no NaN, nothing above 2^9, and a reference that is a number of ordinary size
+                    if (again || __all_sync(0xffffffffu, total <= 512.f && high <= 9.f && fabsf(m) <= FAR)) break;
+                    const float top = max64(v) * p.scale_log2;
+                    if (!(top < INFINITY)) l = __int_as_float(0x7fffffff);        // a NaN or an infinity that the row sees
+                    m = fmaxf(m, top);
+                    const float alpha = before == m ? 1.f : exp2_fast(before - m);
                     l *= alpha;
-                    if (j > w.j0) {
-#pragma unroll
+                    if (key > w.j0 * KEYS && __any_sync(0xffffffffu, alpha != 1.f)) {
+                        if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][buf ^ 1], (steps - 1) >> 1 & 1, tp.wait_limit, abort_flag))) return false;      // the product before this one's
+                        tc_fence_after();
+#pragma unroll 1
                         for (int c = 0; c < HDP; c += 16) {
                             float o[16];
                             tmem_ld16(to + c, o);
@@ -475,198 +579,228 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl,
                             tmem_st16(to + c, u);
                         }
                     }
-                }
-                const float ref = m == -INFINITY ? 0.f : -m;
-                float factor = p.scale_log2;
-                if (__any_sync(0xffffffffu, fabsf(ref) > 1048576.f)) {
-                    // s c - m in one operation: m is rounded, so the largest score's difference is off by up to 2^-24 m.  That only moves the
-                    // reference, unless m is so large that it leaves the range of the exponentials: then scores are rounded like m first.
-                    factor = 1.f;
+                    if (__any_sync(0xffffffffu, fabsf(m) > FAR && m != -INFINITY)) {
+                        // s c - m in one operation: m is rounded, so the largest score's difference is off by up to 2^-24 m.  That only moves
+                        // the reference, unless m is so large that it leaves the range of the exponentials: then scores are rounded like m first.
+                        factor = 1.f;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) v[c][e] = __float_as_uint(__fmul_rn(__uint_as_float(v[c][e]), p.scale_log2));
-                }
-                const float2 cc = make_float2(factor, factor), rr = make_float2(ref, ref);
-                float2 sum = make_float2(0.f, 0.f), sum1 = sum;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float2 x = fma2(make_float2(__uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1])), cc, rr);
-                        const float2 y = make_float2(exp2_fast(x.x), exp2_fast(x.y));
-                        if (e & 2) sum1 = add2(sum1, y);
-                        else sum = add2(sum, y);
-                        pk[e / 2] = pack2(y.x, y.y);
+                        for (int e = 0; e < 32; ++e) {
+                            v[0][e] = __float_as_uint(__fmul_rn(__uint_as_float(v[0][e]), p.scale_log2));
+                            v[1][e] = __float_as_uint(__fmul_rn(__uint_as_float(v[1][e]), p.scale_log2));
+                        }
                     }
-                    tmem_st16(ts + c * 16, pk);
                 }
-                sum = add2(sum, sum1);
-                l += sum.x + sum.y;
+                tmem_st16(ts, pk[0]);
+                tmem_st16(ts + 16, pk[1]);
+                l += total;
                 tmem_st_wait();
                 tc_fence_before();
-                arrive(&ctl.p_full[half]);
-                if (last && have_next && active(next)) q_ready();
             }
-            // ---- the item's end: divide, or leave a part ----
-            if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half], o_parity, tp.wait_limit, abort_flag))) return false;
-            o_parity ^= 1;
+            arrive(&ctl.p_full[half][buf]);
+        }
+        // ---- the item's end: divide, or leave a part ----
+        if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][1], (steps - 1) >> 1 & 1, tp.wait_limit, abort_flag))) return false;
+        if (any) {
             tc_fence_after();
             const long long row = w.s.row0 + i;
             const int h = w.kvh * p.group + (qv - i * p.group);
-            const int slot = 2 * blockIdx.x + (w.j0 == 0), r = half * QTILE + tid;
-            float* part_o = tp.part_o + (size_t)slot * QROWS * HDP;
-            float2* part_ml = tp.part_ml + (size_t)slot * QROWS;
-            const bool nan = !w.s.ok || *(volatile int*)&ctl.bad[index & 15] == index + 1;
+            const bool nan = !w.s.ok || *(volatile int*)&ctl.bad[list.index % (2 * ITEMS)] == list.index + 1, whole = w.whole();
             const float undefined = __int_as_float(0x7fffffff);
             if (nan) l = undefined;
-            const float inv = w.whole() ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-            float check = l * 0.f;                                                 // NaN where something is not finite
-#pragma unroll
-            for (int c = 0; c < HDP; c += 32) {
-                uint32_t o[32];
-                tmem_ld32_issue(to + c, o);
-                tmem_ld_wait();
-                float f[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    f[e] = __uint_as_float(o[e]);
-                    check = fmaf(f[e], 0.f, check);
-                    f[e] = nan ? undefined : f[e] * inv;
-                }
-                if (!valid) {
-                } else if (w.whole()) {
-                    bf16* dst = p.out + row * p.out_ld + (long long)h * p.head_dim + c;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-                        if (c + e < p.head_dim)
-                            *reinterpret_cast<uint4*>(dst + e) =
-                                make_uint4(pack2(f[e], f[e + 1]), pack2(f[e + 2], f[e + 3]), pack2(f[e + 4], f[e + 5]), pack2(f[e + 6], f[e + 7]));
-                } else {
-                    float* dst = part_o + (size_t)r * HDP + c;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
-                }
+            const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+            const size_t slot = ((size_t)(2 * blockIdx.x + (w.j0 == 0)) * NH + half) * QTILE + r;
+            bf16* out = p.out + row * p.out_ld + (long long)h * p.head_dim;
+            float* part_o = tp.part_o + slot * HDP;
+            float check = fabsf(l);                                                // infinite or NaN where something is
+#pragma unroll 1
+            for (int c = 0; c < HDP; c += 16) {
+                float o[16];
                 __syncwarp();
+                tmem_ld16(to + c, o);
+                uint32_t u[16];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) check = max3_nan(check, fabsf(o[e]), fabsf(o[e + 1]));
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    o[e] = nan ? undefined : o[e] * inv;
+                    u[e] = __float_as_uint(o[e]);
+                }
+                if (!valid) continue;
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[e] = pack2(o[2 * e], o[2 * e + 1]);
+                    if (c < p.head_dim) store32(out + c, u, tp.out_32, c + 8 < p.head_dim);
+                } else {
+                    store32(part_o + c, u, true, true);
+                    store32(part_o + c + 8, u + 8, true, true);
+                }
             }
-            tc_fence_before();                                                     // (the next product's start waits for the next probabilities)
+            __syncwarp();
+            tc_fence_before();                                                     // (the next product waits for the next probabilities)
             if (valid) {
-                if (!w.whole()) part_ml[r] = make_float2(m, l);
+                if (!whole) tp.part_ml[slot] = make_float2(m, l);
                 else if (p.lse) p.lse[row * p.heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
             }
-            const bool bad = valid && !nan && check != check;
+            const bool bad = valid && !nan && !(check < INFINITY);
             if (__any_sync(0xffffffffu, bad)) {
                 __syncwarp();
-                repair_rows(p, w, qv, bad, part_o, part_ml, HDP);
+                repair_rows(p, w, qv, bad, tp.part_o + (slot - r - half * QTILE) * HDP, tp.part_ml + (slot - r - half * QTILE), HDP, 128 * NH);
             }
-        } else if (have_next && active(next)) {
-            load_q(next);                                                          // (the tile has been free since the item that it was last loaded for)
-            q_ready();
         }
-        w = next;
-        have = have_next;
     }
-    return true;
 }
 
-// MMA warp.  Per unit and half: O += P V, then the scores of the half's next unit, so that one half's softmax runs beside the other's MMAs.
-template <int HDP>
-__device__ __forceinline__ bool mma_role(const TileParams& tp, Control& ctl, uint8_t* q_tiles, uint8_t* ring, Items t) {
+// Q warp: the rows of each item by copies of 16 bytes into the swizzled tiles; rows and elements that do not exist are zero.
+template <int HDP, int NH>
+__device__ __forceinline__ bool query_role(const TileParams& tp, Control& ctl, uint8_t* q_tiles) {
+    const Params& p = tp.a;
+    constexpr int CH = HDP / 8, RPI = 32 / CH;               // chunks of a row, rows at a time
+    const int lane = threadIdx.x & 31, c = lane % CH;
+    uint32_t items[2] = {0, 0};                              // of a half so far
+    Listed list;
+    Item w;
+    for (;; list.done(ctl)) {
+        if (!list.get(ctl, tp, w)) return false;
+        if (w.j1 == 0) return true;
+#pragma unroll 1
+        for (int half = 0; half < NH; ++half) {
+            if (!active<NH>(p, w, half)) continue;
+            if (!__all_sync(0xffffffffu, wait(&ctl.q_empty[half], (items[half] & 1) ^ 1, tp.wait_limit, &ctl.abort_flag))) return false;
+            ++items[half];
+            const uint32_t q_addr = smem_u32(q_tiles) + half * (QTILE * HDP * 2);
+#pragma unroll 1
+            for (int r0 = 0; r0 < QTILE; r0 += 32) {
+                const int qv = (w.qt * NH + half) * QTILE + r0 + lane, i = qv / p.group, h = w.kvh * p.group + (qv - i * p.group);
+                const unsigned long long mine =
+                    qv < w.s.n * p.group ? (unsigned long long)(p.q + (long long)(w.s.row0 + i) * p.q_ld + (long long)h * p.head_dim) : 0;
+#pragma unroll 4
+                for (int k = 0; k < 32 / RPI; ++k) {
+                    const int rr = k * RPI + lane / CH, r = r0 + rr;
+                    const unsigned long long src = __shfl_sync(0xffffffffu, mine, rr);
+                    const bool here = src && c * 8 < p.head_dim;
+                    copy16(q_addr + (c >> 3) * (QTILE * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), here ? (const bf16*)src + c * 8 : p.q, here);
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) arrive(&ctl.q_full[half]);
+        }
+    }
+}
+
+// MMA warps, one per half: a warp that has to look after both needs more time for its instructions and waits (2300 cycles per half and unit)
+// than the tensor core for the MMAs.  The scores of the next step go in front of O += P V.  The tensor core takes MMAs of a thread in the
+// order of their issue: the scores of step u + 1 come behind the product of step u - 1, whose probabilities they overwrite.
+template <int HDP, int NH>
+__device__ __forceinline__ bool mma_role(const TileParams& tp, Control& ctl, uint8_t* q_tiles, uint8_t* ring, int half) {
     const Params& p = tp.a;
     constexpr int SB = KEYS * HDP * 2;
     volatile int* abort_flag = &ctl.abort_flag;
     const int lane = threadIdx.x & 31;
-    const uint32_t tmem = ctl.tmem_slot, idesc_s = idesc_bf16(KEYS, 0), idesc_o = idesc_bf16(HDP, 1);
-    const uint32_t qa = smem_u32(q_tiles), ra = smem_u32(ring);
+    const uint32_t t_s = ctl.tmem_slot + half * 2 * STEP, t_o = ctl.tmem_slot + 256 + half * HDP;
+    // D fp32, A and B bf16, M = 128; A K-major, B K-major (keys) or MN-major (values)
+    constexpr uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(STEP >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    constexpr uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(HDP >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    const uint64_t q_desc = desc_k(smem_u32(q_tiles) + half * (QTILE * HDP * 2)), k_desc = desc_k(smem_u32(ring)), v_desc = desc_mn(smem_u32(ring), KEYS * 128);
     Ring rk, rv;                                             // K of the next scores, V of the next product
     rv.next(tp.stages);
-    uint32_t q_parity[2] = {0, 0}, p_parity[2] = {0, 0};
+    uint32_t steps = 0, items = 0;                           // products, and items whose scores have begun, of this half
     auto all = [&](bool ok) { return __all_sync(0xffffffffu, ok); };
-    auto scores = [&](int half, int stage) {
+    auto given = [&](uint64_t* bar, uint32_t parity) { return all(wait(bar, parity, tp.wait_limit, abort_flag)); };
+    auto step = [&](Ring& r) {
+        r.next(tp.stages);
+        r.next(tp.stages);
+    };
+    // S = Q K^T for the first or second 64 keys of the K tile; behind the second the tile is free, and Q if the item has no more
+    auto scores = [&](int part, bool last) {
         tc_fence_after();
         if (elect()) {
 #pragma unroll
-            for (int k = 0; k < HDP / 16; ++k)
-                umma_bf16(tmem + half * KEYS, desc_k(qa + half * (QTILE * HDP * 2) + (k >> 2) * (QTILE * 128)) + 2 * (k & 3),
-                          desc_k(ra + stage * SB + (k >> 2) * (KEYS * 128)) + 2 * (k & 3), idesc_s, k ? 1u : 0u);
-            umma_commit(&ctl.s_full[half]);
+            for (int k = 0; k < HDP / 16; ++k) {
+                const int at = (k >> 2) * (QTILE * 128 >> 4) + 2 * (k & 3);
+                umma_bf16(t_s + part * STEP, q_desc + at, k_desc + (rk.s * (SB >> 4) + part * (STEP * 128 >> 4) + at), idesc_s, k ? 1u : 0u);
+            }
+            umma_commit(&ctl.s_full[half][part]);
+            if (part) umma_commit(&ctl.empty[rk.s]);
+            if (last) umma_commit(&ctl.q_empty[half]);
         }
         __syncwarp();
+        if (part) step(rk);
     };
-    auto release = [&](Ring& r) {
-        if (elect()) umma_commit(&ctl.empty[r.s]);
-        __syncwarp();
-        r.next(tp.stages);
-        r.next(tp.stages);
-    };
-    auto active = [&](const Item& w, int half) { return w.s.n * p.group > w.qt * QROWS + half * QTILE; };
+    auto is_active = [&](const Item& x) { return active<NH>(p, x, half); };
 
+    Listed list;
     Item w, next;
-    bool have = next_item(p, t, w);
-    int issued = 0;                                          // halves whose first scores of the item are on their way
-    while (have) {
-        const bool have_next = next_item(p, t, next);
-        int issued_next = 0;
-        if (!all(wait(&ctl.full[rk.s], rk.parity, tp.wait_limit, abort_flag))) return false;
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-            if (active(w, half) && !(issued >> half & 1)) {
-                if (!all(wait(&ctl.q_full[half], q_parity[half], tp.wait_limit, abort_flag))) return false;
-                q_parity[half] ^= 1;
-                scores(half, rk.s);
+    if (!list.get(ctl, tp, w)) return false;
+    bool issued = false;                                     // the first scores of the item are on their way
+    while (w.j1) {
+        list.done(ctl);
+        if (!list.get(ctl, tp, next)) return false;
+        if (!is_active(w)) {                                 // gives the stages back
+            for (int j = w.j0; j < w.j1; ++j) {
+                for (Ring* r : {&rk, &rv}) {
+                    if (!given(&ctl.full[r->s], r->parity)) return false;
+                    if (lane == 0) arrive(&ctl.empty[r->s]);
+                    step(*r);
+                }
             }
-        release(rk);
-        for (int j = w.j0; j < w.j1; ++j) {
-            const bool last = j + 1 == w.j1;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (!active(w, half)) continue;
-                if (!all(wait(&ctl.p_full[half], p_parity[half], tp.wait_limit, abort_flag))) return false;
-                p_parity[half] ^= 1;
-                if (half == 0) {                             // (half 0 of an item is never empty)
-                    if (!all(wait(&ctl.full[rv.s], rv.parity, tp.wait_limit, abort_flag))) return false;
-                    const int n = w.s.kv - j * KEYS;         // tokens of the tile
-                    if (n < KEYS) {
-                        // values behind the last token are whatever stands in the page or in the ring: a NaN times a probability of zero is a NaN
-                        for (int e = lane; e < (KEYS - max(n, 0)) * (HDP / 64) * 8; e += 32) {
-                            const int r = max(n, 0) + (e >> 3) / (HDP / 64), c = e & 7, hh = (e >> 3) % (HDP / 64);
-                            *reinterpret_cast<uint4*>(ring + rv.s * SB + hh * (KEYS * 128) + r * 128 + c * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_async_shared();
-                        __syncwarp();
+            w = next;
+            continue;
+        }
+        if (!issued) {
+            if (!given(&ctl.q_full[half], items & 1) || !given(&ctl.full[rk.s], rk.parity)) return false;
+            scores(0, false);
+            ++items;
+        }
+        issued = false;
+        const int n_steps = 2 * (w.j1 - w.j0);
+#pragma unroll 1
+        for (int u = 0; u < n_steps; ++u, ++steps) {
+            const int part = u & 1;
+            // the scores of the next step: of this item, or of the next one if all that they need is there
+            if (u + 1 < n_steps) {
+                if (part && !given(&ctl.full[rk.s], rk.parity)) return false;
+                scores(part ^ 1, u + 2 == n_steps);
+            } else if (next.j1 && is_active(next) && all(peek(&ctl.q_full[half], items & 1) && peek(&ctl.full[rk.s], rk.parity))) {
+                scores(0, false);
+                issued = true;
+                ++items;
+            }
+            if (!part) {
+                if (!given(&ctl.full[rv.s], rv.parity)) return false;
+                const int n = max(w.s.kv - (w.j0 + (u >> 1)) * KEYS, 0);          // tokens of the tile
+                if (n < KEYS) {
+                    // values behind the last token are whatever stands in the page or in the ring: a NaN times a probability of zero is a
+                    // NaN (both MMA warps write the same zeros)
+                    for (int e = lane; e < (KEYS - n) * (HDP / 64) * 8; e += 32) {
+                        const int r = n + (e >> 3) / (HDP / 64), c = e & 7, hh = (e >> 3) % (HDP / 64);
+                        *reinterpret_cast<uint4*>(ring + rv.s * SB + hh * (KEYS * 128) + r * 128 + c * 16) = make_uint4(0, 0, 0, 0);
                     }
-                }
-                tc_fence_after();
-                if (elect()) {
-#pragma unroll
-                    for (int k = 0; k < KEYS / 16; ++k)
-                        umma_bf16_ta(tmem + 2 * KEYS + half * HDP, tmem + half * KEYS + k * 8, desc_mn(ra + rv.s * SB + k * 2048, KEYS * 128), idesc_o,
-                                     (j > w.j0 || k) ? 1u : 0u);
-                    if (last) umma_commit(&ctl.o_full[half]);
-                }
-                __syncwarp();
-                if (!last) {
-                    if (half == 0 && !all(wait(&ctl.full[rk.s], rk.parity, tp.wait_limit, abort_flag))) return false;
-                    scores(half, rk.s);
-                } else if (have_next && active(next, half) && all(poll(&ctl.q_full[half], q_parity[half])) && all(poll(&ctl.full[rk.s], rk.parity))) {
-                    q_parity[half] ^= 1;                     // the next item's first scores, if everything is there
-                    scores(half, rk.s);
-                    issued_next |= 1 << half;
+                    fence_async_shared();
+                    __syncwarp();
                 }
             }
-            release(rv);
-            if (!last) release(rk);
+            if (!given(&ctl.p_full[half][part], steps >> 1 & 1)) return false;
+            tc_fence_after();
+            if (elect()) {                                   // 64 keys of O += P V
+#pragma unroll
+                for (int k = 0; k < STEP / 16; ++k)
+                    umma_bf16_ta(t_o, t_s + part * STEP + k * 8, v_desc + (rv.s * (SB >> 4) + part * (STEP * 128 >> 4) + k * 128), idesc_o, u || k ? 1u : 0u);
+                umma_commit(&ctl.o_full[half][part]);
+                if (part) umma_commit(&ctl.empty[rv.s]);
+            }
+            __syncwarp();
+            if (part) step(rv);
         }
         w = next;
-        have = have_next;
-        issued = issued_next;
     }
     return true;
 }
 
-// Copy warp: K and V tiles of 128 keys, page by page (a lane per page), in the order in which the MMA warp takes them.
-template <int HDP>
+// Copy warp: lists the items for the others, and loads their K and V tiles of 128 keys, page by page (a lane per page), in the order in which the
+// MMA warp takes them.
+template <int HDP, int NH>
 __device__ __forceinline__ bool copy_role(const TileParams& tp, Control& ctl, uint8_t* ring, Items t, const CUtensorMap* map_k, const CUtensorMap* map_v) {
     const Params& p = tp.a;
     constexpr int SB = KEYS * HDP * 2;
@@ -674,8 +808,23 @@ __device__ __forceinline__ bool copy_role(const TileParams& tp, Control& ctl, ui
     const uint32_t ra = smem_u32(ring);
     Ring r;
     r.parity = 1;                                            // a fresh barrier passes a wait for the phase before its first
-    Item w;
-    for (int index = 0; next_item(p, t, w); ++index) {
+    // The next item, or the end, is listed before this one's tiles are loaded: the MMA warp wants to know what comes behind an item that
+    // it gives room for.
+    Item w, next;
+    auto publish = [&](int index, Item& x) {
+        if (!next_item<NH>(p, t, x)) x.j1 = 0;
+        if (!__all_sync(0xffffffffu, wait(&ctl.item_empty[index % ITEMS], (index / ITEMS & 1) ^ 1, tp.wait_limit, &ctl.abort_flag))) return false;
+        if (lane == 0) {
+            ctl.items[index % ITEMS] = x;
+            if (x.j1) note_split(tp, ctl.setup, x);
+            arrive(&ctl.item_full[index % ITEMS]);
+        }
+        __syncwarp();
+        return true;
+    };
+    if (!publish(0, w)) return false;
+    for (int index = 0; w.j1; ++index, w = next) {
+        if (!publish(index + 1, next)) return false;
         for (int j = w.j0; j < w.j1; ++j) {
             const int key = j * KEYS + lane * box;
             bool some = lane < pages && key < w.s.kv;
@@ -706,23 +855,28 @@ __device__ __forceinline__ bool copy_role(const TileParams& tp, Control& ctl, ui
     return true;
 }
 
-template <int HDP>
-__global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TileParams tp) {
+template <int HDP, int NH>
+__global__ void __launch_bounds__(threads(NH), 1)
+tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TileParams tp) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* base = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t* ring = base + 2 * QTILE * HDP * 2;
+    uint8_t* ring = base + NH * QTILE * HDP * 2;
     Control& ctl = *(Control*)(base + tp.control_at);
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < tp.stages; ++s) mbar_init(&ctl.full[s], 1), mbar_init(&ctl.empty[s], 1);
-        for (int h = 0; h < 2; ++h) mbar_init(&ctl.q_full[h], 128), mbar_init(&ctl.s_full[h], 1), mbar_init(&ctl.p_full[h], 128), mbar_init(&ctl.o_full[h], 1);
+        for (int s = 0; s < tp.stages; ++s) mbar_init(&ctl.full[s], 1), mbar_init(&ctl.empty[s], NH);
+        for (int i = 0; i < ITEMS; ++i) mbar_init(&ctl.item_full[i], 1), mbar_init(&ctl.item_empty[i], 4 * NH + NH + 1);      // softmax, MMA, Q
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(&ctl.q_full[h], 1), mbar_init(&ctl.q_empty[h], 1);
+            for (int i = 0; i < 2; ++i) mbar_init(&ctl.s_full[h][i], 1), mbar_init(&ctl.p_full[h][i], 128), mbar_init(&ctl.o_full[h][i], 1);
+        }
         ctl.abort_flag = 0;
-        for (int i = 0; i < 16; ++i) ctl.bad[i] = 0;
+        for (int i = 0; i < 2 * ITEMS; ++i) ctl.bad[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
-    if (warp == 8) {
+    if (warp == 4 * NH) {
         tmem_alloc(&ctl.tmem_slot, 512);
         tmem_relinquish();
     }
@@ -733,17 +887,12 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     // all warps: nothing in front reads or writes what this kernel does, and the bounded waits begin behind it
     pdl_wait();
     Items items;
-    plan(tp, ctl.setup, items);
+    plan<NH>(tp, ctl.setup, items);
     bool ok = true;
-    // 168 registers per thread at launch: 2 x 216 + 72 = 3 x 168
-    if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        ok = softmax_role<HDP>(tp, ctl, base, items, warp >> 2);
-    } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == 8) ok = mma_role<HDP>(tp, ctl, base, ring, items);
-        else if (warp == 9) ok = copy_role<HDP>(tp, ctl, ring, items, &map_k, &map_v);
-    }
+    if (warp < 4 * NH) ok = softmax_role<HDP, NH>(tp, ctl);
+    else if (warp == 4 * NH) ok = copy_role<HDP, NH>(tp, ctl, ring, items, &map_k, &map_v);
+    else if (warp == 4 * NH + 1) ok = query_role<HDP, NH>(tp, ctl, base);
+    else if (warp - 4 * NH - 2 < NH) ok = mma_role<HDP, NH>(tp, ctl, base, ring, warp - 4 * NH - 2);
     if (!ok) *(volatile int*)&ctl.abort_flag = 1;
     __syncwarp();
     __syncthreads();
@@ -754,10 +903,10 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) tmem_dealloc(ctl.tmem_slot, 512);
+    if (warp == 4 * NH) tmem_dealloc(ctl.tmem_slot, 512);
     if (failed) {
         if (threadIdx.x == 0) atomicAdd(tp.timeouts, 1);
-        all_nan(tp, ctl.setup, items, HDP);
+        all_nan<NH>(tp, ctl.setup, items, HDP);
     }
 }
 
@@ -773,7 +922,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ TileP
     const int4 d = tp.split[2 * c];
     if (d.x < 0) return;
     const int4 s = tp.split[2 * c + 1];
-    const int q0 = d.z * QROWS, n = min(QROWS, s.y * p.group - q0), lane = threadIdx.x & 31;
+    const int q0 = d.z * tp.rows, n = min(tp.rows, s.y * p.group - q0), lane = threadIdx.x & 31;
     for (int r = blockIdx.y * 32 + (threadIdx.x >> 5); r < min(n, (int)blockIdx.y * 32 + 32); r += 8) {
         float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
@@ -781,8 +930,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ TileP
 #pragma unroll 4
         for (int part = c; part <= d.w; ++part) {
             const size_t slot = 2 * part + (part == c);
-            const float2 ml = tp.part_ml[slot * QROWS + r];
-            const float* src = tp.part_o + (slot * QROWS + r) * HDP + lane * E;
+            const float2 ml = tp.part_ml[slot * tp.rows + r];
+            const float* src = tp.part_o + (slot * tp.rows + r) * HDP + lane * E;
             float x[E];
             if constexpr (E == 4) {
                 const float4 v = *reinterpret_cast<const float4*>(src);

@@ -170,6 +170,12 @@ def test_many_sequences(s2d2):
     run(s2d2, lens, 2, 1, 64, page=16)
 
 
+@pytest.mark.parametrize("n", [1, 40, 300])
+def test_many_units_per_cta(s2d2, n):
+    """Items far longer than the ring of tiles, short ones in front of and behind them."""
+    run(s2d2, [(1, 60), (n, 30000), (n, 31000), (0, 100), (n, 300), (2, 29000), (1, 5)], 4, 4, 64, seed=n)
+
+
 def test_without_lse_and_with_output_padding(s2d2):
     b = au.Batch([(4, 90), (130, 200)], 4, 2, 64)
     want = b.want()
