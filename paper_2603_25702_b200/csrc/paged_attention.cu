@@ -27,19 +27,24 @@ int check_shape(const char* op, const s2d2_rows* rows, const s2d2_paged_kv* kv, 
 
 // How the work is cut, from what the host knows.
 struct Plan {
-    int hdp, nh, ctas, stages, smem, control_at;
+    int hdp, nh, gs, rows_half, ctas, stages, smem, control_at;
     bool joins;                      // an item may be cut
     long long ml_at, o_at, bytes;    // of the workspace
+    double costs;                    // units, at most
 };
 Plan make_plan(const s2d2_rows* rows, const s2d2_paged_kv* kv, int n_q_heads) {
     Plan n;
     n.hdp = kv->head_dim > 64 ? 128 : 64;
-    const long long group = n_q_heads / kv->n_kv_heads, most = std::max(1LL, ((long long)rows->max_pages * kv->page_tokens + patt::KEYS - 1) / patt::KEYS);
-    // items of 128 query vectors where no sequence has more, as far as the host knows
-    n.nh = rows->max_rows * group <= patt::QTILE ? 1 : 2;
-    const int per = patt::QTILE * n.nh;
-    const long long items = (rows->n_rows * group + per - 1) / per + std::min(rows->n_seqs, rows->n_rows);
-    n.ctas = (int)std::min<long long>(patt::MAX_CTAS, items * most >= patt::MAX_CTAS ? patt::MAX_CTAS : items * most * kv->n_kv_heads);
+    const int group = n_q_heads / kv->n_kv_heads;
+    n.gs = std::min(group, patt::QTILE);
+    while (group % n.gs) --n.gs;
+    n.rows_half = patt::QTILE / n.gs;
+    // items of one tile where no sequence has more rows, as far as the host knows
+    n.nh = rows->max_rows <= n.rows_half ? 1 : 2;
+    const long long most = std::max(1LL, ((long long)rows->max_pages * kv->page_tokens + patt::KEYS - 1) / patt::KEYS), per = n.nh * n.rows_half;
+    const long long items = (rows->n_rows + per - 1) / per + std::min(rows->n_seqs, rows->n_rows);
+    n.costs = (double)items * (double)(most + 1) * (n_q_heads / n.gs);
+    n.ctas = (int)std::min<double>(patt::MAX_CTAS, std::max(1., (double)items * (double)most * (n_q_heads / n.gs)));
     n.joins = most > 1;
     const int stage = patt::KEYS * n.hdp * 2, q = n.nh * patt::QTILE * n.hdp * 2, most_smem = 227 * 1024 - 1024 - (int)sizeof(patt::Control);
     n.stages = std::min(patt::MAX_STAGES, (most_smem - q) / stage);
@@ -47,8 +52,8 @@ Plan make_plan(const s2d2_rows* rows, const s2d2_paged_kv* kv, int n_q_heads) {
     // (at least 200 KB: no other CTA that takes tensor memory is on the SM, so taking all of it does not wait)
     n.smem = std::max(200 * 1024, 1024 + n.control_at + (int)sizeof(patt::Control));
     n.ml_at = n.ctas * 32LL;
-    n.o_at = n.ml_at + (n.joins ? 2LL * n.ctas * per * 8 : 0);      // (a multiple of 32)
-    n.bytes = n.o_at + (n.joins ? 2LL * n.ctas * per * n.hdp * 4 : 0);
+    n.o_at = n.ml_at + (n.joins ? 2LL * n.ctas * patt::QTILE * n.nh * 8 : 0);      // (a multiple of 32)
+    n.bytes = n.o_at + (n.joins ? 2LL * n.ctas * patt::QTILE * n.nh * n.hdp * 4 : 0);
     return n;
 }
 
@@ -63,10 +68,21 @@ int encode(const ops::Device* dev, CUtensorMap* map, const void* base, const s2d
     return r == CUDA_SUCCESS ? S2D2_OK : ops::fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
 }
 
+// Queries as [row][head][element] in boxes of a tile's rows x heads x 64 elements.
+int encode_q(const ops::Device* dev, CUtensorMap* map, const void* q, long long q_stride, int n_rows, int heads, int head_dim, const Plan& n) {
+    cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)n_rows};
+    cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)q_stride * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)n.gs, (cuuint32_t)n.rows_half}, step[3] = {1, 1, 1};
+    const CUresult r = dev->encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, step,
+                                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? S2D2_OK : ops::fail(S2D2_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+
 template <int HDP, int NH>
-cudaError_t launch_tiles(const CUtensorMap& map_k, const CUtensorMap& map_v, const patt::TileParams& t, const Plan& n, cudaStream_t st) {
-    cudaError_t e = ops::launch(patt::tile_kernel<HDP, NH>, dim3(n.ctas), patt::threads(NH), n.smem, 1, st, map_k, map_v, t);
-    if (!e && n.joins) e = ops::launch(patt::join_kernel<HDP>, dim3(n.ctas, 4 * NH), 256, 0, 1, st, t);
+cudaError_t launch_tiles(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const patt::TileParams& t, const Plan& n, cudaStream_t st) {
+    cudaError_t e = ops::launch(patt::tile_kernel<HDP, NH>, dim3(n.ctas), patt::threads(NH), n.smem, 1, st, map_q, map_k, map_v, t);
+    if (!e && n.joins) e = ops::launch(patt::join_kernel<HDP, NH>, dim3(n.ctas, 4 * NH), 1024, 0, 1, st, t);
     return e;
 }
 
@@ -79,8 +95,10 @@ cudaError_t load_attention_kernels() {
     if (!e) e = load(patt::tile_kernel<64, 2>, most);
     if (!e) e = load(patt::tile_kernel<128, 1>, most);
     if (!e) e = load(patt::tile_kernel<128, 2>, most);
-    if (!e) e = load(patt::join_kernel<64>);
-    return e ? e : load(patt::join_kernel<128>);
+    if (!e) e = load(patt::join_kernel<64, 1>);
+    if (!e) e = load(patt::join_kernel<64, 2>);
+    if (!e) e = load(patt::join_kernel<128, 1>);
+    return e ? e : load(patt::join_kernel<128, 2>);
 }
 }  // namespace ops
 }  // namespace s2d2
@@ -110,6 +128,7 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     if (!(scale > 0.f) || !isfinite(scale)) return ops::fail(S2D2_ERR_INVALID, "%s: scale must be positive", op);
     const Plan n = make_plan(rows, kv, n_q_heads);
     const bool work = rows->n_rows && rows->n_seqs;
+    if (n.costs > 2e9) return ops::fail(S2D2_ERR_UNSUPPORTED, "%s: rows x max_pages: too much for one call", op);
     if (work && ws_bytes < n.bytes) return ops::fail(S2D2_ERR_INVALID, "%s: workspace of %lld bytes, needs %lld", op, (long long)ws_bytes, n.bytes);
     const ops::Device* dev;
     if (int rc = ops::device(&dev)) return rc;
@@ -137,17 +156,21 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     p.group = n_q_heads / kv->n_kv_heads;
     p.head_dim = kv->head_dim;
     p.scale_log2 = scale * 1.4426950408889634f;
-    CUtensorMap map_k, map_v;
+    CUtensorMap map_q, map_k, map_v;
+    if (int rc = encode_q(dev, &map_q, d_q, q_stride, rows->n_rows, n_q_heads, kv->head_dim, n)) return rc;
     if (int rc = encode(dev, &map_k, kv->d_k, kv)) return rc;
     if (int rc = encode(dev, &map_v, kv->d_v, kv)) return rc;
     t.ctas = n.ctas;
     t.stages = n.stages;
     t.control_at = n.control_at;
-    // threads per sequence when units are counted: as many as it may have items, as long as one round takes all sequences
-    t.rows = patt::QTILE * n.nh;
+    t.gs = n.gs;
+    t.vsub = p.group / n.gs;
+    t.rows_half = n.rows_half;
+    const uint32_t per = n.rows_half * n.nh;
+    t.items_magic = per == 1 ? 0u : (uint32_t)((0x100000000ULL + per - 1) / per);
+    // lanes per sequence when units are counted: as many as it may have items, as long as one round takes all sequences
     t.seq_lanes = 1;
-    while (t.seq_lanes < 32 && t.seq_lanes * t.rows < (long long)rows->max_rows * p.group && (long long)rows->n_seqs * t.seq_lanes * 2 <= patt::threads(n.nh))
-        t.seq_lanes *= 2;
+    while (t.seq_lanes < 32 && (long long)t.seq_lanes * per < rows->max_rows && (long long)rows->n_seqs * t.seq_lanes * 2 <= 32) t.seq_lanes *= 2;
     t.split = (int4*)d_ws;
     t.part_ml = (float2*)((char*)d_ws + n.ml_at);
     t.part_o = (float*)((char*)d_ws + n.o_at);
@@ -158,7 +181,7 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     g_wait_limit = tc::WAIT_LIMIT;
     g_withhold = 0;
     const auto launch = n.hdp == 128 ? (n.nh == 1 ? launch_tiles<128, 1> : launch_tiles<128, 2>) : (n.nh == 1 ? launch_tiles<64, 1> : launch_tiles<64, 2>);
-    const cudaError_t e = launch(map_k, map_v, t, n, (cudaStream_t)cuda_stream);
+    const cudaError_t e = launch(map_q, map_k, map_v, t, n, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return ops::fail(S2D2_ERR_CUDA, "%s: %s", op, cudaGetErrorString(e));

@@ -2,9 +2,9 @@
 //
 //   O[row] = sum_j p_j V[j] / sum_j p_j,   p_j = 2^(s_j - m),   s = scale log2(e) Q K^T,   in one pass over the keys with a running m and sum
 //
-// The query vectors of a kv head are its sequence's rows times the group of heads that read it (row-major: vector = row * group + head
-// of the group), so K and V are read once for a whole group.  An item is (sequence, kv head, 256 or 128 query vectors); its units are the
-// tiles of 128 keys that any of its rows sees.  All units, in the order of the items, are cut into as many equal ranges as there
+// The query vectors of a kv head are its sequence's rows times the group of heads that read it, so K and V are read once for a whole group:
+// a MMA tile of 128 takes as many whole rows as fit (128 / group; of a group above 128 the largest part of it that divides it).  An item is
+// (sequence, heads, one or two tiles of query vectors, its halves); its units are the tiles of 128 keys that any of its rows sees.  All units, in the order of the items, are cut into as many equal ranges as there
 // are CTAs (an item counts one unit more than it has: its start and its end cost about as much), so that a long cache is shared by many
 // CTAs, many short sequences by few, and a ragged batch evenly.  Items that a cut went through leave parts (maximum, sum, weighted
 // values) in the workspace, which join_kernel adds up in the order of the keys: deterministic, no tickets.  Lengths are read on
@@ -72,10 +72,6 @@ __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* map, in
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
         : "memory");
-}
-// 16 bytes to shared memory, or 16 zeros
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool some) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
 }
 // Operand tiles are rows of 128 bytes with the 128-byte swizzle: K-major (Q, K), or MN-major where the rows are the k index (V)
 __device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
@@ -154,12 +150,14 @@ struct TileParams {
     Params a;
     int ctas;                        // CTAs that share the units, at most
     int stages;
-    int rows;                        // query vectors of an item: 128 NH
-    int seq_lanes;                   // threads that count a sequence's units: a power of two up to 32
+    int gs, vsub;                    // heads of a tile; tiles' heads in a group
+    int rows_half;                   // rows of a tile: 128 / gs
+    uint32_t items_magic;            // n / (rows of an item) = n * items_magic >> 32 for n below 2^23; 0: an item is a row
+    int seq_lanes;                   // lanes that count a sequence's units: a power of two up to 32
     int control_at;                  // byte offset of Control
-    float* part_o;                   // [2 ctas][rows][HDP]
-    float2* part_ml;                 // [2 ctas][rows]: reference, sum
-    int4* split;                     // [ctas][2]: the item that CTA c begins and does not end: sequence, kv head, item, last CTA; row0, n, kv, ok (sequence -1: none)
+    float* part_o;                   // [2 ctas][128 NH][HDP]
+    float2* part_ml;                 // [2 ctas][128 NH]: reference, sum
+    int4* split;                     // [ctas][2]: the item that CTA c begins and does not end: first head (-1: none), item, last CTA, row0; n
     int* timeouts;
     uint32_t wait_limit;
     int out_32;                      // rows of heads of the output are multiples of 32 bytes and aligned to them
@@ -172,33 +170,35 @@ __device__ __forceinline__ paged::Seq usable_seq(const Params& p, int s) {      
     return q;
 }
 template <int NH>
-__device__ __forceinline__ int items_of(const Params& p, int n) { return (n * p.group + 128 * NH - 1) / (128 * NH); }
+__device__ __forceinline__ int items_of(const TileParams& tp, int n) {
+    return tp.items_magic ? (int)__umulhi((uint32_t)(n + NH * tp.rows_half - 1), tp.items_magic) : n;
+}
 // Units of item qt of a sequence: at least one, so that rows that see nothing are written.
 template <int NH>
-__device__ __forceinline__ int units_of(const Params& p, const paged::Seq& s, int qt) {
-    const int last = (min(s.n * p.group, (qt + 1) * 128 * NH) - 1) / p.group;
-    const int end = paged::key_end(p.mask_block, p.row_mask != nullptr, s.n, s.kv, last);
+__device__ __forceinline__ int units_of(const TileParams& tp, const paged::Seq& s, int qt) {
+    const int end = paged::key_end(tp.a.mask_block, tp.a.row_mask != nullptr, s.n, s.kv, min(s.n, (qt + 1) * NH * tp.rows_half) - 1);
     return max(1, (end + KEYS - 1) / KEYS);
 }
 
 // The items of a CTA's range, one after the other.  Ranges are in costs: an item has `extra` in front of its units.
 struct Items {
-    int seq, kvh, qt, extra;
-    long long at, left;              // costs of item qt in front of the range, costs of the range that are left
+    int seq, vh, qt, extra;
+    int at, left;                    // costs of item qt in front of the range, costs of the range that are left
     paged::Seq s;                    // of seq
 };
 struct Item {
     paged::Seq s;
-    int seq, kvh, qt, j0, j1, units;     // j1 = 0: there are no more
+    int seq, kvh, head0, qt, j0, j1, units;     // head0: first query head; j1 = 0: there are no more
     __device__ __forceinline__ bool whole() const { return j0 == 0 && j1 == units; }
 };
 template <int NH>
-__device__ __forceinline__ bool next_item(const Params& p, Items& t, Item& w) {
+__device__ __forceinline__ bool next_item(const TileParams& tp, Items& t, Item& w) {
+    const Params& p = tp.a;
     while (t.left > 0) {
-        while (t.qt >= items_of<NH>(p, t.s.n)) {       // behind the last item of a head
+        while (t.qt >= items_of<NH>(tp, t.s.n)) {      // behind the last item of these heads
             t.qt = 0;
-            if (t.s.n == 0 || ++t.kvh >= p.kv_heads) {
-                t.kvh = 0;
+            if (t.s.n == 0 || ++t.vh >= p.kv_heads * tp.vsub) {
+                t.vh = 0;
                 if (++t.seq >= p.b.n_seqs) {           // (cannot be: the range ends with the last unit)
                     t.left = 0;
                     return false;
@@ -208,12 +208,13 @@ __device__ __forceinline__ bool next_item(const Params& p, Items& t, Item& w) {
         }
         w.s = t.s;
         w.seq = t.seq;
-        w.kvh = t.kvh;
+        w.kvh = tp.vsub == 1 ? t.vh : t.vh / tp.vsub;
+        w.head0 = t.vh * tp.gs;
         w.qt = t.qt;
-        w.units = units_of<NH>(p, t.s, t.qt);
-        const long long end = min(t.at + t.left, (long long)w.units + t.extra);
-        w.j0 = (int)max(0LL, t.at - t.extra);
-        w.j1 = (int)max(0LL, end - t.extra);
+        w.units = units_of<NH>(tp, t.s, t.qt);
+        const int end = min(t.at + t.left, w.units + t.extra);
+        w.j0 = max(0, t.at - t.extra);
+        w.j1 = max(0, end - t.extra);
         t.left -= end - t.at;
         t.at = 0;
         ++t.qt;
@@ -223,139 +224,120 @@ __device__ __forceinline__ bool next_item(const Params& p, Items& t, Item& w) {
 }
 
 struct Setup {
-    long long warp_sum[threads(2) / 32];
-    long long front;                 // costs in front of the sequence of the range's begin
-    long long total, ctas, u1;       // all costs, the CTAs that share them, the end of this CTA's range
+    uint32_t u1, base, more;         // end of this CTA's range; costs of a CTA, CTAs that have one more
     Items first;
 };
 
-// All threads: the begin of this CTA's range and its length, from the lengths on the device.  Sequences are counted threads / seq_lanes at
-// a time.
+// One warp: the begin of this CTA's range and its length, from the lengths on the device.  Sequences are counted 32 / seq_lanes at a time.
 template <int NH>
 __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out) {
-    constexpr int NT = threads(NH);
     const Params& p = tp.a;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = NT / tp.seq_lanes;
-    // items (from bit 40 on; below 2^23) and units of a sequence, by seq_lanes threads; the first of them has the sums
-    auto count = [&](int s) -> long long {
-        long long n = 0;
+    const int lane = threadIdx.x & 31, per = 32 / tp.seq_lanes, heads = p.kv_heads * tp.vsub;
+    // items (x) and units (y) of a sequence, by seq_lanes lanes; the first of them has the sums
+    auto count = [&](int s) {
+        uint2 n = make_uint2(0, 0);
         if (s < p.b.n_seqs) {
             const paged::Seq q = usable_seq(p, s);
-            const int items = items_of<NH>(p, q.n);
-            for (int t = tid & (tp.seq_lanes - 1); t < items; t += tp.seq_lanes) n += units_of<NH>(p, q, t) + (1LL << 40);
+            const int items = items_of<NH>(tp, q.n);
+            for (int t = lane & (tp.seq_lanes - 1); t < items; t += tp.seq_lanes) n.y += units_of<NH>(tp, q, t), ++n.x;
         }
-        for (int o = tp.seq_lanes >> 1; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        return (tid & (tp.seq_lanes - 1)) ? 0 : n;
+        for (int o = tp.seq_lanes >> 1; o; o >>= 1) n.x += __shfl_xor_sync(0xffffffffu, n.x, o), n.y += __shfl_xor_sync(0xffffffffu, n.y, o);
+        return (lane & (tp.seq_lanes - 1)) ? make_uint2(0, 0) : n;
     };
-    auto cost = [&](long long n, int extra) { return ((n & ((1LL << 40) - 1)) + (n >> 40) * extra) * p.kv_heads; };
-    long long mine = 0, before = 0;
-    // sum over the CTA's threads; `before` is that of the threads in front of this one
-    auto scan = [&](long long v) -> long long {
-        long long x = v;
+    uint2 mine = make_uint2(0, 0);
+    uint32_t items = 0, units = 0;
+#pragma unroll 2
+    for (int s0 = 0; s0 < p.b.n_seqs; s0 += per) {
+        mine = count(s0 + lane / tp.seq_lanes);
+        items += mine.x, units += mine.y;
+    }
+    items = __reduce_add_sync(0xffffffffu, items);
+    units = __reduce_add_sync(0xffffffffu, units);
+    out.left = 0;
+    if (lane == 0) tp.split[2 * blockIdx.x] = make_int4(-1, 0, 0, 0), sh.first.left = 0;
+    // With few units per CTA every one of them counts more than an even spread of starts and ends
+    const uint32_t extra = (unsigned long long)units * heads > 4ull * tp.ctas ? 1 : 0;
+    const uint32_t total = (units + extra * items) * heads, ctas = min((uint32_t)tp.ctas, total), c = blockIdx.x;
+    if (c >= ctas) return;
+    const uint32_t base = total / ctas, more = total - base * ctas;
+    const uint32_t u0 = c * base + min(c, more), u1 = u0 + base + (c < more);
+    uint32_t front = 0, at = 0;
+    int seq = 0;
+    for (int s0 = 0; s0 < p.b.n_seqs; s0 += per) {
+        if (p.b.n_seqs > per) mine = count(s0 + lane / tp.seq_lanes);
+        const uint32_t cost = (mine.y + extra * mine.x) * heads;
+        uint32_t x = cost;                     // inclusive sums
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, x, o);
+            const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
-        __syncthreads();
-        if (lane == 31) sh.warp_sum[warp] = x;
-        __syncthreads();
-        long long all = 0, front = 0;
-#pragma unroll
-        for (int i = 0; i < NT / 32; ++i) {
-            if (i == warp) front = all;
-            all += sh.warp_sum[i];
+        const unsigned in = __ballot_sync(0xffffffffu, u0 < front + x);
+        if (in) {                              // the first lane whose sum is above
+            const int i = __ffs(in) - 1;
+            seq = s0 + i / tp.seq_lanes;
+            at = u0 - (front + __shfl_sync(0xffffffffu, x - cost, i));
+            break;
         }
-        before = front + x - v;
-        return all;
-    };
-    long long sum = 0;
-    for (int s0 = 0; s0 < p.b.n_seqs; s0 += per) {
-        mine = count(s0 + tid / tp.seq_lanes);
-        sum += scan(mine);
+        front += __shfl_sync(0xffffffffu, x, 31);
     }
-    out.left = 0;
-    if (tid == 0) tp.split[2 * blockIdx.x] = make_int4(-1, 0, 0, 0);
-    // With few units per CTA every one of them counts more than an even spread of starts and ends
-    const int extra = cost(sum, 0) > 4LL * tp.ctas ? 1 : 0;
-    const long long total = cost(sum, extra), ctas = min((long long)tp.ctas, total), c = blockIdx.x;
-    if (c >= ctas) return;
-    const long long u0 = total * c / ctas, u1 = total * (c + 1) / ctas;
-    long long base = 0;
-    for (int s0 = 0; s0 < p.b.n_seqs; s0 += per) {
-        if (p.b.n_seqs > per) mine = count(s0 + tid / tp.seq_lanes);
-        const long long all = p.b.n_seqs > per ? scan(mine) : sum;
-        const long long lo = base + cost(before, extra);
-        if (mine > 0 && lo <= u0 && u0 < lo + cost(mine, extra)) {
-            sh.first.seq = s0 + tid / tp.seq_lanes;
-            sh.front = lo;
-        }
-        base += cost(all, extra);
-        if (u0 < base) break;                  // (the same for all threads)
-    }
-    __syncthreads();
-    if (warp == 0) {                           // the head and the item inside the sequence
-        Items t;
-        t.seq = sh.first.seq;
-        t.s = usable_seq(p, t.seq);
-        t.extra = extra;
-        const int items = items_of<NH>(p, t.s.n);
-        long long per_head = 0;
-        for (int i = lane; i < items; i += 32) per_head += units_of<NH>(p, t.s, i) + extra;
+    // the heads and the item inside the sequence
+    Items t;
+    t.seq = seq;
+    t.s = usable_seq(p, seq);
+    t.extra = (int)extra;
+    const int n_items = items_of<NH>(tp, t.s.n);
+    uint32_t per_head = 0;
+    for (int i = lane; i < n_items; i += 32) per_head += units_of<NH>(tp, t.s, i) + extra;
+    per_head = __reduce_add_sync(0xffffffffu, per_head);
+    t.vh = at / per_head;
+    at -= t.vh * per_head;
+    for (t.qt = 0; t.qt + 1 < n_items; t.qt += 32) {          // 32 items at a time
+        const uint32_t n = t.qt + lane < n_items ? units_of<NH>(tp, t.s, t.qt + lane) + extra : 0;
+        uint32_t x = n;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) per_head += __shfl_xor_sync(0xffffffffu, per_head, o);
-        long long rest = u0 - sh.front;
-        t.kvh = (int)(rest / per_head);
-        rest -= t.kvh * per_head;
-        for (t.qt = 0;; t.qt += 32) {          // 32 items at a time
-            const int n = t.qt + lane < items ? units_of<NH>(p, t.s, t.qt + lane) + extra : 0;
-            int x = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            const unsigned in = __ballot_sync(0xffffffffu, rest < x);      // inclusive sums grow: the first lane above
-            if (in) {
-                const int i = __ffs(in) - 1;
-                rest -= __shfl_sync(0xffffffffu, x - n, i);
-                t.qt += i;
-                break;
-            }
-            rest -= __shfl_sync(0xffffffffu, x, 31);
-            if (t.qt + 32 >= items) {          // (cannot be)
-                rest = 0;
-                break;
-            }
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
         }
-        t.at = rest;
-        t.left = u1 - u0;
-        if (lane == 0) sh.first = t, sh.total = total, sh.ctas = ctas, sh.u1 = u1;
+        const unsigned in = __ballot_sync(0xffffffffu, at < x);
+        if (in) {
+            const int i = __ffs(in) - 1;
+            at -= __shfl_sync(0xffffffffu, x - n, i);
+            t.qt += i;
+            break;
+        }
+        at -= __shfl_sync(0xffffffffu, x, 31);
     }
-    __syncthreads();
-    out = sh.first;
+    t.at = (int)at;
+    t.left = (int)(u1 - u0);
+    if (lane == 0) sh.first = t, sh.u1 = u1, sh.base = base, sh.more = more;
+    __syncwarp();
+    out = t;
 }
 // Notes the item that this CTA's range begins and does not end for join_kernel (one thread).
 __device__ __forceinline__ void note_split(const TileParams& tp, const Setup& sh, const Item& w) {
     if (w.j0 || w.j1 == w.units) return;
-    const long long end = sh.u1 + (w.units - w.j1);          // behind its last unit
-    tp.split[2 * blockIdx.x] = make_int4(w.seq, w.kvh, w.qt, (int)((end * sh.ctas + sh.total - 1) / sh.total - 1));
-    tp.split[2 * blockIdx.x + 1] = make_int4(w.s.row0, w.s.n, w.s.kv, w.s.ok);
+    const uint32_t last = sh.u1 + (w.units - w.j1) - 1, longer = sh.more * (sh.base + 1);      // its last unit; costs of the CTAs with one more
+    const uint32_t cta = last < longer ? last / (sh.base + 1) : sh.more + (last - longer) / sh.base;
+    tp.split[2 * blockIdx.x] = make_int4(w.head0, w.qt, (int)cta, w.s.row0);
+    tp.split[2 * blockIdx.x + 1] = make_int4(w.s.n, 0, 0, 0);
 }
 
 constexpr int MAX_STAGES = 12;
 constexpr int ITEMS = 8;             // that the copy warp may be ahead of the others
 struct Control {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES], item_full[ITEMS], item_empty[ITEMS];
-    uint64_t q_full[2], q_empty[2];                                          // per half
     // Per half and buffer (a unit's first and second 64 keys).  A barrier of a buffer cannot be two phases ahead of who waits for it.
-    uint64_t s_full[2][2], p_full[2][2], o_full[2][2];
+    uint64_t s_full[2][2], o_full[2][2], p_full[2][2];
+    uint64_t q_full[2], q_empty[2];                                          // per half
     Item items[ITEMS];
     int bad[2 * ITEMS];                    // bad[i % 16] == i + 1: item i of this CTA has a page that is not one
     uint32_t tmem_slot;
     int abort_flag;
     Setup setup;
 };
+constexpr int BARRIERS = 2 * MAX_STAGES + 2 * ITEMS + 16;
 struct Ring {                        // position in the ring: stage, and the parity of its current use
     int s = 0;
     uint32_t parity = 0;
@@ -365,46 +347,49 @@ struct Ring {                        // position in the ring: stage, and the par
 };
 
 // Rows whose accumulators are not finite: a NaN or an infinity in a value that a row does not see has come in through a probability of zero (or the
-// row sees it: then the result is the same).  The warp takes them again, one by one, without the keys that they do not see.
-__device__ __noinline__ void repair_rows(const Params& p, const Item& w, int qv, bool bad, float* part_o, float2* part_ml, int hdp, int rows) {
+// row sees it: then the result is the same).  The warp takes them again, one by one, without the keys that they do not see.  `i`, `h`: this
+// lane's row of the sequence and head; `slot`: its place in the parts.
+__device__ __noinline__ void repair_rows(const TileParams& tp, const Item& w, int i, int h, bool bad, unsigned long long slot, int hdp) {
+    const Params& p = tp.a;
     unsigned todo = __ballot_sync(0xffffffffu, bad);
     const int lane = threadIdx.x & 31;
     while (todo) {
-        const int v = __shfl_sync(0xffffffffu, qv, __ffs(todo) - 1);
+        const int from = __ffs(todo) - 1;
         todo &= todo - 1;
-        const int i = v / p.group, h = w.kvh * p.group + (v - i * p.group);
-        const long long row = w.s.row0 + i;
-        const paged::View view = paged::row_view(p.mask_block, p.row_mask, w.s, i);
-        const RowSum a = row_sum(p, w.seq, w.s.kv, w.kvh, p.q + row * p.q_ld + (long long)h * p.head_dim, view, w.j0 * KEYS, w.j1 * KEYS);
-        const int r = v - w.qt * rows;
+        const int ri = __shfl_sync(0xffffffffu, i, from), rh = __shfl_sync(0xffffffffu, h, from);
+        const unsigned long long rs = __shfl_sync(0xffffffffu, slot, from);
+        const long long row = w.s.row0 + ri;
+        const paged::View view = paged::row_view(p.mask_block, p.row_mask, w.s, ri);
+        const RowSum a = row_sum(p, w.seq, w.s.kv, w.kvh, p.q + row * p.q_ld + (long long)rh * p.head_dim, view, w.j0 * KEYS, w.j1 * KEYS);
         const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int d = lane + 32 * e;
             if (w.whole()) {
-                if (d < p.head_dim) p.out[row * p.out_ld + (long long)h * p.head_dim + d] = __float2bfloat16_rn(a.o[e] * inv);
+                if (d < p.head_dim) p.out[row * p.out_ld + (long long)rh * p.head_dim + d] = __float2bfloat16_rn(a.o[e] * inv);
             } else if (d < hdp) {
-                part_o[r * hdp + d] = d < p.head_dim ? a.o[e] : 0.f;
+                tp.part_o[rs * hdp + d] = d < p.head_dim ? a.o[e] : 0.f;
             }
         }
         if (lane == 0) {
-            if (!w.whole()) part_ml[r] = make_float2(a.m, a.l);
-            else if (p.lse) p.lse[row * p.heads + h] = a.l == 0.f ? -INFINITY : (a.m + log2f(a.l)) * 0.6931471805599453f;
+            if (!w.whole()) tp.part_ml[rs] = make_float2(a.m, a.l);
+            else if (p.lse) p.lse[row * p.heads + rh] = a.l == 0.f ? -INFINITY : (a.m + log2f(a.l)) * 0.6931471805599453f;
         }
     }
 }
 
 // After a time-out: NaN in all outputs of the CTA's range, those that were finished included.
 template <int NH>
-__device__ __noinline__ void all_nan(const TileParams& tp, const Setup& sh, Items t, int hdp) {
+__device__ __noinline__ void all_nan(const TileParams& tp, const Setup& sh, int hdp) {
     const Params& p = tp.a;
     const float nan = __int_as_float(0x7fffffff);
+    Items t = sh.first;
     Item w;
-    while (next_item<NH>(p, t, w)) {
+    while (next_item<NH>(tp, t, w)) {
         if (threadIdx.x == 0) note_split(tp, sh, w);
-        const int n = min(128 * NH, w.s.n * p.group - w.qt * 128 * NH);
-        for (int r = threadIdx.x; r < n; r += threads(NH)) {
-            const int qv = w.qt * 128 * NH + r, i = qv / p.group, h = w.kvh * p.group + (qv - i * p.group);
+        for (int r = threadIdx.x; r < 128 * NH; r += threads(NH)) {
+            const int ti = (r & 127) / tp.gs, i = (w.qt * NH + (r >> 7)) * tp.rows_half + ti, h = w.head0 + (r & 127) - ti * tp.gs;
+            if (ti >= tp.rows_half || i >= w.s.n) continue;
             const long long row = w.s.row0 + i;
             if (w.whole()) {
                 for (int d = 0; d < p.head_dim; ++d) p.out[row * p.out_ld + (long long)h * p.head_dim + d] = __float2bfloat16_rn(nan);
@@ -437,7 +422,7 @@ struct Listed {
     }
 };
 template <int NH>
-__device__ __forceinline__ bool active(const Params& p, const Item& w, int half) { return half == 0 || w.s.n * p.group > (w.qt * NH + half) * QTILE; }
+__device__ __forceinline__ bool active(const TileParams& tp, const Item& w, int half) { return half == 0 || w.s.n > (w.qt * NH + half) * tp.rows_half; }
 
 // 32 bytes of a lane's own row: with one store, a whole sector, where rows are aligned to that.
 __device__ __forceinline__ void store32(void* dst, const uint32_t* v, bool aligned, bool second) {
@@ -519,15 +504,16 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
     volatile int* abort_flag = &ctl.abort_flag;
     const int half = threadIdx.x >> 7, r = threadIdx.x & 127;
     const uint32_t tmem = ctl.tmem_slot + ((uint32_t)(r & 96) << 16), to = tmem + 256 + half * HDP;
+    const int ti = r / tp.gs, hi = r - ti * tp.gs;           // row of the half, head of the tile
     uint32_t steps = 0;                                      // of this half so far
     Listed list;
     Item w;
     for (;; list.done(ctl)) {
         if (!list.get(ctl, tp, w)) return false;
         if (w.j1 == 0) return true;
-        if (!active<NH>(p, w, half)) continue;
-        const int qv = (w.qt * NH + half) * QTILE + r, i = qv / p.group;
-        const bool valid = qv < w.s.n * p.group, any = __any_sync(0xffffffffu, valid);
+        if (!active<NH>(tp, w, half)) continue;
+        const int i = (w.qt * NH + half) * tp.rows_half + ti;
+        const bool valid = ti < tp.rows_half && i < w.s.n, any = __any_sync(0xffffffffu, valid);
         paged::View view;
         view.lim = 0x7fffffff;
         view.base = 0;
@@ -560,7 +546,7 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
                     sum = add2(sum, sum1);
                     total = sum.x + sum.y;
                     // in order: no NaN, nothing above 2^9, and a reference that is a number of ordinary size
-                    if (again || __all_sync(0xffffffffu, total <= 512.f && high <= 9.f && fabsf(m) <= FAR)) break;
+                    if (again || __all_sync(0xffffffffu, !valid || (total <= 512.f && high <= 9.f && fabsf(m) <= FAR))) break;
                     const float top = max64(v) * p.scale_log2;
                     if (!(top < INFINITY)) l = __int_as_float(0x7fffffff);        // a NaN or an infinity that the row sees
                     m = fmaxf(m, top);
@@ -603,36 +589,42 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
         if (any) {
             tc_fence_after();
             const long long row = w.s.row0 + i;
-            const int h = w.kvh * p.group + (qv - i * p.group);
+            const int h = w.head0 + hi;
             const bool nan = !w.s.ok || *(volatile int*)&ctl.bad[list.index % (2 * ITEMS)] == list.index + 1, whole = w.whole();
             const float undefined = __int_as_float(0x7fffffff);
             if (nan) l = undefined;
-            const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+            const float inv = nan ? undefined : whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
             const size_t slot = ((size_t)(2 * blockIdx.x + (w.j0 == 0)) * NH + half) * QTILE + r;
-            bf16* out = p.out + row * p.out_ld + (long long)h * p.head_dim;
-            float* part_o = tp.part_o + slot * HDP;
-            float check = fabsf(l);                                                // infinite or NaN where something is
+            char* dst = whole ? (char*)(p.out + row * p.out_ld + (long long)h * p.head_dim) : (char*)(tp.part_o + slot * HDP);
+            float check = fabsf(l), check1 = 0.f;                                  // infinite or NaN where something is
 #pragma unroll 1
-            for (int c = 0; c < HDP; c += 16) {
-                float o[16];
+            for (int c = 0; c < HDP; c += 32) {
+                uint32_t u[32];
                 __syncwarp();
-                tmem_ld16(to + c, o);
-                uint32_t u[16];
+                tmem_ld32_issue(to + c, u);
+                tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) check = max3_nan(check, fabsf(o[e]), fabsf(o[e + 1]));
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    o[e] = nan ? undefined : o[e] * inv;
-                    u[e] = __float_as_uint(o[e]);
+                for (int e = 0; e < 32; e += 4) {
+                    check = max3_nan(check, fabsf(__uint_as_float(u[e])), fabsf(__uint_as_float(u[e + 1])));
+                    check1 = max3_nan(check1, fabsf(__uint_as_float(u[e + 2])), fabsf(__uint_as_float(u[e + 3])));
                 }
-                if (!valid) continue;
                 if (whole) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) u[e] = pack2(o[2 * e], o[2 * e + 1]);
-                    if (c < p.head_dim) store32(out + c, u, tp.out_32, c + 8 < p.head_dim);
-                } else {
-                    store32(part_o + c, u, true, true);
-                    store32(part_o + c + 8, u + 8, true, true);
+                    for (int e = 0; e < 16; ++e) u[e] = pack2(__uint_as_float(u[2 * e]) * inv, __uint_as_float(u[2 * e + 1]) * inv);
+                } else if (nan) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) u[e] = 0x7fffffffu;
+                }
+                if (valid) {
+                    if (whole) {
+                        if (c < p.head_dim) store32(dst, u, tp.out_32, c + 8 < p.head_dim);
+                        if (c + 16 < p.head_dim) store32(dst + 32, u + 8, tp.out_32, c + 24 < p.head_dim);
+                        dst += 64;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) store32(dst + 32 * e, u + 8 * e, true, true);
+                        dst += 128;
+                    }
                 }
             }
             __syncwarp();
@@ -641,50 +633,37 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
                 if (!whole) tp.part_ml[slot] = make_float2(m, l);
                 else if (p.lse) p.lse[row * p.heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
             }
-            const bool bad = valid && !nan && !(check < INFINITY);
+            const bool bad = valid && !nan && !(max3_nan(check, check1, check1) < INFINITY);
             if (__any_sync(0xffffffffu, bad)) {
                 __syncwarp();
-                repair_rows(p, w, qv, bad, tp.part_o + (slot - r - half * QTILE) * HDP, tp.part_ml + (slot - r - half * QTILE), HDP, 128 * NH);
+                repair_rows(tp, w, i, h, bad, slot, HDP);
             }
         }
     }
 }
 
-// Q warp: the rows of each item by copies of 16 bytes into the swizzled tiles; rows and elements that do not exist are zero.
+// Q warp: the query vectors of each item's halves, a box of rows x heads x 64 elements at a time.  Rows behind the sequence's are some other
+// rows or zeros, and the tile's last vectors (128 is no multiple of the group) whatever was there: nobody looks at their results.
 template <int HDP, int NH>
-__device__ __forceinline__ bool query_role(const TileParams& tp, Control& ctl, uint8_t* q_tiles) {
-    const Params& p = tp.a;
-    constexpr int CH = HDP / 8, RPI = 32 / CH;               // chunks of a row, rows at a time
-    const int lane = threadIdx.x & 31, c = lane % CH;
+__device__ __forceinline__ bool query_role(const TileParams& tp, Control& ctl, uint8_t* q_tiles, const CUtensorMap* map_q) {
     uint32_t items[2] = {0, 0};                              // of a half so far
     Listed list;
     Item w;
     for (;; list.done(ctl)) {
         if (!list.get(ctl, tp, w)) return false;
         if (w.j1 == 0) return true;
-#pragma unroll 1
+#pragma unroll
         for (int half = 0; half < NH; ++half) {
-            if (!active<NH>(p, w, half)) continue;
+            if (!active<NH>(tp, w, half)) continue;
             if (!__all_sync(0xffffffffu, wait(&ctl.q_empty[half], (items[half] & 1) ^ 1, tp.wait_limit, &ctl.abort_flag))) return false;
             ++items[half];
-            const uint32_t q_addr = smem_u32(q_tiles) + half * (QTILE * HDP * 2);
-#pragma unroll 1
-            for (int r0 = 0; r0 < QTILE; r0 += 32) {
-                const int qv = (w.qt * NH + half) * QTILE + r0 + lane, i = qv / p.group, h = w.kvh * p.group + (qv - i * p.group);
-                const unsigned long long mine =
-                    qv < w.s.n * p.group ? (unsigned long long)(p.q + (long long)(w.s.row0 + i) * p.q_ld + (long long)h * p.head_dim) : 0;
-#pragma unroll 4
-                for (int k = 0; k < 32 / RPI; ++k) {
-                    const int rr = k * RPI + lane / CH, r = r0 + rr;
-                    const unsigned long long src = __shfl_sync(0xffffffffu, mine, rr);
-                    const bool here = src && c * 8 < p.head_dim;
-                    copy16(q_addr + (c >> 3) * (QTILE * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), here ? (const bf16*)src + c * 8 : p.q, here);
-                }
+            if (elect()) {
+                mbar_expect_tx(&ctl.q_full[half], (uint32_t)(tp.gs * tp.rows_half) * HDP * 2);
+#pragma unroll
+                for (int c = 0; c < HDP / 64; ++c)
+                    tma_load_3d(q_tiles + (half * (HDP / 64) + c) * (QTILE * 128), map_q, c * 64, w.head0, w.s.row0 + (w.qt * NH + half) * tp.rows_half, &ctl.q_full[half]);
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_async_shared();
             __syncwarp();
-            if (lane == 0) arrive(&ctl.q_full[half]);
         }
     }
 }
@@ -728,7 +707,7 @@ __device__ __forceinline__ bool mma_role(const TileParams& tp, Control& ctl, uin
         __syncwarp();
         if (part) step(rk);
     };
-    auto is_active = [&](const Item& x) { return active<NH>(p, x, half); };
+    auto is_active = [&](const Item& x) { return active<NH>(tp, x, half); };
 
     Listed list;
     Item w, next;
@@ -801,36 +780,38 @@ __device__ __forceinline__ bool mma_role(const TileParams& tp, Control& ctl, uin
 // Copy warp: lists the items for the others, and loads their K and V tiles of 128 keys, page by page (a lane per page), in the order in which the
 // MMA warp takes them.
 template <int HDP, int NH>
-__device__ __forceinline__ bool copy_role(const TileParams& tp, Control& ctl, uint8_t* ring, Items t, const CUtensorMap* map_k, const CUtensorMap* map_v) {
+__device__ __forceinline__ bool copy_role(const TileParams& tp, Control& ctl, uint8_t* ring, const CUtensorMap* map_k, const CUtensorMap* map_v) {
     const Params& p = tp.a;
     constexpr int SB = KEYS * HDP * 2;
     const int lane = threadIdx.x & 31, box = min(KEYS, p.c.page_mask + 1), pages = KEYS / box;
     const uint32_t ra = smem_u32(ring);
     Ring r;
     r.parity = 1;                                            // a fresh barrier passes a wait for the phase before its first
-    // The next item, or the end, is listed before this one's tiles are loaded: the MMA warp wants to know what comes behind an item that
-    // it gives room for.
+    Items t;
+    plan<NH>(tp, ctl.setup, t);
+    // The next item, or the end, is listed before this one's last tiles are loaded: the MMA warps want to know what comes behind an item that
+    // they give room for.
     Item w, next;
     auto publish = [&](int index, Item& x) {
-        if (!next_item<NH>(p, t, x)) x.j1 = 0;
+        if (!next_item<NH>(tp, t, x)) x.j1 = 0;
         if (!__all_sync(0xffffffffu, wait(&ctl.item_empty[index % ITEMS], (index / ITEMS & 1) ^ 1, tp.wait_limit, &ctl.abort_flag))) return false;
         if (lane == 0) {
             ctl.items[index % ITEMS] = x;
-            if (x.j1) note_split(tp, ctl.setup, x);
             arrive(&ctl.item_full[index % ITEMS]);
+            if (x.j1) note_split(tp, ctl.setup, x);
         }
         __syncwarp();
         return true;
     };
     if (!publish(0, w)) return false;
     for (int index = 0; w.j1; ++index, w = next) {
-        if (!publish(index + 1, next)) return false;
         for (int j = w.j0; j < w.j1; ++j) {
+            if (j == w.j0 + 1 && !publish(index + 1, next)) return false;          // (the first tile is on its way)
             const int key = j * KEYS + lane * box;
             bool some = lane < pages && key < w.s.kv;
             const int page = some ? paged::page_of(p.b, w.seq, key) : -1;
             if (some && page < 0) {
-                *(volatile int*)&ctl.bad[index & 15] = index + 1;
+                *(volatile int*)&ctl.bad[index % (2 * ITEMS)] = index + 1;
                 some = false;
             }
             const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, some)) * box * HDP * 2;
@@ -851,34 +832,34 @@ __device__ __forceinline__ bool copy_role(const TileParams& tp, Control& ctl, ui
                 r.next(tp.stages);
             }
         }
+        if (w.j1 - w.j0 == 1 && !publish(index + 1, next)) return false;
     }
     return true;
 }
 
 template <int HDP, int NH>
 __global__ void __launch_bounds__(threads(NH), 1)
-tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TileParams tp) {
+tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+            const __grid_constant__ TileParams tp) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* base = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* ring = base + NH * QTILE * HDP * 2;
     Control& ctl = *(Control*)(base + tp.control_at);
-    const int warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < tp.stages; ++s) mbar_init(&ctl.full[s], 1), mbar_init(&ctl.empty[s], NH);
-        for (int i = 0; i < ITEMS; ++i) mbar_init(&ctl.item_full[i], 1), mbar_init(&ctl.item_empty[i], 4 * NH + NH + 1);      // softmax, MMA, Q
-        for (int h = 0; h < 2; ++h) {
-            mbar_init(&ctl.q_full[h], 1), mbar_init(&ctl.q_empty[h], 1);
-            for (int i = 0; i < 2; ++i) mbar_init(&ctl.s_full[h][i], 1), mbar_init(&ctl.p_full[h][i], 128), mbar_init(&ctl.o_full[h][i], 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == 0) {
+        for (int i = lane; i < BARRIERS; i += 32) {
+            const int k = i - 2 * MAX_STAGES;                // behind full (1) and empty (MMA warps); then the members of Control in their order
+            const int count = k < 0 ? (i < MAX_STAGES ? 1 : NH) : k < ITEMS ? 1 : k < 2 * ITEMS ? 5 * NH + 1 : k < 2 * ITEMS + 8 ? 1 : k < 2 * ITEMS + 12 ? 128 : 1;
+            mbar_init(&ctl.full[0] + i, count);
         }
-        ctl.abort_flag = 0;
-        for (int i = 0; i < 2 * ITEMS; ++i) ctl.bad[i] = 0;
+        if (lane < 2 * ITEMS) ctl.bad[lane] = 0;
+        if (lane == 0) ctl.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
-    }
-    if (warp == 4 * NH) {
+    } else if (warp == 4 * NH + 2) {
         tmem_alloc(&ctl.tmem_slot, 512);
         tmem_relinquish();
+    } else if (warp == 4 * NH && lane < 3) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v) : "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -886,34 +867,29 @@ tile_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ C
     pdl_launch();
     // all warps: nothing in front reads or writes what this kernel does, and the bounded waits begin behind it
     pdl_wait();
-    Items items;
-    plan<NH>(tp, ctl.setup, items);
     bool ok = true;
     if (warp < 4 * NH) ok = softmax_role<HDP, NH>(tp, ctl);
-    else if (warp == 4 * NH) ok = copy_role<HDP, NH>(tp, ctl, ring, items, &map_k, &map_v);
-    else if (warp == 4 * NH + 1) ok = query_role<HDP, NH>(tp, ctl, base);
+    else if (warp == 4 * NH) ok = copy_role<HDP, NH>(tp, ctl, ring, &map_k, &map_v);
+    else if (warp == 4 * NH + 1) ok = query_role<HDP, NH>(tp, ctl, base, &map_q);
     else if (warp - 4 * NH - 2 < NH) ok = mma_role<HDP, NH>(tp, ctl, base, ring, warp - 4 * NH - 2);
     if (!ok) *(volatile int*)&ctl.abort_flag = 1;
     __syncwarp();
     __syncthreads();
     const bool failed = *(volatile int*)&ctl.abort_flag;
-    if (failed) {
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        settle();
-    }
+    if (failed) settle();
     tc_fence_before();
     __syncthreads();
-    if (warp == 4 * NH) tmem_dealloc(ctl.tmem_slot, 512);
+    if (warp == 4 * NH + 2) tmem_dealloc(ctl.tmem_slot, 512);
     if (failed) {
         if (threadIdx.x == 0) atomicAdd(tp.timeouts, 1);
-        all_nan<NH>(tp, ctl.setup, items, HDP);
+        all_nan<NH>(tp, ctl.setup, HDP);
     }
 }
 
 // Sum of the parts of an item that the cuts went through, in the order of the keys: block (c, y) takes 32 vectors of the item that CTA c
-// began, a warp a vector at a time, a lane four elements (HDP 64: two).
-template <int HDP>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ TileParams tp) {
+// began, a warp a vector.  The lanes take the parts' references and sums, 32 at a time, then four elements each (HDP 64: two) of all parts.
+template <int HDP, int NH>
+__global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ TileParams tp) {
     constexpr int E = HDP / 32;
     pdl_wait();
     pdl_launch();
@@ -921,42 +897,43 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ TileP
     const int c = blockIdx.x;
     const int4 d = tp.split[2 * c];
     if (d.x < 0) return;
-    const int4 s = tp.split[2 * c + 1];
-    const int q0 = d.z * tp.rows, n = min(tp.rows, s.y * p.group - q0), lane = threadIdx.x & 31;
-    for (int r = blockIdx.y * 32 + (threadIdx.x >> 5); r < min(n, (int)blockIdx.y * 32 + 32); r += 8) {
-        float m = -INFINITY, l = 0.f, o[E];
+    const int r = blockIdx.y * 32 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int ti = (r & 127) / tp.gs, i = (d.y * NH + (r >> 7)) * tp.rows_half + ti, h = d.x + (r & 127) - ti * tp.gs;
+    if (ti >= tp.rows_half || i >= tp.split[2 * c + 1].x) return;
+    float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 4
-        for (int part = c; part <= d.w; ++part) {
-            const size_t slot = 2 * part + (part == c);
-            const float2 ml = tp.part_ml[slot * tp.rows + r];
-            const float* src = tp.part_o + (slot * tp.rows + r) * HDP + lane * E;
-            float x[E];
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int first = c; first <= d.z; first += 32) {
+        const int part = first + lane, n = min(32, d.z + 1 - first);
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (lane < n) ml = tp.part_ml[(size_t)(2 * part + (part == c)) * (128 * NH) + r];
+        const float top = fmaxf(m, warp_max(ml.x)), ref = top == -INFINITY ? 0.f : top;
+        const float f = exp2_fast(m - ref), g = exp2_fast(ml.x - ref);
+        l = l * f + warp_sum(ml.y * g);
+        m = top;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll 8
+        for (int k = 0; k < n; ++k) {
+            const float* src = tp.part_o + ((size_t)(2 * (first + k) + (first + k == c)) * (128 * NH) + r) * HDP + lane * E;
+            const float weight = __shfl_sync(0xffffffffu, g, k);
             if constexpr (E == 4) {
                 const float4 v = *reinterpret_cast<const float4*>(src);
-                x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+                o[0] = fmaf(v.x, weight, o[0]), o[1] = fmaf(v.y, weight, o[1]), o[2] = fmaf(v.z, weight, o[2]), o[3] = fmaf(v.w, weight, o[3]);
             } else {
                 const float2 v = *reinterpret_cast<const float2*>(src);
-                x[0] = v.x, x[1] = v.y;
+                o[0] = fmaf(v.x, weight, o[0]), o[1] = fmaf(v.y, weight, o[1]);
             }
-            const float top = fmaxf(m, ml.x), ref = top == -INFINITY ? 0.f : top;
-            const float f = exp2_fast(m - ref), g = exp2_fast(ml.x - ref);
-            l = l * f + ml.y * g;
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = o[e] * f + x[e] * g;
-            m = top;
         }
-        const int qv = q0 + r, i = qv / p.group, h = d.y * p.group + (qv - i * p.group);
-        const long long row = s.x + i;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        bf16* out = p.out + row * p.out_ld + (long long)h * p.head_dim + lane * E;
-        if (lane * E < p.head_dim) {
-            if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv));
-            else *reinterpret_cast<uint32_t*>(out) = pack2(o[0] * inv, o[1] * inv);
-        }
-        if (p.lse && lane == 0) p.lse[row * p.heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
     }
+    const long long row = d.w + i;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bf16* out = p.out + row * p.out_ld + (long long)h * p.head_dim + lane * E;
+    if (lane * E < p.head_dim) {
+        if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv));
+        else *reinterpret_cast<uint32_t*>(out) = pack2(o[0] * inv, o[1] * inv);
+    }
+    if (p.lse && lane == 0) p.lse[row * p.heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 }  // namespace patt
