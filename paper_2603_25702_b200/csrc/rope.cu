@@ -11,7 +11,7 @@ namespace s2d2 {
 namespace {
 
 constexpr int RT = 256;              // threads of a CTA
-constexpr int MAX_ROWS = 16;         // rows of a CTA, at most
+constexpr int MAX_ROWS = 20;         // rows of a CTA, at most
 
 // One of the matrices of a call: [rows, heads, head_dim], rows `ld` elements apart.
 struct Mat {
@@ -25,7 +25,7 @@ struct RopeParams {
     Mat q, k, v;                     // v: append only
     const int* pos;                  // null: the cache index
     const double* freqs;
-    float scale, eps;
+    float scale, eps, inv_dim;       // inv_dim: 1 / head_dim
     int rot, interleaved, head_dim;
     long long n_rows;
     int rows_per_cta;
@@ -39,26 +39,58 @@ struct Place {
     int seq, pos, page, token;
 };
 
-// Eight elements in registers, fp32.
-__device__ __forceinline__ void load8(const float* p, float* v) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+// Two operations in one instruction
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
 }
-__device__ __forceinline__ void load8(const bf16* p, float* v) {
-    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+// Eight elements as they stand in memory, and in fp32.
+template <typename T>
+struct Raw8 {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    }
+    __device__ __forceinline__ void values(float2* v) const {
+        if (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint4 a = w[i % (sizeof(T) / 2)];
+                v[2 * i] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+                v[2 * i + 1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+            }
+        } else {
+            const uint32_t x[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
+        }
+    }
+};
+// 1 / sqrt(x), the approximation improved once: within 2 units in the last place
+__device__ __forceinline__ float inverse_root(float x) {
+    const float y = rsqrtf(x);
+    return x > 0.f && x < INFINITY ? y * fmaf(-0.5f * x * y, y, 1.5f) : y;
 }
-__device__ __forceinline__ void store8(float* p, const float* v) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    *(reinterpret_cast<float4*>(p) + 1) = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ void store8(float* p, const float2* v) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+    *(reinterpret_cast<float4*>(p) + 1) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
 }
-__device__ __forceinline__ void store8(bf16* p, const float* v) {
+__device__ __forceinline__ void store8(bf16* p, const float2* v) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[i].x, v[i].y);
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -104,9 +136,9 @@ __device__ __forceinline__ TO* target(const RopeParams& p, const Place& w, int k
     return (TO*)(kind ? p.k.out : p.q.out) + row * (kind ? p.k.out_ld : p.q.out_ld) + (long long)head * p.head_dim;
 }
 // Eight numbers from shared memory.
-__device__ __forceinline__ void read8(const float* p, float* v) {
+__device__ __forceinline__ void read8(const float* p, float2* v) {
     const float4 a = *reinterpret_cast<const float4*>(p), b = *(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    v[0] = make_float2(a.x, a.y), v[1] = make_float2(a.z, a.w), v[2] = make_float2(b.x, b.y), v[3] = make_float2(b.z, b.w);
 }
 // (x, y) turned by the angle of cosine c and sine s
 __device__ __forceinline__ void rotate(float& x, float& y, float c, float s) {
@@ -115,8 +147,10 @@ __device__ __forceinline__ void rotate(float& x, float& y, float c, float s) {
     x = t;
 }
 
-// One pass: a head is read once, its squares are summed by the threads that hold it, and it is rotated in registers.  Bound by
-// memory.  Cosines and sines of a row are computed once per CTA, in shared memory, for all of its heads.
+// One pass: a head is read once, its squares are summed by the threads that hold it, and it is rotated in registers.  Cosines and sines of
+// a row are computed once per CTA, in shared memory, for all of its heads.  Should be bound by memory; what it has to watch is the start of
+// a CTA (positions, angles, two barriers: with two rows a CTA 42 us for 8192 x 40 heads, with 14 33 us, 5.1 TB/s) and the number of
+// instructions (packed arithmetic 46.7 -> 42 us, loads a round ahead 56 -> 47).
 // VEC: a thread holds two groups of eight elements of a head: the two halves of eight pairs (half layout), or two neighbours'.
 // Otherwise a warp takes a head, element pair by element pair, and reads it twice where there is a norm.
 template <typename TI, typename TO, bool APPEND, bool VEC>
@@ -128,6 +162,41 @@ __global__ void __launch_bounds__(RT) rope_kernel(const RopeParams p) {
     const long long row0 = (long long)blockIdx.x * p.rows_per_cta;
     const int rows = (int)min((long long)p.rows_per_cta, p.n_rows - row0), pairs = p.rot >> 1, hd = p.head_dim;
     float* gains = table + p.rows_per_cta * p.rot;
+    const int heads = p.q.heads + p.k.heads + (APPEND ? p.v.heads : 0);
+    const int lanes = VEC ? p.tph : 32, sub = threadIdx.x & (lanes - 1), step = RT / lanes;
+    const int total = rows * heads;
+    // VEC: groups of eight elements of this thread: the two halves of eight pairs (half layout) or any two; behind the rotated part neighbours
+    const int n = hd >> 4, n_rot = p.rot >> 4;               // threads with elements, with pairs
+    const int c0 = sub < n_rot ? sub : 2 * sub, c1 = sub < n_rot ? sub + n_rot : 2 * sub + 1;
+    struct Task {
+        int r, head, kind;                                   // row, head of q, k or v (r >= rows: none)
+        const TI* in;
+    };
+    // the heads of all rows one after the other; this thread's tasks are `step` apart
+    const int step_r = step / heads, step_h = step - step_r * heads;
+    const long long q_ld = p.q.in_ld, k_ld = p.k.in_ld, v_ld = p.v.in_ld;
+    const TI* q_in = (const TI*)p.q.in + row0 * q_ld;
+    const TI* k_in = (const TI*)p.k.in + row0 * k_ld;
+    const TI* v_in = APPEND ? (const TI*)p.v.in + row0 * v_ld : nullptr;
+    int at_r = (int)(threadIdx.x / lanes) / heads, at_h = (int)(threadIdx.x / lanes) - at_r * heads;
+    auto next_task = [&]() {
+        Task t;
+        t.r = at_r, t.head = at_h, t.kind = 0;
+        t.in = q_in + at_r * q_ld;
+        if (t.head >= p.q.heads) {
+            t.head -= p.q.heads, t.kind = 1;
+            t.in = k_in + at_r * k_ld;
+            if (APPEND && t.head >= p.k.heads) t.head -= p.k.heads, t.kind = 2, t.in = v_in + at_r * v_ld;
+        }
+        t.in += t.head * hd;
+        at_r += step_r, at_h += step_h;
+        if (at_h >= heads) at_h -= heads, ++at_r;
+        return t;
+    };
+    // a head's elements are asked for while the angles are computed, or the head before is
+    Task t = next_task();
+    Raw8<TI> ra, rb;
+    if (VEC && t.r < rows && sub < n) ra.load(t.in + c0 * 8), rb.load(t.in + c1 * 8);
     if (VEC) {
         for (int i = threadIdx.x; i < hd; i += RT) {
             if (p.q.gain) gains[i] = p.q.gain[i];
@@ -143,47 +212,39 @@ __global__ void __launch_bounds__(RT) rope_kernel(const RopeParams p) {
         table[r * p.rot + pairs + f] = cs.y;
     }
     __syncthreads();
-    const int heads = p.q.heads + p.k.heads + (APPEND ? p.v.heads : 0);
-    const int lanes = VEC ? p.tph : 32, sub = threadIdx.x & (lanes - 1), step = RT / lanes;
     // (whole warps stay together: the sums below are shuffles)
-    const int total = rows * heads, rounds = (total + step - 1) / step;
-    for (int it = 0; it < rounds; ++it) {
-        const int task = it * step + threadIdx.x / lanes;
-        const bool some = task < total;
-        const int r = some ? task / heads : 0;
-        int head = some ? task - r * heads : 0, kind = 0;            // of q, k, v
-        if (head >= p.q.heads) {
-            head -= p.q.heads, kind = 1;
-            if (APPEND && head >= p.k.heads) head -= p.k.heads, kind = 2;
-        }
+    for (int rounds = (total + step - 1) / step; rounds; --rounds) {
+        const Task next = next_task();
+        const int r = min(t.r, rows - 1), kind = t.kind;
         const Place w = places[r];
-        TO* out = some && w.seq >= 0 ? target<TO, APPEND>(p, w, kind, row0 + r, head) : nullptr;
-        const TI* in = (const TI*)(kind == 0 ? p.q.in : kind == 1 ? p.k.in : p.v.in) +
-                       (row0 + r) * (kind == 0 ? p.q.in_ld : kind == 1 ? p.k.in_ld : p.v.in_ld) + (long long)head * hd;
+        TO* out = t.r < rows && w.seq >= 0 ? target<TO, APPEND>(p, w, kind, row0 + r, t.head) : nullptr;
+        const TI* in = t.in;
         const float* gain = kind == 0 ? p.q.gain : kind == 1 ? p.k.gain : nullptr;
         const float* cosines = table + r * p.rot;
         const float* sines = cosines + pairs;
         const bool turned = !APPEND || kind < 2;
         if (VEC) {
-            const int n = hd >> 4, n_rot = p.rot >> 4;               // threads with elements, with pairs
             const bool mine = out && sub < n;
-            // the two halves of eight pairs (half layout) or any two groups; behind the rotated part neighbours
-            const int c0 = sub < n_rot ? sub : 2 * sub, c1 = sub < n_rot ? sub + n_rot : 2 * sub + 1;
-            float a[8], b[8], c[8], s[8];
-            if (mine) load8(in + c0 * 8, a), load8(in + c1 * 8, b);
-            if (gain || p.q.gain || p.k.gain) {                      // (the same for all threads)
-                float ss = 0.f;
+            float2 a[4], b[4], c[4], s[4];
+            ra.values(a);
+            rb.values(b);
+            if (next.r < rows && sub < n) ra.load(next.in + c0 * 8), rb.load(next.in + c1 * 8);
+            t = next;
+            if (p.q.gain || p.k.gain) {                              // (the same for all threads)
+                float2 ss = make_float2(0.f, 0.f);
                 if (mine) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
+                    for (int e = 0; e < 4; ++e) ss = fma2(a[e], a[e], fma2(b[e], b[e], ss));
                 }
-                for (int o = lanes >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                float square = ss.x + ss.y;
+                for (int o = lanes >> 1; o; o >>= 1) square += __shfl_xor_sync(0xffffffffu, square, o);
                 if (gain && mine) {
-                    const float inv = 1.f / sqrtf(ss / (float)hd + p.eps);
+                    const float inv = inverse_root(fmaf(square, p.inv_dim, p.eps));
+                    const float2 ii = make_float2(inv, inv);
                     read8(gains + (kind ? hd : 0) + c0 * 8, c);
                     read8(gains + (kind ? hd : 0) + c1 * 8, s);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) a[e] *= inv * c[e], b[e] *= inv * s[e];
+                    for (int e = 0; e < 4; ++e) a[e] = mul2(mul2(a[e], ii), c[e]), b[e] = mul2(mul2(b[e], ii), s[e]);
                 }
             }
             if (!mine) continue;
@@ -193,23 +254,28 @@ __global__ void __launch_bounds__(RT) rope_kernel(const RopeParams p) {
                     read8(cosines + sub * 8, c);
                     read8(sines + sub * 8, s);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) rotate(a[e], b[e], c[e], s[e]);
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 x = a[e], y = b[e];
+                        a[e] = fma2(make_float2(-y.x, -y.y), s[e], mul2(x, c[e]));
+                        b[e] = fma2(x, s[e], mul2(y, c[e]));
+                    }
                 } else {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const float4 cc = *reinterpret_cast<const float4*>(cosines + (h ? c1 : c0) * 4);
                         const float4 sn = *reinterpret_cast<const float4*>(sines + (h ? c1 : c0) * 4);
-                        float* v = h ? b : a;
-                        rotate(v[0], v[1], cc.x, sn.x);
-                        rotate(v[2], v[3], cc.y, sn.y);
-                        rotate(v[4], v[5], cc.z, sn.z);
-                        rotate(v[6], v[7], cc.w, sn.w);
+                        float2* v = h ? b : a;
+                        rotate(v[0].x, v[0].y, cc.x, sn.x);
+                        rotate(v[1].x, v[1].y, cc.y, sn.y);
+                        rotate(v[2].x, v[2].y, cc.z, sn.z);
+                        rotate(v[3].x, v[3].y, cc.w, sn.w);
                     }
                 }
             }
             store8(out + c0 * 8, a);
             store8(out + c1 * 8, b);
         } else {
+            t = next;
             if (!out) continue;                                      // the same for all lanes
             float inv = 1.f;
             if (gain) {
@@ -218,7 +284,7 @@ __global__ void __launch_bounds__(RT) rope_kernel(const RopeParams p) {
                     const float x = to_f32(in[e]);
                     ss = fmaf(x, x, ss);
                 }
-                inv = 1.f / sqrtf(warp_sum(ss) / (float)hd + p.eps);
+                inv = inverse_root(fmaf(warp_sum(ss), p.inv_dim, p.eps));
             }
             const int n_rot = turned ? pairs : 0;
             for (int i = sub; i < n_rot; i += 32) {
@@ -277,14 +343,22 @@ int launch_rope(const char* op, const ops::Device* dev, RopeParams& p, int dtype
             vec = vec && aligned(m->in, m->in_ld, size);
             if (m->out) vec = vec && aligned(m->out, m->out_ld, APPEND ? 2 : size);
         }
+    p.inv_dim = 1.f / (float)p.head_dim;
     p.tph = 1;
     while (p.tph * 16 < p.head_dim) p.tph *= 2;                      // at most 32 (head_dim 512)
     const int at_once = vec ? RT / p.tph : RT / 32;
-    // enough rows for about two heads per thread and few rows whose table is made for too few heads, but a wave of CTAs first
-    p.rows_per_cta = (int)std::max(1LL, std::min<long long>({(2LL * at_once + heads - 1) / heads, MAX_ROWS, p.n_rows / (dev->n_sms * 4LL)}));
+    // Rows of a CTA: as few rounds over the heads as possible in all waves of CTAs (four on an SM), a wave's start counted as three rounds
+    // (8192 rows of 40 heads of 128 with norm, bf16: 14 rows, one wave 33 us; 8 rows 34, 9 38, 2 42).
+    p.rows_per_cta = 1;
+    long long best = 1LL << 62;
+    for (int rows = 1; rows <= MAX_ROWS; ++rows) {
+        const long long blocks = (p.n_rows + rows - 1) / rows, waves = (blocks + dev->n_sms * 4 - 1) / (dev->n_sms * 4);
+        const long long cost = waves * ((rows * heads + at_once - 1) / at_once + 3);
+        if (cost < best) best = cost, p.rows_per_cta = rows;
+    }
     const long long grid = (p.n_rows + p.rows_per_cta - 1) / p.rows_per_cta;
     if (grid > 0x7fffffffLL) return ops::fail(S2D2_ERR_INVALID, "%s: too many rows", op);
-    const size_t smem = ((size_t)p.rows_per_cta * p.rot + (vec ? 2 * p.head_dim : 0)) * 4;       // at most 36 KB
+    const size_t smem = ((size_t)p.rows_per_cta * p.rot + (vec ? 2 * p.head_dim : 0)) * 4;       // at most 44 KB
     cudaError_t e;
     if (dtype == S2D2_DTYPE_F32) {
         typedef typename std::conditional<APPEND, bf16, float>::type TO;
