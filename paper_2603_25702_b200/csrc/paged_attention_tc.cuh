@@ -54,11 +54,13 @@ __device__ __forceinline__ bool peek(uint64_t* bar, uint32_t parity) {
         : "memory");
     return done;
 }
-// Bounded wait for the phase with the given parity; false when it has run out or another role of the CTA has given up.
+// Bounded wait for the phase with the given parity; false when it has run out or another role of the CTA has given up.  (Not unrolled: that was
+// most of the kernel's code, 200 KB, which had to be fetched again and again; a wait that was over took 300 cycles instead of 75.)
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, uint32_t limit, volatile int* abort_flag) {
+#pragma unroll 1
     for (uint32_t it = 0; it < WAIT_LIMIT; ++it) {
-        if ((it & 31u) == 31u && (it >= limit || *abort_flag)) return false;
         if (poll(bar, parity)) return true;
+        if ((it & 31u) == 31u && (it >= limit || *abort_flag)) return false;
     }
     return false;
 }
@@ -533,7 +535,7 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
                 tmem_ld_wait();
                 if (!__all_sync(0xffffffffu, key + STEP <= view.lim)) mask64(v, view, key);
                 const float before = m;
-                if (key == w.j0 * KEYS) m = first_reference(v[0]) * p.scale_log2;
+                if (key == w.j0 * KEYS) m = fmaxf(first_reference(v[0]) * p.scale_log2, -INFINITY);
                 float2 sum, sum1;
                 float factor = p.scale_log2, total;
 #pragma unroll 1
