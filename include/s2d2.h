@@ -503,7 +503,8 @@ int s2d2_qk_rope(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out
  * cache index d_kv_len[s] - n + i.  Index j is token j % page_tokens of page d_pages[s * max_pages + j / page_tokens]; entries behind the
  * last used one are not looked at.  Rows behind d_row0[n_seqs] pad the batch: their outputs are left as they were.
  * d_row0 must not decrease and must stay within 0..n_rows: a sequence for which it does not has no rows.  A d_kv_len outside
- * 0..max_pages * page_tokens, or a page outside 0..n_pages - 1, is not followed (see the calls). */
+ * 0..max_pages * page_tokens, or a page outside 0..n_pages - 1, is not followed (see the calls).  Of a list that gives rows to several sequences
+ * (it must decrease for that) s2d2_paged_attention follows none, s2d2_kv_append one of them. */
 typedef struct {
     const int32_t* d_row0;      /* [n_seqs + 1]                                  */
     const int32_t* d_kv_len;    /* [n_seqs]                                      */
@@ -542,7 +543,8 @@ int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_o
  * A row that sees nothing (or only scores of -inf) gets 0 and lse -inf; keys and values that a row does not see have no influence on it, NaN
  * and infinities included.  Scores, sums and maxima are fp32; probabilities are rounded to bf16 for the product with the
  * values.  A kv length that is not followed makes the sequence's rows NaN, a page that is not one the rows that see its tokens (and rows next to
- * them may become NaN, too).  n_rows is at most 2^22, max_pages * page_tokens and n_rows * n_q_heads / n_kv_heads at most 2^30.
+ * them may become NaN, too).  n_rows is at most 2^22, max_pages * page_tokens and n_rows * n_q_heads / n_kv_heads at most 2^30; more than
+ * 2e9 pairs of a tile of query vectors and a tile of 128 keys, by these bounds, is S2D2_ERR_UNSUPPORTED.
  * d_ws: at least s2d2_paged_attention_workspace bytes (they depend on the fields of the structs, not on what is on the device),
  * 32-byte aligned, used by this call alone while it runs, whatever it holds. */
 int s2d2_paged_attention_workspace(const s2d2_rows* rows, const s2d2_paged_kv* kv, int32_t n_q_heads, int64_t* bytes);

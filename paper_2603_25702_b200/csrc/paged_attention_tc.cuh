@@ -235,11 +235,13 @@ template <int NH>
 __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out) {
     const Params& p = tp.a;
     const int lane = threadIdx.x & 31, per = 32 / tp.seq_lanes, heads = p.kv_heads * tp.vsub;
+    uint32_t rows = 0;
     // items (x) and units (y) of a sequence, by seq_lanes lanes; the first of them has the sums
     auto count = [&](int s) {
         uint2 n = make_uint2(0, 0);
         if (s < p.b.n_seqs) {
             const paged::Seq q = usable_seq(p, s);
+            if ((lane & (tp.seq_lanes - 1)) == 0) rows = min(rows + q.n, 1u << 26);
             const int items = items_of<NH>(tp, q.n);
             for (int t = lane & (tp.seq_lanes - 1); t < items; t += tp.seq_lanes) n.y += units_of<NH>(tp, q, t), ++n.x;
         }
@@ -255,12 +257,14 @@ __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out
     }
     items = __reduce_add_sync(0xffffffffu, items);
     units = __reduce_add_sync(0xffffffffu, units);
+    rows = __reduce_add_sync(0xffffffffu, rows);
     out.left = 0;
     if (lane == 0) tp.split[2 * blockIdx.x] = make_int4(-1, 0, 0, 0), sh.first.left = 0;
     // With few units per CTA every one of them counts more than an even spread of starts and ends
     const uint32_t extra = (unsigned long long)units * heads > 4ull * tp.ctas ? 1 : 0;
     const uint32_t total = (units + extra * items) * heads, ctas = min((uint32_t)tp.ctas, total), c = blockIdx.x;
-    if (c >= ctas) return;
+    // (a list that gives rows to several sequences is not followed at all: the host's bound on the costs would not hold)
+    if (c >= ctas || rows > (uint32_t)p.b.n_rows) return;
     const uint32_t base = total / ctas, more = total - base * ctas;
     const uint32_t u0 = c * base + min(c, more), u1 = u0 + base + (c < more);
     uint32_t front = 0, at = 0;

@@ -139,3 +139,26 @@ def test_attention_refusals(s2d2):
     refused(s2d2, "mask_block", call, mask_block=1, d_row_mask=P)
     for scale in (0.0, -1.0, math.nan, math.inf):
         refused(s2d2, "scale", call, scale=scale)
+
+
+def test_attention_limits(s2d2):
+    """Sizes whose indices or counts would not fit are refused before any memory is looked at, and so is a workspace that is too small."""
+    def both(heads, r, c, text):
+        refused(s2d2, text, s2d2.paged_attention_workspace, r, c, heads, code=-6)
+        refused(s2d2, text, s2d2.paged_attention, P, P, heads, r, c, P, 1 << 40, code=-6)
+    both(4, rows(s2d2, n_rows=(1 << 22) + 1), kv(s2d2), "n_rows must be at most 2^22")
+    both(4, rows(s2d2, max_pages=1 << 25), kv(s2d2), "max_pages * page_tokens")
+    both(4, rows(s2d2, max_pages=2 ** 31 - 1), kv(s2d2, page=1 << 20), "max_pages * page_tokens")
+    both(4096, rows(s2d2, n_rows=1 << 22), kv(s2d2, heads=1), "n_rows * n_q_heads / n_kv_heads")
+    refused(s2d2, "too much", s2d2.paged_attention, P, P, 64, rows(s2d2, n_rows=1 << 20, max_pages=1 << 20), kv(s2d2, heads=64), P, 1 << 40, code=-6)
+    for heads, r, c in ((4, rows(s2d2), kv(s2d2)), (64, rows(s2d2, n_rows=5000), kv(s2d2, heads=8, dim=128))):
+        need = s2d2.paged_attention_workspace(r, c, heads)
+        assert 0 < need <= 148 * (32 + 2 * 256 * (8 + 128 * 4))
+        for ws in (need - 1, 0, -1):
+            refused(s2d2, "workspace", s2d2.paged_attention, P, P, heads, r, c, P, ws)
+
+
+def test_attention_wait_tap(s2d2):
+    from paper_2603_25702_b200 import binding
+    for bad in (0, (1 << 20) + 1):
+        refused(s2d2, "limit_polls", binding.debug_attention_wait, bad)
