@@ -892,10 +892,13 @@ tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
     }
 }
 
-// Sum of the parts of an item that the cuts went through, in the order of the keys: block (c, y) takes 32 vectors of the item that CTA c
+// Sum of the parts of an item that the cuts went through, in the order of the keys: block (c, y) takes join_warps vectors of the item that CTA c
 // began, a warp a vector.  The lanes take the parts' references and sums, 32 at a time, then four elements each (HDP 64: two) of all parts.
+// Blocks of 8 warps find room on a SM beside the tiles' CTA of one half, where they wait for its end (131072 tokens 94 us, one token 11.9; blocks of
+// 32: 98 and 13.2); beside two halves there is none, and fewer blocks are better (a prompt of 4096 166 us, with blocks of 8 172).
+__host__ __device__ constexpr int join_warps(int nh) { return nh == 1 ? 8 : 32; }
 template <int HDP, int NH>
-__global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ TileParams tp) {
+__global__ void __launch_bounds__(32 * join_warps(NH)) join_kernel(const __grid_constant__ TileParams tp) {
     constexpr int E = HDP / 32;
     pdl_wait();
     pdl_launch();
@@ -903,7 +906,7 @@ __global__ void __launch_bounds__(1024) join_kernel(const __grid_constant__ Tile
     const int c = blockIdx.x;
     const int4 d = tp.split[2 * c];
     if (d.x < 0) return;
-    const int r = blockIdx.y * 32 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int r = blockIdx.y * join_warps(NH) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int ti = (r & 127) / tp.gs, i = (d.y * NH + (r >> 7)) * tp.rows_half + ti, h = d.x + (r & 127) - ti * tp.gs;
     if (ti >= tp.rows_half || i >= tp.split[2 * c + 1].x) return;
     float m = -INFINITY, l = 0.f, o[E];
