@@ -126,22 +126,6 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
-// 2^x of two numbers below 2^7 on the multipliers, where the unit for exponentials (16 a cycle) is what a tile waits for: x = n + f with n the
-// nearest integer, 2^f = 1 + f (..) by a polynomial of degree 4 with equal ripples of 2.8e-6 on [-1/2, 1/2], n added to the exponent.
-// -127 and less, and NaN: exactly 0 (the bits of 1 less 127 in the exponent).
-__device__ __forceinline__ float2 exp2_poly(float2 x) {
-    const float2 big = make_float2(12582912.f, 12582912.f);      // 1.5 2^23: the sum's last bits are the integer
-    x = make_float2(fmaxf(x.x, -127.f), fmaxf(x.y, -127.f));
-    const float2 t = add2(x, big), n = add2(t, make_float2(-12582912.f, -12582912.f));
-    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
-    float2 y = fma2(make_float2(0.009582576341927052f, 0.009582576341927052f), f, make_float2(0.05590682849287987f, 0.05590682849287987f));
-    y = fma2(y, f, make_float2(0.24024106562137604f, 0.24024106562137604f));
-    y = fma2(y, f, make_float2(0.6931241154670715f, 0.6931241154670715f));
-    y = fma2(y, f, make_float2(1.f, 1.f));
-    y.x = __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
-    y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
-    return y;
-}
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -442,38 +426,15 @@ __device__ __forceinline__ void store32(void* dst, const uint32_t* v, bool align
     }
 }
 
-// 32 probabilities 2^(s factor - m) of scores s as bf16 pairs, and their sum in two chains.  `high`: the largest exponent that went to the
-// polynomial, which is wrong above 2^7, or NaN.
-__device__ __forceinline__ void probabilities(const uint32_t (&v)[32], float factor, float minus_m, uint32_t (&pk)[16], float2& sum, float2& sum1, float& high) {
+// 32 probabilities 2^(s factor - m) of scores s as bf16 pairs; adds them to `sum`, four chains.
+__device__ __forceinline__ void probabilities(const uint32_t (&v)[32], float factor, float minus_m, uint32_t (&pk)[16], float2 (&sum)[2]) {
     const float2 cc = make_float2(factor, factor), rr = make_float2(minus_m, minus_m);
 #pragma unroll
     for (int e = 0; e < 32; e += 2) {
-        const float2 x = fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), cc, rr);
-        // Of four pairs one by the polynomial: the exponentials' unit takes 8 cycles for a warp's instruction, the polynomial's two-fold
-        // instructions about 14 on other units (64 scores of two warps: 890 cycles; without 1190, three of eight 970).
-        float2 y;
-        if ((e / 2) % 4 < 3) {
-            y = make_float2(exp2_fast(x.x), exp2_fast(x.y));
-        } else {
-            high = max3_nan(high, x.x, x.y);
-            y = exp2_poly(x);
-        }
-        if (e & 2) sum1 = add2(sum1, y);
-        else sum = add2(sum, y);
+        const float2 x = fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), cc, rr), y = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+        sum[e >> 1 & 1] = add2(sum[e >> 1 & 1], y);
         pk[e / 2] = pack2(y.x, y.y);
     }
-}
-__device__ __forceinline__ float max64(const uint32_t (&v)[2][32]) {      // NaN if there is one
-    float mx[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const uint32_t* x = v[c >> 1] + (c & 1) * 16;
-        mx[c] = max3_nan(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]));
-#pragma unroll
-        for (int e = 3; e < 15; e += 2) mx[c] = max3_nan(mx[c], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-        mx[c] = max3_nan(mx[c], __uint_as_float(x[15]), __uint_as_float(x[15]));
-    }
-    return max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]);
 }
 __device__ __forceinline__ float first_reference(const uint32_t (&v)[32]) {
     float m = __uint_as_float(v[0]);
@@ -482,30 +443,29 @@ __device__ __forceinline__ float first_reference(const uint32_t (&v)[32]) {
     return m;
 }
 // -inf for the keys from `key` on that are not seen
-__device__ __forceinline__ void mask64(uint32_t (&v)[2][32], const paged::View& view, int key) {
+__device__ __forceinline__ void mask32(uint32_t (&v)[32], const paged::View& view, int key) {
+    const int n = view.lim - key, d = key - view.base;
+    uint32_t seen = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
+    if (d >= 0 && d < 64) seen |= (uint32_t)(view.bits >> d);
+    else if (d < 0 && d > -32) seen |= (uint32_t)view.bits << -d;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int n = view.lim - (key + 32 * c), d = key + 32 * c - view.base;
-        uint32_t seen = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1;
-        if (d >= 0 && d < 64) seen |= (uint32_t)(view.bits >> d);
-        else if (d < 0 && d > -32) seen |= (uint32_t)view.bits << -d;
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-            if (!(seen >> e & 1)) v[c][e] = 0xff800000u;
-    }
+    for (int e = 0; e < 32; ++e)
+        if (!(seen >> e & 1)) v[e] = 0xff800000u;
 }
 
 // Softmax warps: a thread has a query vector's row of scores, a lane of tensor memory, and takes it in steps of 64 keys.  It leaves the probabilities
 // over the scores as bf16 pairs, the left operand of the second product.  The scores of the next step are computed meanwhile (two buffers
 // of 64 columns; with one of 128, the most that fits beside the accumulators, every unit waited 1500 cycles for its scores).  The
-// reference m is not the maximum but what the maximum was when a step's probabilities last added up to more than 512, so these stay below that
-// (their bf16 rounding is relative), the accumulator is rarely rescaled, and no maximum is taken but then: the step's exponentials are taken
-// again with the new reference.  An item's first reference is the maximum of its first 32 scores.
-// What bounds it: 7 cycles per score and warp for exponentials and sums, and code: what runs seldom is kept short and out of
-// the way, straight code of more than one pass over the scores was slowed down by instruction fetches.
+// reference m is not the maximum: it is the maximum of the first 32 scores with one that the row sees, and goes up by a whole number when a step's
+// probabilities add up to more than 512, from the next step on.  So no maximum is taken, the accumulator is rarely rescaled, and nothing
+// has to wait for a sum; probabilities above 1 lose nothing, their rounding to bf16 is relative.  A row whose probabilities add up to more
+// than 2^100 in a step, or whose reference is above 2^20, where s c - m is too coarse, is taken again at the end (repair_rows), like one with a NaN.
+// What bounds it: of a step's 2000 cycles with two halves 1180 are exponentials (16 a cycle: 1024), 830 waits, loads and stores of
+// both halves at the same time.  With the maximum first a prompt of 4096 took 164 us instead of 155, with a check of each step's sum before its
+// probabilities are given away 157, with a quarter of the exponentials as polynomials on the other units 165.
 template <int HDP, int NH>
 __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl) {
-    constexpr float FAR = 1048576.f;
+    constexpr float FAR = 1048576.f, MOST = 1.2676506e30f;     // 2^20, 2^100
     const Params& p = tp.a;
     volatile int* abort_flag = &ctl.abort_flag;
     const int half = threadIdx.x >> 7, r = threadIdx.x & 127;
@@ -525,65 +485,59 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
         view.base = 0;
         view.bits = 0;
         if (valid) view = paged::row_view(p.mask_block, p.row_mask, w.s, i);
-        float m = -INFINITY, l = 0.f;
-        const int end = w.j1 * KEYS;
+        float m = valid ? -INFINITY : 0.f, l = 0.f, total = 0.f;          // total: of the step in front
+        bool live = valid, fresh = true;                         // fresh: a row of the warp has no reference yet
+        const int end = w.j1 * KEYS, all_see = __reduce_min_sync(0xffffffffu, view.lim);
         for (int key = w.j0 * KEYS; key < end; key += STEP, ++steps) {
             const uint32_t buf = steps & 1;
             if (!__all_sync(0xffffffffu, wait(&ctl.s_full[half][buf], steps >> 1 & 1, tp.wait_limit, abort_flag))) return false;
             if (any) {
                 tc_fence_after();
                 const uint32_t ts = tmem + half * 2 * STEP + buf * STEP;
-                uint32_t v[2][32], pk[2][16];
+                if (!__all_sync(0xffffffffu, !live || total <= 512.f)) {
+                    float alpha = 1.f;
+                    if (!(total <= MOST)) {
+                        l = __int_as_float(0x7fffffff);
+                        live = false;
+                    } else if (total > 512.f) {
+                        const float before = m;
+                        m += (float)((int)(__float_as_uint(total) >> 23) - 126);
+                        alpha = exp2_fast(before - m);
+                        l *= alpha;
+                    }
+                    if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][buf ^ 1], (steps - 1) >> 1 & 1, tp.wait_limit, abort_flag))) return false;      // the product before this one's
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int d = 0; d < HDP; d += 16) {
+                        float o[16];
+                        tmem_ld16(to + d, o);
+                        uint32_t u[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(o[e] * alpha);
+                        tmem_st16(to + d, u);
+                    }
+                }
+                uint32_t v[2][32], pk[16];
                 tmem_ld32_issue(ts, v[0]);
                 tmem_ld32_issue(ts + 32, v[1]);
                 tmem_ld_wait();
-                if (!__all_sync(0xffffffffu, key + STEP <= view.lim)) mask64(v, view, key);
-                const float before = m;
-                if (key == w.j0 * KEYS) m = fmaxf(first_reference(v[0]) * p.scale_log2, -INFINITY);
-                float2 sum, sum1;
-                float factor = p.scale_log2, total;
-#pragma unroll 1
-                for (bool again = false;; again = true) {
-                    const float minus_m = m == -INFINITY ? 0.f : -m;
-                    float high = -INFINITY;
-                    sum = sum1 = make_float2(0.f, 0.f);
-                    probabilities(v[0], factor, minus_m, pk[0], sum, sum1, high);
-                    probabilities(v[1], factor, minus_m, pk[1], sum, sum1, high);
-                    sum = add2(sum, sum1);
-                    total = sum.x + sum.y;
-                    // in order: no NaN, nothing above 2^9, and a reference that is a number of ordinary size
-                    if (again || __all_sync(0xffffffffu, !valid || (total <= 512.f && high <= 9.f && fabsf(m) <= FAR))) break;
-                    const float top = max64(v) * p.scale_log2;
-                    if (!(top < INFINITY)) l = __int_as_float(0x7fffffff);        // a NaN or an infinity that the row sees
-                    m = fmaxf(m, top);
-                    const float alpha = before == m ? 1.f : exp2_fast(before - m);
-                    l *= alpha;
-                    if (key > w.j0 * KEYS && __any_sync(0xffffffffu, alpha != 1.f)) {
-                        if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][buf ^ 1], (steps - 1) >> 1 & 1, tp.wait_limit, abort_flag))) return false;      // the product before this one's
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < HDP; c += 16) {
-                            float o[16];
-                            tmem_ld16(to + c, o);
-                            uint32_t u[16];
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(o[e] * alpha);
-                            tmem_st16(to + c, u);
-                        }
-                    }
-                    if (__any_sync(0xffffffffu, fabsf(m) > FAR && m != -INFINITY)) {
-                        // s c - m in one operation: m is rounded, so the largest score's difference is off by up to 2^-24 m.  That only moves
-                        // the reference, unless m is so large that it leaves the range of the exponentials: then scores are rounded like m first.
-                        factor = 1.f;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            v[0][e] = __float_as_uint(__fmul_rn(__uint_as_float(v[0][e]), p.scale_log2));
-                            v[1][e] = __float_as_uint(__fmul_rn(__uint_as_float(v[1][e]), p.scale_log2));
-                        }
-                    }
+                if (key + STEP > all_see) {
+                    mask32(v[0], view, key);
+                    mask32(v[1], view, key + 32);
                 }
-                tmem_st16(ts, pk[0]);
-                tmem_st16(ts + 16, pk[1]);
+                if (fresh) {
+                    if (m == -INFINITY) m = fmaxf(first_reference(v[0]) * p.scale_log2, m);
+                    if (m == -INFINITY) m = fmaxf(first_reference(v[1]) * p.scale_log2, m);
+                    fresh = __any_sync(0xffffffffu, m == -INFINITY);
+                }
+                const float minus_m = m == -INFINITY ? 0.f : -m;
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                probabilities(v[0], p.scale_log2, minus_m, pk, sum);
+                tmem_st16(ts, pk);
+                probabilities(v[1], p.scale_log2, minus_m, pk, sum);
+                tmem_st16(ts + 16, pk);
+                sum[0] = add2(sum[0], sum[1]);
+                total = sum[0].x + sum[0].y;
                 l += total;
                 tmem_st_wait();
                 tc_fence_before();
@@ -598,7 +552,7 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
             const int h = w.head0 + hi;
             const bool nan = !w.s.ok || *(volatile int*)&ctl.bad[list.index % (2 * ITEMS)] == list.index + 1, whole = w.whole();
             const float undefined = __int_as_float(0x7fffffff);
-            if (nan) l = undefined;
+            if (nan || (fabsf(m) > FAR && m != -INFINITY)) l = undefined;
             const float inv = nan ? undefined : whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
             const size_t slot = ((size_t)(2 * blockIdx.x + (w.j0 == 0)) * NH + half) * QTILE + r;
             char* dst = whole ? (char*)(p.out + row * p.out_ld + (long long)h * p.head_dim) : (char*)(tp.part_o + slot * HDP);

@@ -117,9 +117,8 @@ class Batch:
         """(out, lse, tolerance of out, tolerance of lse) in fp64; rows of no sequence hold 7 with tolerance 0.
 
         Tolerances.  A score is a sum of dim products in fp32, each addition off by at most 2^-23 of the sum of magnitudes (the tensor core
-        may cut off): ds = dim 2^-23 scale |q| |k|, plus 2^-22 of the score for the change of base.  It and the exponential
-        (2^-21; 2^-18 where it is a polynomial of degree 4 with ripples of 2.8e-6 = 2^-18.4) change a probability by that factor, in the numerator
-        and in the sum.  Rounding probabilities to bf16 changes each by at
+        may cut off): ds = dim 2^-23 scale |q| |k|, plus 2^-22 of the score for the change of base.  It and the exponential (2^-22)
+        change a probability by that factor, in the numerator and in the sum.  Rounding probabilities to bf16 changes each by at
         most 2^-8 of itself, adding up to kv of them in fp32 by kv 2^-23.  With A = sum p |v| / sum p the output is off by that times A, and
         by one rounding to bf16."""
         dev, group = self.cache.device, self.heads // self.kv_heads
@@ -149,7 +148,7 @@ class Batch:
                     mag = torch.stack([(e[r][seen[r], None] * v[seen[r]].abs()).sum(0) for r in range(n)])
                 out[at, h] = torch.where(total == 0, 0.0, num / total)
                 lse[at, h] = (top0 + torch.log(total))[:, 0]
-                ds = self.dim * 2.0 ** -23 * (big.amax(1, keepdim=True) if kv else 0.0) + 2.0 ** -21 + 2.0 ** -18
+                ds = self.dim * 2.0 ** -23 * (big.amax(1, keepdim=True) if kv else 0.0) + 2.0 ** -21
                 tol[at, h] = torch.where(total == 0, 0.0, mag / total) * (2.0 ** -8 + kv * 2.0 ** -23 + 2 * ds) + out[at, h].abs() * 2.0 ** -8
                 tol_lse[at, h] = (ds + kv * 2.0 ** -24 + lse[at, h].abs()[:, None] * 2.0 ** -21 + 2.0 ** -20)[:, 0]
         return out, lse, tol, tol_lse
