@@ -82,7 +82,7 @@ int encode_q(const ops::Device* dev, CUtensorMap* map, const void* q, long long 
 template <int HDP, int NH>
 cudaError_t launch_tiles(const CUtensorMap& map_q, const CUtensorMap& map_k, const CUtensorMap& map_v, const patt::TileParams& t, const Plan& n, cudaStream_t st) {
     cudaError_t e = ops::launch(patt::tile_kernel<HDP, NH>, dim3(n.ctas), patt::threads(NH), n.smem, 1, st, map_q, map_k, map_v, t);
-    if (!e && n.joins) e = ops::launch(patt::join_kernel<HDP, NH>, dim3(n.ctas, 128 * NH / patt::join_warps(NH)), 32 * patt::join_warps(NH), 0, 1, st, t);
+    if (!e && n.joins) e = ops::launch(patt::join_kernel<HDP, NH>, dim3(n.ctas, 128 * NH / (patt::JOIN_WARPS * patt::join_vectors(NH))), 32 * patt::JOIN_WARPS, 0, 1, st, t);
     return e;
 }
 

@@ -846,57 +846,88 @@ tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
     }
 }
 
-// Sum of the parts of an item that the cuts went through, in the order of the keys: block (c, y) takes join_warps vectors of the item that CTA c
-// began, a warp a vector.  The lanes take the parts' references and sums, 32 at a time, then four elements each (HDP 64: two) of all parts.
-// Blocks of 8 warps find room on a SM beside the tiles' CTA of one half, where they wait for its end (131072 tokens 94 us, one token 11.9; blocks of
-// 32: 98 and 13.2); beside two halves there is none, and fewer blocks are better (a prompt of 4096 166 us, with blocks of 8 172).
-__host__ __device__ constexpr int join_warps(int nh) { return nh == 1 ? 8 : 32; }
+// Sum of the parts of an item that the cuts went through, in the order of the keys: a block takes JOIN_WARPS * join_vectors vectors of the item that
+// CTA blockIdx.x began, a warp join_vectors at a time.  The lanes take the parts' references and sums, 32 at a time, then four elements each
+// (HDP 64: two) of all parts.  Blocks of 8 warps find room on a SM beside the tiles' CTA, where they wait for its end (131072 tokens 94 us, one
+// token 11.8; blocks of 32: 98 and 13.2).  Items of two halves have parts of 256 vectors, of which a warp has two in flight together (ragged
+// chunks 64 us, one by one 67); with one half that costs more than it gives (131072 tokens 98 us).
+constexpr int JOIN_WARPS = 8;
+__host__ __device__ constexpr int join_vectors(int nh) { return nh; }
 template <int HDP, int NH>
-__global__ void __launch_bounds__(32 * join_warps(NH)) join_kernel(const __grid_constant__ TileParams tp) {
-    constexpr int E = HDP / 32;
+__global__ void __launch_bounds__(32 * JOIN_WARPS) join_kernel(const __grid_constant__ TileParams tp) {
+    constexpr int E = HDP / 32, V = join_vectors(NH);
     pdl_wait();
     pdl_launch();
     const Params& p = tp.a;
     const int c = blockIdx.x;
     const int4 d = tp.split[2 * c];
     if (d.x < 0) return;
-    const int r = blockIdx.y * join_warps(NH) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int ti = (r & 127) / tp.gs, i = (d.y * NH + (r >> 7)) * tp.rows_half + ti, h = d.x + (r & 127) - ti * tp.gs;
-    if (ti >= tp.rows_half || i >= tp.split[2 * c + 1].x) return;
-    float m = -INFINITY, l = 0.f, o[E];
+    const int rows = tp.split[2 * c + 1].x, r0 = (blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5)) * V, lane = threadIdx.x & 31;
+    int i[V], h[V];
+    bool some[V], any = false;
+    float m[V], l[V], o[V][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int v = 0; v < V; ++v) {
+        const int r = r0 + v, ti = (r & 127) / tp.gs;
+        i[v] = (d.y * NH + (r >> 7)) * tp.rows_half + ti;
+        h[v] = d.x + (r & 127) - ti * tp.gs;
+        some[v] = ti < tp.rows_half && i[v] < rows;
+        any |= some[v];
+        m[v] = -INFINITY;
+        l[v] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[v][e] = 0.f;
+    }
+    if (!any) return;
     for (int first = c; first <= d.z; first += 32) {
         const int part = first + lane, n = min(32, d.z + 1 - first);
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (lane < n) ml = tp.part_ml[(size_t)(2 * part + (part == c)) * (128 * NH) + r];
-        const float top = fmaxf(m, warp_max(ml.x)), ref = top == -INFINITY ? 0.f : top;
-        const float f = exp2_fast(m - ref), g = exp2_fast(ml.x - ref);
-        l = l * f + warp_sum(ml.y * g);
-        m = top;
+        float g[V];
+        float2 ml[V];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= f;
-#pragma unroll 8
+        for (int v = 0; v < V; ++v) {
+            ml[v] = make_float2(-INFINITY, 0.f);
+            if (some[v] && lane < n) ml[v] = tp.part_ml[(size_t)(2 * part + (part == c)) * (128 * NH) + r0 + v];
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float top = fmaxf(m[v], warp_max(ml[v].x)), ref = top == -INFINITY ? 0.f : top, f = exp2_fast(m[v] - ref);
+            g[v] = exp2_fast(ml[v].x - ref);
+            l[v] = l[v] * f + warp_sum(ml[v].y * g[v]);
+            m[v] = top;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[v][e] *= f;
+        }
+#pragma unroll 8 / V
         for (int k = 0; k < n; ++k) {
-            const float* src = tp.part_o + ((size_t)(2 * (first + k) + (first + k == c)) * (128 * NH) + r) * HDP + lane * E;
-            const float weight = __shfl_sync(0xffffffffu, g, k);
-            if constexpr (E == 4) {
-                const float4 v = *reinterpret_cast<const float4*>(src);
-                o[0] = fmaf(v.x, weight, o[0]), o[1] = fmaf(v.y, weight, o[1]), o[2] = fmaf(v.z, weight, o[2]), o[3] = fmaf(v.w, weight, o[3]);
-            } else {
-                const float2 v = *reinterpret_cast<const float2*>(src);
-                o[0] = fmaf(v.x, weight, o[0]), o[1] = fmaf(v.y, weight, o[1]);
+            const float* src = tp.part_o + ((size_t)(2 * (first + k) + (first + k == c)) * (128 * NH) + r0) * HDP + lane * E;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float weight = __shfl_sync(0xffffffffu, g[v], k);
+                float x[E];
+                if constexpr (E == 4) {
+                    const float4 u = some[v] ? *reinterpret_cast<const float4*>(src + v * HDP) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+                } else {
+                    const float2 u = some[v] ? *reinterpret_cast<const float2*>(src + v * HDP) : make_float2(0.f, 0.f);
+                    x[0] = u.x, x[1] = u.y;
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[v][e] = fmaf(x[e], weight, o[v][e]);
             }
         }
     }
-    const long long row = d.w + i;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    bf16* out = p.out + row * p.out_ld + (long long)h * p.head_dim + lane * E;
-    if (lane * E < p.head_dim) {
-        if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv));
-        else *reinterpret_cast<uint32_t*>(out) = pack2(o[0] * inv, o[1] * inv);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if (!some[v]) continue;
+        const long long row = d.w + i[v];
+        const float inv = l[v] == 0.f ? 0.f : 1.f / l[v];
+        bf16* out = p.out + row * p.out_ld + (long long)h[v] * p.head_dim + lane * E;
+        if (lane * E < p.head_dim) {
+            if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2(o[v][0] * inv, o[v][1] * inv), pack2(o[v][2] * inv, o[v][3] * inv));
+            else *reinterpret_cast<uint32_t*>(out) = pack2(o[v][0] * inv, o[v][1] * inv);
+        }
+        if (p.lse && lane == 0) p.lse[row * p.heads + h[v]] = l[v] == 0.f ? -INFINITY : (m[v] + log2f(l[v])) * 0.6931471805599453f;
     }
-    if (p.lse && lane == 0) p.lse[row * p.heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 }  // namespace patt
