@@ -437,7 +437,7 @@ __device__ __forceinline__ void probabilities(const uint32_t (&v)[32], float fac
     }
 }
 __device__ __forceinline__ float first_reference(const uint32_t (&v)[32]) {
-    float m = __uint_as_float(v[0]);
+    float m = fmaxf(__uint_as_float(v[0]), __uint_as_float(v[31]));
 #pragma unroll
     for (int e = 1; e < 31; e += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(__uint_as_float(v[e])), "f"(__uint_as_float(v[e + 1])));
     return m;

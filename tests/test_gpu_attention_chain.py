@@ -210,3 +210,13 @@ def test_references_that_rise_and_fall(s2d2):
     for sign in (1, -1):
         b.q.copy_(b.q.abs() * sign)
         b.check(b.attend(s2d2, scale=0.25), b.want(scale=0.25))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens", [[(64, 64)], [(64, 64), (40, 40), (64, 64)]])
+def test_rows_that_see_a_single_key(s2d2, lens, dim):
+    """Each at another place of the tile, with scores far from zero on either side."""
+    bits = torch.cat([1 << torch.arange(n, dtype=torch.int64).roll(7) for n, _ in lens]).cuda()
+    b = au.Batch(lens, 4, 2, dim)
+    b.q.mul_(20)
+    b.check(b.attend(s2d2, 0, bits), b.want(0, bits))
