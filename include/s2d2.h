@@ -532,7 +532,7 @@ int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_o
                    const s2d2_rows* rows, const s2d2_paged_kv* kv, void* cuda_stream);
 
 /* out[row, h] <- softmax over the visible keys of (scale q[row, h] . k) times the values, q and out [n_rows, n_q_heads, head_dim] bf16,
- * rows *_stride elements apart (16-byte aligned, strides multiples of 8); head h reads kv head h / (n_q_heads / n_kv_heads);
+ * rows *_stride elements apart (16-byte aligned, strides multiples of 8; they must not overlap); head h reads kv head h / (n_q_heads / n_kv_heads);
  * d_lse [n_rows, n_q_heads] (may be NULL) <- log sum exp of its scores.  head_dim up to 128.  scale > 0.
  * Visible to row i of n (the cache holds kv tokens, the row's index is p = kv - n + i):
  *   mask_block = 1     j <= p (causal)
@@ -542,7 +542,7 @@ int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_o
  *                      d_row_mask[row] is set
  * A row that sees nothing (or only scores of -inf) gets 0 and lse -inf; keys and values that a row does not see have no influence on it, NaN
  * and infinities included.  Scores, sums and maxima are fp32; probabilities are rounded to bf16 for the product with the
- * values.  A kv length that is not followed makes the sequence's rows NaN, a page that is not one the rows that see its tokens (and rows next to
+ * values (of few rows, half of them to twice its bits).  A kv length that is not followed makes the sequence's rows NaN, a page that is not one the rows that see its tokens (and rows next to
  * them may become NaN, too).  n_rows is at most 2^22, max_pages * page_tokens and n_rows * n_q_heads / n_kv_heads at most 2^30; more than
  * 2e9 pairs of a tile of query vectors and a tile of 128 keys, by these bounds, is S2D2_ERR_UNSUPPORTED.
  * d_ws: at least s2d2_paged_attention_workspace bytes (they depend on the fields of the structs, not on what is on the device),
