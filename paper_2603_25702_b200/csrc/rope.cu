@@ -77,7 +77,7 @@ struct Raw8 {
         }
     }
 };
-// 1 / sqrt(x), the approximation improved once: within 2 units in the last place
+// 1 / sqrt(x), the approximation improved by a step of Newton's method: within 2 units in the last place
 __device__ __forceinline__ float inverse_root(float x) {
     const float y = rsqrtf(x);
     return x > 0.f && x < INFINITY ? y * fmaf(-0.5f * x * y, y, 1.5f) : y;
