@@ -121,7 +121,7 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     const char* op = "paged_attention";
     if (int rc = check_shape(op, rows, kv, n_q_heads)) return rc;
     const long long width = (long long)n_q_heads * kv->head_dim;
-    if (q_stride < width || q_stride % 8 || q_stride > (1LL << 40)) return ops::fail(S2D2_ERR_INVALID, "%s: q_stride must be a multiple of 8 in heads * head_dim..2^40", op);
+    if (q_stride < width || q_stride % 8 || q_stride >= (1LL << 39)) return ops::fail(S2D2_ERR_INVALID, "%s: q_stride must be a multiple of 8 from heads * head_dim on, below 2^39", op);
     if (out_stride < width || out_stride % 8 || out_stride > (1LL << 40)) return ops::fail(S2D2_ERR_INVALID, "%s: out_stride must be a multiple of 8 in heads * head_dim..2^40", op);
     if (mask_block < 0) return ops::fail(S2D2_ERR_INVALID, "%s: mask_block must not be negative", op);
     if (d_row_mask && mask_block) return ops::fail(S2D2_ERR_INVALID, "%s: mask_block must be 0 with row masks", op);

@@ -860,9 +860,9 @@ tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
 
 // Sum of the parts of an item that the cuts went through, in the order of the keys: a block takes JOIN_WARPS * join_vectors vectors of the item that
 // CTA blockIdx.x began, a warp join_vectors at a time.  The lanes take the parts' references and sums, 32 at a time, then four elements each
-// (HDP 64: two) of all parts.  Blocks of 8 warps find room on a SM beside the tiles' CTA, where they wait for its end (131072 tokens 94 us, one
-// token 11.8; blocks of 32: 98 and 13.2).  Items of two halves have parts of 256 vectors, of which a warp has two in flight together (ragged
-// chunks 64 us, one by one 67); with one half that costs more than it gives (131072 tokens 98 us).
+// (HDP 64: two) of all parts.  Blocks of 8 warps find room on a SM beside the tiles' CTA, where they wait for its end (131072 tokens 3.9 us
+// less than with blocks of 32, one token 1.3 less).  Items of two halves have parts of 256 vectors, of which a warp has two in flight together (ragged
+// chunks 64 us, one by one 67); with one half that costs more than it gives (131072 tokens 3.4 us more).
 constexpr int JOIN_WARPS = 8;
 __host__ __device__ constexpr int join_vectors(int nh) { return nh; }
 template <int HDP, int NH>

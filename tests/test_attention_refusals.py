@@ -158,6 +158,12 @@ def test_attention_limits(s2d2):
             refused(s2d2, "workspace", s2d2.paged_attention, P, P, heads, r, c, P, ws)
 
 
+def test_attention_strides_that_no_copy_can_have(s2d2):
+    for q in (1 << 39, 1 << 40, -8):
+        refused(s2d2, "q_stride", s2d2.paged_attention, P, P, 4, rows(s2d2), kv(s2d2), P, 1 << 40, q_stride=q)
+    refused(s2d2, "out_stride", s2d2.paged_attention, P, P, 4, rows(s2d2), kv(s2d2), P, 1 << 40, out_stride=(1 << 40) + 8)
+
+
 def test_attention_wait_tap(s2d2):
     from paper_2603_25702_b200 import binding
     for bad in (0, (1 << 20) + 1):
