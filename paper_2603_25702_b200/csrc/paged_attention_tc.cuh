@@ -458,13 +458,23 @@ __device__ __forceinline__ void mask32(uint32_t (&v)[32], const paged::View& vie
         if (!(seen >> e & 1)) v[e] = 0xff800000u;
 }
 
+// The reference goes up by a whole number, so far that `total` is below 1 against it; gives the factor of what was added up against the old one.
+__device__ __forceinline__ float raise_reference(float& m, float& l, float total) {
+    const float before = m;
+    m += (float)((int)(__float_as_uint(total) >> 23) - 126);
+    const float alpha = exp2_fast(before - m);
+    l *= alpha;
+    return alpha;
+}
+
 // Softmax warps: a thread has a query vector's row of scores, a lane of tensor memory, and takes it in steps of 64 keys.  It leaves the probabilities
 // over the scores as bf16 pairs, the left operand of the second product.  The scores of the next step are computed meanwhile (two buffers
 // of 64 columns; with one of 128, the most that fits beside the accumulators, every unit waited 1500 cycles for its scores).  The
 // reference m is not the maximum: it is the maximum of the first 32 scores with one that the row sees, and goes up by a whole number when a step's
 // probabilities add up to more than 512, from the next step on.  So no maximum is taken, the accumulator is rarely rescaled, and nothing
 // has to wait for a sum; probabilities above 1 lose nothing, their rounding to bf16 is relative.  A row whose probabilities add up to more
-// than 2^100 in a step, or whose reference is above 2^20, where s c - m is too coarse, is taken again at the end (repair_rows), like one with a NaN.
+// than 2^100 in a step, the last of an item or part included, or whose reference is above 2^20, where s c - m is too coarse, is taken again at the end
+// (repair_rows), like one with a NaN.
 // Rounding: with probabilities in bf16 the output is off by 1.4 times the rounding of the output itself (0.0023 of it, root mean square; 0.0016).  Items of
 // one tile, bound by memory, also take what the rounding left of the first 32 of a step's 64 probabilities: 1.2 times, for 3 % of
 // the time (131072 tokens 94.5 -> 97.7 us); of all 64 it would be 11 % (105), and items of two tiles are bound by this warp.
@@ -508,10 +518,7 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
                         l = __int_as_float(0x7fffffff);
                         live = false;
                     } else if (total > 512.f) {
-                        const float before = m;
-                        m += (float)((int)(__float_as_uint(total) >> 23) - 126);
-                        alpha = exp2_fast(before - m);
-                        l *= alpha;
+                        alpha = raise_reference(m, l, total);
                     }
                     if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][buf ^ 1], (steps - 1) >> 1 & 1, tp.wait_limit, abort_flag))) return false;      // the product before this one's
                     tc_fence_after();
@@ -561,8 +568,15 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
             const int h = w.head0 + hi;
             const bool nan = !w.s.ok || *(volatile int*)&ctl.bad[list.index % (2 * ITEMS)] == list.index + 1, whole = w.whole();
             const float undefined = __int_as_float(0x7fffffff);
-            if (nan || (fabsf(m) > FAR && m != -INFINITY)) l = undefined;
-            const float inv = nan ? undefined : whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+            // what the step in front of a next one would do with the last one's sum; a part's reference goes up, too, so that join_kernel weighs parts
+            // by references that are not far below what they hold
+            float raised = 1.f;
+            if (nan || !(total <= MOST) || (fabsf(m) > FAR && m != -INFINITY)) {
+                l = undefined;
+            } else if (!whole && total > 512.f) {
+                raised = raise_reference(m, l, total);
+            }
+            const float factor = nan ? undefined : whole ? (l == 0.f ? 0.f : 1.f / l) : raised;
             const size_t slot = ((size_t)(2 * blockIdx.x + (w.j0 == 0)) * NH + half) * QTILE + r;
             char* dst = whole ? (char*)(p.out + row * p.out_ld + (long long)h * p.head_dim) : (char*)(tp.part_o + slot * HDP);
             float check = fabsf(l), check1 = 0.f;                                  // infinite or NaN where something is
@@ -579,10 +593,10 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
                 }
                 if (whole) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) u[e] = pack2(__uint_as_float(u[2 * e]) * inv, __uint_as_float(u[2 * e + 1]) * inv);
-                } else if (nan) {
+                    for (int e = 0; e < 16; ++e) u[e] = pack2(__uint_as_float(u[2 * e]) * factor, __uint_as_float(u[2 * e + 1]) * factor);
+                } else {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) u[e] = 0x7fffffffu;
+                    for (int e = 0; e < 32; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * factor);
                 }
                 if (valid) {
                     if (whole) {
