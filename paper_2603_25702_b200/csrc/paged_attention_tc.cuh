@@ -214,18 +214,41 @@ struct Setup {
     Items first;
 };
 
+// One warp: whether a sequence with rows begins in front of the end of an earlier one that has some.
+__device__ __noinline__ bool out_of_order(const Params& p) {
+    const int lane = threadIdx.x & 31;
+    int front = 0;                             // end of the rows so far
+    for (int s0 = 0; s0 < p.b.n_seqs; s0 += 32) {
+        int first = 0, end = 0;
+        if (s0 + lane < p.b.n_seqs) {
+            const paged::Seq q = paged::read_seq(p.b, s0 + lane);
+            if (q.n) first = q.row0, end = q.row0 + q.n;
+        }
+        int most = end;                        // inclusive maxima
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, most, o);
+            if (lane >= o) most = max(most, y);
+        }
+        const int before = __shfl_up_sync(0xffffffffu, most, 1);
+        if (__any_sync(0xffffffffu, end && first < max(front, lane ? before : 0))) return true;
+        front = max(front, __shfl_sync(0xffffffffu, most, 31));
+    }
+    return false;
+}
+
 // One warp: the begin of this CTA's range and its length, from the lengths on the device.  Sequences are counted 32 / seq_lanes at a time.
 template <int NH>
 __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out) {
     const Params& p = tp.a;
     const int lane = threadIdx.x & 31, per = 32 / tp.seq_lanes, heads = p.kv_heads * tp.vsub;
-    uint32_t rows = 0;
+    bool falls = false;                        // row0 decreases somewhere
     // items (x) and units (y) of a sequence, by seq_lanes lanes; the first of them has the sums
     auto count = [&](int s) {
         uint2 n = make_uint2(0, 0);
         if (s < p.b.n_seqs) {
             const paged::Seq q = usable_seq(p, s);
-            if ((lane & (tp.seq_lanes - 1)) == 0) rows = min(rows + q.n, 1u << 26);
+            falls |= p.b.row0[s + 1] < q.row0;
             const int items = items_of<NH>(tp, q.n);
             for (int t = lane & (tp.seq_lanes - 1); t < items; t += tp.seq_lanes) n.y += units_of<NH>(tp, q, t), ++n.x;
         }
@@ -241,14 +264,15 @@ __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out
     }
     items = __reduce_add_sync(0xffffffffu, items);
     units = __reduce_add_sync(0xffffffffu, units);
-    rows = __reduce_add_sync(0xffffffffu, rows);
     out.left = 0;
     if (lane == 0) tp.split[2 * blockIdx.x] = make_int4(-1, 0, 0, 0), sh.first.left = 0;
     // With few units per CTA every one of them counts more than an even spread of starts and ends
     const uint32_t extra = (unsigned long long)units * heads > 4ull * tp.ctas ? 1 : 0;
     const uint32_t total = (units + extra * items) * heads, ctas = min((uint32_t)tp.ctas, total), c = blockIdx.x;
-    // (a list that gives rows to several sequences is not followed at all: the host's bound on the costs would not hold)
-    if (c >= ctas || rows > (uint32_t)p.b.n_rows) return;
+    if (c >= ctas) return;
+    // Rows of several sequences would be written by several CTAs, and the host's bound on the costs would not hold: such a list is not followed at all.
+    // (One that never decreases has none.)
+    if (__any_sync(0xffffffffu, falls) && out_of_order(p)) return;
     const uint32_t base = total / ctas, more = total - base * ctas;
     const uint32_t u0 = c * base + min(c, more), u1 = u0 + base + (c < more);
     uint32_t front = 0, at = 0;
