@@ -504,8 +504,8 @@ int s2d2_qk_rope(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out
  * last used one are not looked at.  Rows behind d_row0[n_seqs] pad the batch: their outputs are left as they were.
  * d_row0 must not decrease and must stay within 0..n_rows: a sequence for which it does not has no rows.  A d_kv_len outside
  * 0..max_pages * page_tokens, or a page outside 0..n_pages - 1, is not followed (see the calls).  Where a sequence with rows begins in front of the
- * end of an earlier one with rows (d_row0 must decrease for that), s2d2_paged_attention follows none of the list; of sequences that share rows
- * s2d2_kv_append follows one. */
+ * end of an earlier one with rows (d_row0 must decrease for that), s2d2_paged_attention follows none of the list;
+ * s2d2_kv_append gives each row to one of the sequences that have it. */
 typedef struct {
     const int32_t* d_row0;      /* [n_seqs + 1]                                  */
     const int32_t* d_kv_len;    /* [n_seqs]                                      */

@@ -105,7 +105,7 @@ __device__ __forceinline__ float2 turn(int pos, double freq, float scale) {
 }
 
 template <bool APPEND>
-__device__ __forceinline__ Place place_of(const RopeParams& p, long long row) {
+__device__ __forceinline__ Place place_of(const RopeParams& p, long long row, int seq) {      // seq: append only
     Place w;
     if (!APPEND) {
         w.seq = 0;
@@ -113,7 +113,7 @@ __device__ __forceinline__ Place place_of(const RopeParams& p, long long row) {
         w.page = w.token = 0;
         return w;
     }
-    w.seq = paged::find_seq(p.b, (int)row);
+    w.seq = seq;
     w.page = -1;
     w.pos = w.token = 0;
     if (w.seq < 0) return w;
@@ -125,6 +125,23 @@ __device__ __forceinline__ Place place_of(const RopeParams& p, long long row) {
         w.token = j & p.c.page_mask;
     }
     return w;
+}
+// Rows of a CTA that the search in row0 gave to no sequence: they pad the batch, or row0 decreases and the search went the wrong way.  The CTA looks
+// through all sequences; the first that has a row gets it.
+__device__ __forceinline__ void find_by_scan(const RopeParams& p, long long row0, int rows, Place* places) {
+    __shared__ int owner[MAX_ROWS];
+    const bool lost = threadIdx.x < rows && places[threadIdx.x].seq < 0;
+    if (threadIdx.x < rows) owner[threadIdx.x] = p.b.n_seqs;
+    __syncthreads();
+    for (int s = threadIdx.x; s < p.b.n_seqs; s += RT) {
+        const paged::Seq q = paged::read_seq(p.b, s);
+        if (!q.n) continue;
+        const int first = q.row0 - (int)row0, end = min(rows, first + q.n);
+        for (int r = max(0, first); r < end; ++r) atomicMin(&owner[r], s);
+    }
+    __syncthreads();
+    if (lost && owner[threadIdx.x] < p.b.n_seqs) places[threadIdx.x] = place_of<true>(p, row0 + threadIdx.x, owner[threadIdx.x]);
+    __syncthreads();
 }
 // First element of a head of the output, or null where there is none.
 template <typename TO, bool APPEND>
@@ -203,8 +220,17 @@ __global__ void __launch_bounds__(RT) rope_kernel(const RopeParams p) {
             if (p.k.gain) gains[hd + i] = p.k.gain[i];
         }
     }
-    if (threadIdx.x < rows) places[threadIdx.x] = place_of<APPEND>(p, row0 + threadIdx.x);
-    __syncthreads();
+    bool lost = false;
+    if (threadIdx.x < rows) {
+        const int seq = APPEND ? paged::find_seq(p.b, (int)(row0 + threadIdx.x)) : 0;
+        places[threadIdx.x] = place_of<APPEND>(p, row0 + threadIdx.x, seq);
+        lost = seq < 0;
+    }
+    if (APPEND) {
+        if (__syncthreads_or(lost)) find_by_scan(p, row0, rows, places);
+    } else {
+        __syncthreads();
+    }
     for (int i = threadIdx.x; i < rows * pairs; i += RT) {
         const int r = i / pairs, f = i - r * pairs;
         const float2 cs = turn(places[r].pos, p.freqs[f], p.scale);
