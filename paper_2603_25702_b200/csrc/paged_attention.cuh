@@ -35,11 +35,13 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
 }
 
 // Maximum (times scale_log2), sum and weighted values of one (row, head) over the keys [k0, k1), by a warp: a lane takes a key's
-// score, then every lane takes the elements lane, lane + 32, .. of the values.  Keys that are not seen are not read.
+// score, then every lane takes the elements lane, lane + 32, .. of the values.  Keys that are not seen are not read.  `progress` (shared memory)
+// goes up by one per 32 keys.
 struct RowSum {
     float m, l, o[4];
 };
-__device__ __forceinline__ RowSum row_sum(const Params& p, int seq, int kv, int kvh, const bf16* q, const paged::View& view, int k0, int k1) {
+__device__ __forceinline__ RowSum row_sum(const Params& p, int seq, int kv, int kvh, const bf16* q, const paged::View& view, int k0, int k1,
+                                          int* progress) {
     const int lane = threadIdx.x & 31;
     RowSum a;
     a.m = -INFINITY;
@@ -48,6 +50,7 @@ __device__ __forceinline__ RowSum row_sum(const Params& p, int seq, int kv, int 
     for (int i = 0; i < 4; ++i) a.o[i] = 0.f;
     const long long head = (long long)kvh * p.c.head_stride;
     for (int j0 = k0; j0 < k1; j0 += 32) {
+        if (lane == 0) atomicAdd(progress, 1);
         const int j = j0 + lane;
         const bool seen = j < min(k1, kv) && view.sees(j);
         long long at = -1;

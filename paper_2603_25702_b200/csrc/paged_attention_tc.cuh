@@ -54,15 +54,28 @@ __device__ __forceinline__ bool peek(uint64_t* bar, uint32_t parity) {
         : "memory");
     return done;
 }
-// Bounded wait for the phase with the given parity; false when it has run out or another role of the CTA has given up.  (Not unrolled: that was
-// most of the kernel's code, 200 KB, which had to be fetched again and again; a wait that was over took 300 cycles instead of 75.)
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, uint32_t limit, volatile int* abort_flag) {
+// What ends or lengthens the waits of a CTA
+struct Watch {
+    int abort;                       // a role has given up
+    int progress;                    // counts blocks of keys of rows that are taken again: what waits for them does not give up
+};
+// Bounded wait for the phase with the given parity; false when it has run out (`limit` polls without progress) or another role of the CTA has given
+// up.  (Not unrolled: that was most of the kernel's code, 200 KB, which had to be fetched again and again; a wait that was over took 300 cycles instead
+// of 75.)
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, uint32_t limit, const volatile Watch* watch) {
+    int progress = 0;
 #pragma unroll 1
-    for (uint32_t it = 0; it < WAIT_LIMIT; ++it) {
+    for (uint32_t it = 0;; ++it) {
         if (poll(bar, parity)) return true;
-        if ((it & 31u) == 31u && (it >= limit || *abort_flag)) return false;
+        if ((it & 31u) != 31u) continue;
+        if (watch->abort) return false;
+        if (it >= limit) {
+            const int now = watch->progress;
+            if (now == progress) return false;
+            progress = now;
+            it = 0;
+        }
     }
-    return false;
 }
 __device__ __forceinline__ void arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory"); }
 __device__ __forceinline__ void settle() {                     // after a time-out: copies in flight land
@@ -348,7 +361,7 @@ struct Control {
     Item items[ITEMS];
     int bad[2 * ITEMS];                    // bad[i % 16] == i + 1: item i of this CTA has a page that is not one
     uint32_t tmem_slot;
-    int abort_flag;
+    Watch watch;
     Setup setup;
 };
 constexpr int BARRIERS = 2 * MAX_STAGES + 2 * ITEMS + 16;
@@ -362,8 +375,8 @@ struct Ring {                        // position in the ring: stage, and the par
 
 // Rows whose accumulators are not finite: a NaN or an infinity in a value that a row does not see has come in through a probability of zero (or the
 // row sees it: then the result is the same).  The warp takes them again, one by one, without the keys that they do not see.  `i`, `h`: this
-// lane's row of the sequence and head; `slot`: its place in the parts.
-__device__ __noinline__ void repair_rows(const TileParams& tp, const Item& w, int i, int h, bool bad, unsigned long long slot, int hdp) {
+// lane's row of the sequence and head; `slot`: its place in the parts; `progress` counts for the roles that wait.
+__device__ __noinline__ void repair_rows(const TileParams& tp, const Item& w, int i, int h, bool bad, unsigned long long slot, int hdp, int* progress) {
     const Params& p = tp.a;
     unsigned todo = __ballot_sync(0xffffffffu, bad);
     const int lane = threadIdx.x & 31;
@@ -374,7 +387,7 @@ __device__ __noinline__ void repair_rows(const TileParams& tp, const Item& w, in
         const unsigned long long rs = __shfl_sync(0xffffffffu, slot, from);
         const long long row = w.s.row0 + ri;
         const paged::View view = paged::row_view(p.mask_block, p.row_mask, w.s, ri);
-        const RowSum a = row_sum(p, w.seq, w.s.kv, w.kvh, p.q + row * p.q_ld + (long long)rh * p.head_dim, view, w.j0 * KEYS, w.j1 * KEYS);
+        const RowSum a = row_sum(p, w.seq, w.s.kv, w.kvh, p.q + row * p.q_ld + (long long)rh * p.head_dim, view, w.j0 * KEYS, w.j1 * KEYS, progress);
         const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -425,7 +438,7 @@ constexpr int STEP = 64;
 struct Listed {
     int index = 0;
     __device__ __forceinline__ bool get(Control& ctl, const TileParams& tp, Item& w) const {
-        if (!__all_sync(0xffffffffu, wait(&ctl.item_full[index % ITEMS], index / ITEMS & 1, tp.wait_limit, &ctl.abort_flag))) return false;
+        if (!__all_sync(0xffffffffu, wait(&ctl.item_full[index % ITEMS], index / ITEMS & 1, tp.wait_limit, &ctl.watch))) return false;
         w = ctl.items[index % ITEMS];
         return true;
     }
@@ -509,7 +522,7 @@ template <int HDP, int NH>
 __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl) {
     constexpr float FAR = 1048576.f, MOST = 1.2676506e30f;     // 2^20, 2^100
     const Params& p = tp.a;
-    volatile int* abort_flag = &ctl.abort_flag;
+    const volatile Watch* watch = &ctl.watch;
     const int half = threadIdx.x >> 7, r = threadIdx.x & 127;
     const uint32_t tmem = ctl.tmem_slot + ((uint32_t)(r & 96) << 16), to = tmem + 256 + half * HDP;
     const int ti = r / tp.gs, hi = r - ti * tp.gs;           // row of the half, head of the tile
@@ -532,7 +545,7 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
         const int end = w.j1 * KEYS, all_see = __reduce_min_sync(0xffffffffu, view.lim);
         for (int key = w.j0 * KEYS; key < end; key += STEP, ++steps) {
             const uint32_t buf = steps & 1;
-            if (!__all_sync(0xffffffffu, wait(&ctl.s_full[half][buf], steps >> 1 & 1, tp.wait_limit, abort_flag))) return false;
+            if (!__all_sync(0xffffffffu, wait(&ctl.s_full[half][buf], steps >> 1 & 1, tp.wait_limit, watch))) return false;
             if (any) {
                 tc_fence_after();
                 const uint32_t ts = tmem + half * 2 * STEP + buf * STEP;
@@ -544,7 +557,7 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
                     } else if (total > 512.f) {
                         alpha = raise_reference(m, l, total);
                     }
-                    if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][buf ^ 1], (steps - 1) >> 1 & 1, tp.wait_limit, abort_flag))) return false;      // the product before this one's
+                    if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][buf ^ 1], (steps - 1) >> 1 & 1, tp.wait_limit, watch))) return false;      // the product before this one's
                     tc_fence_after();
 #pragma unroll 1
                     for (int d = 0; d < HDP; d += 16) {
@@ -585,7 +598,7 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
             arrive(&ctl.p_full[half][buf]);
         }
         // ---- the item's end: divide, or leave a part ----
-        if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][1], (steps - 1) >> 1 & 1, tp.wait_limit, abort_flag))) return false;
+        if (!__all_sync(0xffffffffu, wait(&ctl.o_full[half][1], (steps - 1) >> 1 & 1, tp.wait_limit, watch))) return false;
         if (any) {
             tc_fence_after();
             const long long row = w.s.row0 + i;
@@ -643,7 +656,7 @@ __device__ __forceinline__ bool softmax_role(const TileParams& tp, Control& ctl)
             const bool bad = valid && !nan && !(max3_nan(check, check1, check1) < INFINITY);
             if (__any_sync(0xffffffffu, bad)) {
                 __syncwarp();
-                repair_rows(tp, w, i, h, bad, slot, HDP);
+                repair_rows(tp, w, i, h, bad, slot, HDP, &ctl.watch.progress);
             }
         }
     }
@@ -662,7 +675,7 @@ __device__ __forceinline__ bool query_role(const TileParams& tp, Control& ctl, u
 #pragma unroll
         for (int half = 0; half < NH; ++half) {
             if (!active<NH>(tp, w, half)) continue;
-            if (!__all_sync(0xffffffffu, wait(&ctl.q_empty[half], (items[half] & 1) ^ 1, tp.wait_limit, &ctl.abort_flag))) return false;
+            if (!__all_sync(0xffffffffu, wait(&ctl.q_empty[half], (items[half] & 1) ^ 1, tp.wait_limit, &ctl.watch))) return false;
             ++items[half];
             if (elect()) {
                 mbar_expect_tx(&ctl.q_full[half], (uint32_t)(tp.gs * tp.rows_half) * HDP * 2);
@@ -682,7 +695,7 @@ template <int HDP, int NH>
 __device__ __forceinline__ bool mma_role(const TileParams& tp, Control& ctl, uint8_t* q_tiles, uint8_t* ring, int half) {
     const Params& p = tp.a;
     constexpr int SB = KEYS * HDP * 2;
-    volatile int* abort_flag = &ctl.abort_flag;
+    const volatile Watch* watch = &ctl.watch;
     const int lane = threadIdx.x & 31;
     const uint32_t t_s = ctl.tmem_slot + half * 2 * STEP, t_o = ctl.tmem_slot + 256 + half * HDP;
     // D fp32, A and B bf16, M = 128; A K-major, B K-major (keys) or MN-major (values)
@@ -693,7 +706,7 @@ __device__ __forceinline__ bool mma_role(const TileParams& tp, Control& ctl, uin
     rv.next(tp.stages);
     uint32_t steps = 0, items = 0;                           // products, and items whose scores have begun, of this half
     auto all = [&](bool ok) { return __all_sync(0xffffffffu, ok); };
-    auto given = [&](uint64_t* bar, uint32_t parity) { return all(wait(bar, parity, tp.wait_limit, abort_flag)); };
+    auto given = [&](uint64_t* bar, uint32_t parity) { return all(wait(bar, parity, tp.wait_limit, watch)); };
     auto step = [&](Ring& r) {
         r.next(tp.stages);
         r.next(tp.stages);
@@ -804,7 +817,7 @@ __device__ __forceinline__ bool copy_role(const TileParams& tp, Control& ctl, ui
     Item w, next;
     auto publish = [&](int index, Item& x) {
         if (!next_item<NH>(tp, t, x)) x.j1 = 0;
-        if (!__all_sync(0xffffffffu, wait(&ctl.item_empty[index % ITEMS], (index / ITEMS & 1) ^ 1, tp.wait_limit, &ctl.abort_flag))) return false;
+        if (!__all_sync(0xffffffffu, wait(&ctl.item_empty[index % ITEMS], (index / ITEMS & 1) ^ 1, tp.wait_limit, &ctl.watch))) return false;
         if (lane == 0) {
             ctl.items[index % ITEMS] = x;
             arrive(&ctl.item_full[index % ITEMS]);
@@ -827,7 +840,7 @@ __device__ __forceinline__ bool copy_role(const TileParams& tp, Control& ctl, ui
             const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, some)) * box * HDP * 2;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
-                if (!__all_sync(0xffffffffu, wait(&ctl.empty[r.s], r.parity, tp.wait_limit, &ctl.abort_flag))) return false;
+                if (!__all_sync(0xffffffffu, wait(&ctl.empty[r.s], r.parity, tp.wait_limit, &ctl.watch))) return false;
                 __syncwarp();
                 if (!tp.withhold) {
                     if (lane == 0) mbar_expect_tx(&ctl.full[r.s], bytes);
@@ -863,7 +876,7 @@ tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
             mbar_init(&ctl.full[0] + i, count);
         }
         if (lane < 2 * ITEMS) ctl.bad[lane] = 0;
-        if (lane == 0) ctl.abort_flag = 0;
+        if (lane == 0) ctl.watch = Watch{0, 0};
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     } else if (warp == 4 * NH + 2) {
         tmem_alloc(&ctl.tmem_slot, 512);
@@ -882,10 +895,10 @@ tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
     else if (warp == 4 * NH) ok = copy_role<HDP, NH>(tp, ctl, ring, &map_k, &map_v);
     else if (warp == 4 * NH + 1) ok = query_role<HDP, NH>(tp, ctl, base, &map_q);
     else if (warp - 4 * NH - 2 < NH) ok = mma_role<HDP, NH>(tp, ctl, base, ring, warp - 4 * NH - 2);
-    if (!ok) *(volatile int*)&ctl.abort_flag = 1;
+    if (!ok) *(volatile int*)&ctl.watch.abort = 1;
     __syncwarp();
     __syncthreads();
-    const bool failed = *(volatile int*)&ctl.abort_flag;
+    const bool failed = *(volatile int*)&ctl.watch.abort;
     if (failed) settle();
     tc_fence_before();
     __syncthreads();
