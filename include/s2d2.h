@@ -515,7 +515,7 @@ typedef struct {
 } s2d2_rows;
 
 /* A paged cache of one layer in bf16.  Element e of token t of head h of page p is d_k[p * page_stride + h * head_stride +
- * t * token_stride + e], and the same of d_v: tokens of a head or heads of a token may be the neighbours, and keys and values may share a
+ * t * token_stride + e], and the same of d_v: pages, heads and tokens may lie inside one another in any order, and keys and values may share a
  * buffer.  d_k, d_v 16-byte aligned, strides multiples of 8, head_dim a multiple of 8; page_tokens a power of two, 8..S2D2_MAX_PAGE_TOKENS. */
 typedef struct {
     void* d_k;

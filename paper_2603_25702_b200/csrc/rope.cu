@@ -432,15 +432,17 @@ int check_kv(const char* op, const s2d2_paged_kv* c) {
     const long long t = c->token_stride, h = c->head_stride, g = c->page_stride, top = 1LL << 38;
     if (t % 8 || h % 8 || g % 8 || t < 1 || h < 1 || g < 1 || t > top || h > top || g > top)
         return fail(S2D2_ERR_INVALID, "%s: cache strides must be positive multiples of 8, at most 2^38", op);
-    // heads of a token or tokens of a head are the neighbours; nothing may lie on something else
-    const long long heads = c->n_kv_heads, tokens = c->page_tokens;
-    const bool token_inner = t >= c->head_dim && (heads == 1 || h >= t * (tokens - 1) + c->head_dim) && g >= h * (heads - 1) + t * (tokens - 1) + c->head_dim;
-    const bool head_inner = (heads == 1 || h >= c->head_dim) && t >= (heads == 1 ? 0 : h * (heads - 1)) + c->head_dim &&
-                            g >= t * (tokens - 1) + (heads == 1 ? 0 : h * (heads - 1)) + c->head_dim;
-    if (c->n_pages > 1 ? !(token_inner || head_inner)
-                       : !(t >= c->head_dim && (heads == 1 || h >= t * (tokens - 1) + c->head_dim)) &&
-                             !((heads == 1 || h >= c->head_dim) && t >= (heads == 1 ? 0 : h * (heads - 1)) + c->head_dim))
-        return fail(S2D2_ERR_INVALID, "%s: cache strides: elements overlap", op);
+    // Nothing may lie on something else: from the smallest stride on, each must be at least what lies inside of it (spans in 128 bits: they are up to 2^69)
+    struct Dim {
+        long long stride, size;
+    } dims[3] = {{t, c->page_tokens}, {h, c->n_kv_heads}, {g, c->n_pages}};
+    std::sort(dims, dims + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+    __int128 span = c->head_dim;
+    for (const Dim& d : dims) {
+        if (d.size == 1) continue;
+        if (d.stride < span) return fail(S2D2_ERR_INVALID, "%s: cache strides: elements overlap, or the dimensions do not nest", op);
+        span += (__int128)d.stride * (d.size - 1);
+    }
     return S2D2_OK;
 }
 
