@@ -371,7 +371,7 @@ def paged_attention(d_q: int, d_out: int, n_q_heads: int, rows: Rows, kv: PagedK
     width = n_q_heads * kv.head_dim
     _ops_check(lib.s2d2_paged_attention(d_q, _c64(width if q_stride is None else q_stride), d_out, _c64(width if out_stride is None else out_stride),
                                         d_lse, _c32(n_q_heads), rows, kv, _c32(mask_block), d_row_mask,
-                                        kv.head_dim ** -0.5 if scale is None else scale, d_ws, _c64(ws_bytes), stream))
+                                        max(kv.head_dim, 1) ** -0.5 if scale is None else scale, d_ws, _c64(ws_bytes), stream))
 
 
 def debug_mxfp4_wait(limit_polls: int, withhold: bool = False) -> None:

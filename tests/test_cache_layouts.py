@@ -66,3 +66,11 @@ def test_the_largest_strides_do_not_wrap(s2d2):
         with pytest.raises(s2d2.S2D2Error) as e:
             needs(s2d2, kv(s2d2, {"page": 1 << 38, "head": head, "token": 64}, sizes=big), 4)
         assert "overlap" in str(e.value)
+
+
+@pytest.mark.parametrize("dim", [0, -8, 2 ** 40, 12])
+def test_a_head_size_that_is_none_is_refused_like_any_other(s2d2, dim):
+    """With the scale that follows from it left out, too."""
+    with pytest.raises(s2d2.S2D2Error) as e:
+        s2d2.paged_attention(P, P, 6, s2d2.Rows(8, 2, P, P, P, 3), kv(s2d2, strides(("page", "head", "token"), 64), dim), P, 1 << 40)
+    assert e.value.code == -1 and "head_dim" in str(e.value)
