@@ -279,8 +279,9 @@ __device__ __forceinline__ void plan(const TileParams& tp, Setup& sh, Items& out
     units = __reduce_add_sync(0xffffffffu, units);
     out.left = 0;
     if (lane == 0) tp.split[2 * blockIdx.x] = make_int4(-1, 0, 0, 0), sh.first.left = 0;
-    // With few units per CTA every one of them counts more than an even spread of starts and ends
-    const uint32_t extra = (unsigned long long)units * heads > 4ull * tp.ctas ? 1 : 0;
+    // With less than a unit per CTA every one of them counts more than an even spread of starts and ends (tokens over 1222: 80 units 12.2 us without
+    // the extra, 12.4 with it; 160 units 13.4, 13.2; 320 16.5, 15.4; 800 21.3, 20.1; a ragged batch of 776 units 41.5, 31.0)
+    const uint32_t extra = (unsigned long long)units * heads > tp.ctas ? 1 : 0;
     const uint32_t total = (units + extra * items) * heads, ctas = min((uint32_t)tp.ctas, total), c = blockIdx.x;
     if (c >= ctas) return;
     // Rows of several sequences would be written by several CTAs, and the host's bound on the costs would not hold: such a list is not followed at all.
