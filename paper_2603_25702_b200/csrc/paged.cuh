@@ -85,10 +85,10 @@ __device__ __forceinline__ View row_view(int mask_block, const unsigned long lon
 }  // namespace paged
 
 namespace ops {
-// Checks of the structs and their device forms (paged.cu); `op` names the call.
+// Checks of the structs and their device forms (rope.cu); `op` names the call.
 int check_rows(const char* op, const s2d2_rows* r);                              // fields only
 int check_kv(const char* op, const s2d2_paged_kv* c);
-int device_rows(const Device* d, const char* op, const s2d2_rows* r, const s2d2_paged_kv* c, paged::Batch* out);     // and pointers
-int device_kv(const Device* d, const char* op, const s2d2_paged_kv* c, paged::Cache* out);
+int device_rows(const Device* d, const s2d2_rows* r, const s2d2_paged_kv* c, paged::Batch* out);     // and pointers
+int device_kv(const Device* d, const s2d2_paged_kv* c, paged::Cache* out);
 }  // namespace ops
 }  // namespace s2d2

@@ -135,8 +135,8 @@ extern "C" int s2d2_paged_attention(const void* d_q, int64_t q_stride, void* d_o
     if (!work) return S2D2_OK;
     patt::TileParams t = {};
     patt::Params& p = t.a;
-    if (int rc = ops::device_rows(dev, op, rows, kv, &p.b)) return rc;
-    if (int rc = ops::device_kv(dev, op, kv, &p.c)) return rc;
+    if (int rc = ops::device_rows(dev, rows, kv, &p.b)) return rc;
+    if (int rc = ops::device_kv(dev, kv, &p.c)) return rc;
     if (int rc = ops::check_ptr(dev, d_q, 16, "q")) return rc;
     if (int rc = ops::check_ptr(dev, d_out, 16, "out")) return rc;
     if (int rc = ops::check_ptr(dev, d_ws, 32, "workspace")) return rc;

@@ -360,10 +360,10 @@ int check_rope(const char* op, const s2d2_rope* r, int head_dim) {
 }
 
 template <bool APPEND>
-int launch_rope(const char* op, const ops::Device* dev, RopeParams& p, int dtype, bool out_vec, cudaStream_t st) {
+int launch_rope(const char* op, const ops::Device* dev, RopeParams& p, int dtype, cudaStream_t st) {
     const size_t size = dtype == S2D2_DTYPE_F32 ? 4 : 2;
     const int heads = p.q.heads + p.k.heads + (APPEND ? p.v.heads : 0);
-    bool vec = out_vec && p.head_dim % 16 == 0 && p.rot % 16 == 0;
+    bool vec = p.head_dim % 16 == 0 && p.rot % 16 == 0;
     for (const Mat* m : {&p.q, &p.k, &p.v})
         if (m->heads) {
             vec = vec && aligned(m->in, m->in_ld, size);
@@ -446,8 +446,7 @@ int check_kv(const char* op, const s2d2_paged_kv* c) {
     return S2D2_OK;
 }
 
-int device_rows(const Device* d, const char* op, const s2d2_rows* r, const s2d2_paged_kv* c, paged::Batch* out) {
-    (void)op;
+int device_rows(const Device* d, const s2d2_rows* r, const s2d2_paged_kv* c, paged::Batch* out) {
     if (int rc = check_ptr(d, r->d_row0, 4, "row0")) return rc;
     if (int rc = check_ptr(d, r->d_kv_len, 4, "kv_len")) return rc;
     if (r->max_pages)
@@ -465,8 +464,7 @@ int device_rows(const Device* d, const char* op, const s2d2_rows* r, const s2d2_
     return S2D2_OK;
 }
 
-int device_kv(const Device* d, const char* op, const s2d2_paged_kv* c, paged::Cache* out) {
-    (void)op;
+int device_kv(const Device* d, const s2d2_paged_kv* c, paged::Cache* out) {
     if (int rc = check_ptr(d, c->d_k, 16, "cache keys")) return rc;
     if (int rc = check_ptr(d, c->d_v, 16, "cache values")) return rc;
     out->k = (bf16*)c->d_k;
@@ -562,7 +560,7 @@ extern "C" int s2d2_qk_rope(const void* d_q, int64_t q_stride, void* d_q_out, in
         p.interleaved = rope->layout == S2D2_ROPE_INTERLEAVED;
         p.head_dim = head_dim;
         p.n_rows = n_rows;
-        return launch_rope<false>(op, dev, p, dtype, true, (cudaStream_t)cuda_stream);
+        return launch_rope<false>(op, dev, p, dtype, (cudaStream_t)cuda_stream);
     }
     return S2D2_OK;
 }
@@ -595,8 +593,8 @@ extern "C" int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, 
         if (int rc = check_mat(dev, op, "k", p.k, hd, size, 0)) return rc;
         if (int rc = check_mat(dev, op, "v", p.v, hd, size, 0)) return rc;
         if (!pass) continue;
-        if (int rc = ops::device_rows(dev, op, rows, kv, &p.b)) return rc;
-        if (int rc = ops::device_kv(dev, op, kv, &p.c)) return rc;
+        if (int rc = ops::device_rows(dev, rows, kv, &p.b)) return rc;
+        if (int rc = ops::device_kv(dev, kv, &p.c)) return rc;
         if (d_pos)
             if (int rc = ops::check_ptr(dev, d_pos, 4, "pos")) return rc;
         if (rope && rope->rot_dim)
@@ -611,7 +609,7 @@ extern "C" int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, 
         }
         p.head_dim = hd;
         p.n_rows = rows->n_rows;
-        return launch_rope<true>(op, dev, p, dtype, true, (cudaStream_t)cuda_stream);
+        return launch_rope<true>(op, dev, p, dtype, (cudaStream_t)cuda_stream);
     }
     return S2D2_OK;
 }
