@@ -87,7 +87,8 @@ class Rope(C.Structure):
 
 class Rows(C.Structure):
     """The rows (new tokens) of a batch: device pointers to row0 [n_seqs + 1], kv_len [n_seqs] and page lists [n_seqs, max_pages],
-    all int32 (semantics: include/s2d2.h).  ``max_rows``: most rows of a sequence, as far as the host knows (default: n_rows)."""
+    all int32 (semantics: include/s2d2.h).  ``max_rows``: most rows of a sequence, as far as the host knows.  Its default, n_rows, is right for every
+    batch, but paged_attention then takes single tokens of many sequences in the form for long chunks, slower and with one rounding more: give 1 for them."""
     _fields_ = [("d_row0", C.c_void_p), ("d_kv_len", C.c_void_p), ("d_pages", C.c_void_p), ("n_rows", C.c_int32), ("n_seqs", C.c_int32),
                 ("max_pages", C.c_int32), ("max_rows", C.c_int32)]
 
