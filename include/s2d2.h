@@ -543,12 +543,12 @@ int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_o
  *   d_row_mask given   (mask_block must be 0) all tokens in front of the sequence's rows, and row b < min(n, 64) of them if bit b of
  *                      d_row_mask[row] is set
  * A row that sees nothing (or only scores of -inf) gets 0 and lse -inf; keys and values that a row does not see have no influence on it, NaN
- * and infinities included.  Scores, sums and maxima are fp32; probabilities are rounded to bf16 for the product with the values.  Where
+ * and infinities included; a NaN or an infinity in a value that it sees makes that element one, however small the probability.  Scores, sums and maxima are fp32; probabilities are rounded to bf16 for the product with the values.  Where
  * max_rows * n_q_heads / n_kv_heads is at most 128 (a group of more than 128 heads counts in its largest parts up to 128 that divide it), those of the first
  * 32 of every 64 cache indices keep twice the bits.  Beside the output's own rounding (0.0017 of it, root mean square) that is an error of 0.0012 of it, otherwise
  * of 0.0017.  Rows that a NaN or an infinity among the values of their tiles touches, seen or not, and rows with a score beyond 2^20 or a jump of
  * more than 2^100 between probabilities of neighbouring keys are computed again key by key: right, but slow (a prompt of 4096
- * whose last value holds a NaN: 134 ms instead of 0.16).  A kv length that is not followed makes the sequence's rows NaN, a page that is not one the rows that see its tokens
+ * whose last value holds a NaN: 46 ms instead of 0.16).  A kv length that is not followed makes the sequence's rows NaN, a page that is not one the rows that see its tokens
  * (and rows next to them may become NaN, too).  n_rows is at most 2^22, max_pages * page_tokens and n_rows * n_q_heads / n_kv_heads at most 2^30; more than
  * 2e9 pairs of a tile of query vectors and a tile of 128 keys, by these bounds, is S2D2_ERR_UNSUPPORTED.
  * d_ws: at least s2d2_paged_attention_workspace bytes (they depend on the fields of the structs, not on what is on the device),

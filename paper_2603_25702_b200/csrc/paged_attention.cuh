@@ -35,8 +35,8 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
 }
 
 // Maximum (times scale_log2), sum and weighted values of one (row, head) over the keys [k0, k1), by a warp: a lane takes a key's
-// score, then every lane takes the elements lane, lane + 32, .. of the values.  Keys that are not seen are not read.  `progress` (shared memory)
-// goes up by one per 32 keys.
+// score, then every lane takes the elements lane, lane + 32, .. of the values.  Keys that are not seen are not read; a value that
+// is seen counts even if its probability is zero: NaN and infinities are not lost.  `progress` (shared memory) goes up by one per 32 keys.
 struct RowSum {
     float m, l, o[4];
 };
@@ -74,14 +74,34 @@ __device__ __forceinline__ RowSum row_sum(const Params& p, int seq, int kv, int 
         a.m = m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) a.o[i] *= shrink;
-        for (int t = 0; t < 32; ++t) {
-            const float w = __shfl_sync(0xffffffffu, e, t);
-            const long long from = __shfl_sync(0xffffffffu, at, t);
-            if (w == 0.f) continue;                      // not seen, or nothing
+        // eight keys' values on their way together; for a key that is not seen (weight 0) or has no page (weight NaN) those of one that is there
+        const unsigned there = __ballot_sync(0xffffffffu, at >= 0);
+        if (!there) continue;
+        const long long other = __shfl_sync(0xffffffffu, at, __ffs(there) - 1);
+#pragma unroll 1
+        for (int t0 = 0; t0 < 32; t0 += 8) {
+            float x[8][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (lane + 32 * i < p.head_dim) a.o[i] = from < 0 ? w : fmaf(w, to_f32(p.c.v[from + lane + 32 * i]), a.o[i]);
+            for (int t = 0; t < 8; ++t) {
+                const long long from = __shfl_sync(0xffffffffu, at, t0 + t);
+                const bf16* v = p.c.v + (from < 0 ? other : from);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float y = to_f32(v[min(lane + 32 * i, p.head_dim - 1)]);
+                    x[t][i] = from < 0 ? 0.f : y;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const float w = __shfl_sync(0xffffffffu, e, t0 + t);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a.o[i] = fmaf(w, x[t][i], a.o[i]);
+            }
         }
+    }
+    if (a.l == 0.f) {                                    // scores of -inf only
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.o[i] = 0.f;
     }
     return a;
 }
