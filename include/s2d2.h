@@ -527,8 +527,8 @@ typedef struct {
 
 /* Cache <- k (normed, rotated) and v [n_rows, n_kv_heads, head_dim] of the batch's rows, and q_out <- q normed and rotated (bf16; d_q NULL or n_q_heads 0:
  * none).  Inputs of dtype S2D2_DTYPE_*, layout as in s2d2_qk_rope.  Position of a row: d_pos[row], or its cache index (d_pos NULL).
- * rope NULL: no norm, no rotation.  A row whose cache index is negative, or whose page is not one, is not written to the cache (its q_out
- * is).  Two rows must not have the same place in the cache. */
+ * rope NULL: no norm, no rotation.  A row whose cache index is negative, whose sequence has a kv length that is not followed, or whose
+ * page is not one, is not written to the cache (its q_out is).  Two rows must not have the same place in the cache. */
 int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride, int32_t n_q_heads, const void* d_k,
                    int64_t k_stride, const void* d_v, int64_t v_stride, int32_t dtype, const int32_t* d_pos, const s2d2_rope* rope,
                    const s2d2_rows* rows, const s2d2_paged_kv* kv, void* cuda_stream);
@@ -548,7 +548,7 @@ int s2d2_kv_append(const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_o
  * 32 of every 64 cache indices keep twice the bits.  Beside the output's own rounding (0.0017 of it, root mean square) that is an error of 0.0012 of it, otherwise
  * of 0.0017.  Rows that a NaN or an infinity among the values of their tiles touches, seen or not, and rows with a score beyond 2^20 or a jump of
  * more than 2^100 between probabilities of neighbouring keys are computed again key by key: right, but slow (a prompt of 4096
- * whose last value holds a NaN: 46 ms instead of 0.16).  A kv length that is not followed makes the sequence's rows NaN, a page that is not one the rows that see its tokens
+ * whose last value holds a NaN: 45 ms instead of 0.16).  A kv length that is not followed makes the sequence's rows NaN, a page that is not one the rows that see its tokens
  * (and rows next to them may become NaN, too).  n_rows is at most 2^22, max_pages * page_tokens and n_rows * n_q_heads / n_kv_heads at most 2^30; more than
  * 2e9 pairs of a tile of query vectors and a tile of 128 keys, by these bounds, is S2D2_ERR_UNSUPPORTED.
  * d_ws: at least s2d2_paged_attention_workspace bytes (they depend on the fields of the structs, not on what is on the device),

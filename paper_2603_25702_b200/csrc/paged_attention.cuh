@@ -74,15 +74,15 @@ __device__ __forceinline__ RowSum row_sum(const Params& p, int seq, int kv, int 
         a.m = m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) a.o[i] *= shrink;
-        // eight keys' values on their way together; for a key that is not seen (weight 0) or has no page (weight NaN) those of one that is there
+        // four keys' values on their way together (with eight, 164 registers leave the join's blocks no room beside the tiles); for a key that is not seen (weight 0) or has no page (weight NaN) those of one that is there
         const unsigned there = __ballot_sync(0xffffffffu, at >= 0);
         if (!there) continue;
         const long long other = __shfl_sync(0xffffffffu, at, __ffs(there) - 1);
 #pragma unroll 1
-        for (int t0 = 0; t0 < 32; t0 += 8) {
-            float x[8][4];
+        for (int t0 = 0; t0 < 32; t0 += 4) {
+            float x[4][4];
 #pragma unroll
-            for (int t = 0; t < 8; ++t) {
+            for (int t = 0; t < 4; ++t) {
                 const long long from = __shfl_sync(0xffffffffu, at, t0 + t);
                 const bf16* v = p.c.v + (from < 0 ? other : from);
 #pragma unroll
@@ -92,7 +92,7 @@ __device__ __forceinline__ RowSum row_sum(const Params& p, int seq, int kv, int 
                 }
             }
 #pragma unroll
-            for (int t = 0; t < 8; ++t) {
+            for (int t = 0; t < 4; ++t) {
                 const float w = __shfl_sync(0xffffffffu, e, t0 + t);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) a.o[i] = fmaf(w, x[t][i], a.o[i]);
